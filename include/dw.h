@@ -281,6 +281,41 @@ int dw_draw_batch(dw_handle* h, const void* d_data, const int32_t* d_labels, int
                   int64_t m, uint64_t seed, const uint8_t* h_active, void* d_x, int32_t* d_y, void* stream);
 
 /*
+ * Operators for training steps that the caller puts together: a language model's layers and loss in front of
+ * dw_update_only.  All of them work for k worker replicas at once (1 <= k <= DW_MAX_K, each with its own parameters) and
+ * need no handle; the conventions above hold (caller's memory and stream, nothing allocated, nothing synchronised).
+ * A matrix argument is d_p, ld, stride: element j of row r of worker w is d_p[w*stride + r*ld + j].  Rows are contiguous
+ * and may start at any multiple of the element size; ld >= row length; the stride of an input may be 0 (shared by the
+ * workers).  Outputs overlap neither each other nor an input, unless a call says so.  dtype is DW_F32 or DW_BF16; sums are
+ * kept in fp32 or more and results do not depend on the order in which blocks run.
+ * Scratch is device memory, 256-byte aligned, of the bytes that the call's own function gives (0: none is needed, it may
+ * be NULL); its contents need not be kept from one call to the next.
+ */
+
+/*
+ * Layer norm of rows of n:  y = (x - mu) r gamma + beta,  mu = mean(x),  r = 1/sqrt(mean((x - mu)^2) + eps).
+ *   d_gamma, d_beta   [k] rows of n floats, worker w's at w*param_stride; NULL: 1 and 0
+ *   d_mean, d_rstd    [k][rows] floats receiving mu and r for the backward pass; either may be NULL
+ * rows >= 0, 1 <= n <= DW_MAX_NORM, eps >= 0.
+ */
+#define DW_MAX_NORM (1 << 24)
+int dw_layer_norm(const void* d_x, int64_t x_ld, int64_t x_stride, const float* d_gamma, const float* d_beta,
+                  int64_t param_stride, int k, int64_t rows, int64_t n, int dtype, float eps, void* d_y, int64_t y_ld,
+                  int64_t y_stride, float* d_mean, float* d_rstd, void* stream);
+
+/*
+ * Its backward pass.  With h = (x - mu) r and a = dy gamma:
+ *   dx = r (a - mean(a) - h mean(a h)),  dgamma = sum over the worker's rows of dy h,  dbeta = sum of dy
+ *   d_mean, d_rstd      as dw_layer_norm left them
+ *   d_dx                may be NULL; so may d_dgamma and d_dbeta ([k] rows of n floats at w*grad_stride, overwritten)
+ */
+size_t dw_layer_norm_grad_scratch_bytes(int k, int64_t rows, int64_t n, int dtype);
+int dw_layer_norm_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const void* d_x, int64_t x_ld, int64_t x_stride,
+                       const float* d_gamma, int64_t param_stride, const float* d_mean, const float* d_rstd, int k,
+                       int64_t rows, int64_t n, int dtype, void* d_dx, int64_t dx_ld, int64_t dx_stride, float* d_dgamma,
+                       float* d_dbeta, int64_t grad_stride, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Per-kernel timing for benchmarks (not part of the method).  While enabled, every kernel the handle launches
  * is bracketed by two HIP events on the caller's stream.  dw_profile_read synchronises the stream and returns,
  * per kernel class, the number of launches and their summed duration in milliseconds since the last read

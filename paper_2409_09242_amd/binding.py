@@ -28,7 +28,7 @@ DW_S_ACT = 16
 EXPORTS = ("dw_strerror", "dw_last_hip_error", "dw_param_count", "dw_workspace_bytes", "dw_init", "dw_destroy",
            "dw_worker_step", "dw_update_only", "dw_elastic_sync", "dw_get_state", "dw_set_state",
            "dw_profile", "dw_profile_read", "dw_partition_scratch_bytes", "dw_overlap_partition", "dw_draw_batch",
-           "dw_overlap_partition_static")
+           "dw_overlap_partition_static", "dw_layer_norm", "dw_layer_norm_grad_scratch_bytes", "dw_layer_norm_grad")
 KERNEL_CLASSES = ("rademacher", "gemm_fwd", "head", "gemm_wgrad", "gemm_dgrad", "update", "weights", "pull", "gather", "step")
 
 
@@ -87,6 +87,14 @@ def lib() -> C.CDLL:
     L.dw_overlap_partition_static.argtypes = [i64, i64, i32, C.c_uint64, vp, vp]
     L.dw_draw_batch.restype = i32
     L.dw_draw_batch.argtypes = [vp, vp, vp, i64, vp, i64, C.c_uint64, vp, vp, vp, vp]
+    f32, sz = C.c_float, C.c_size_t
+    L.dw_layer_norm.restype = i32
+    L.dw_layer_norm.argtypes = [vp, i64, i64, vp, vp, i64, i32, i64, i64, i32, f32, vp, i64, i64, vp, vp, vp]
+    L.dw_layer_norm_grad_scratch_bytes.restype = sz
+    L.dw_layer_norm_grad_scratch_bytes.argtypes = [i32, i64, i64, i32]
+    L.dw_layer_norm_grad.restype = i32
+    L.dw_layer_norm_grad.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, vp, vp, i32, i64, i64, i32, vp, i64, i64, vp, vp,
+                                     i64, vp, sz, vp]
     _LIB = L
     return L
 

@@ -1,0 +1,144 @@
+// Internal declarations shared by the operators for training steps that the caller puts together (layer norm, 8-bit
+// block products, policy loss, gradient clipping): loads and stores of rows, reductions, argument checks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "dw_internal.h"
+
+namespace dw {
+
+constexpr int kCus = 256;             // compute units: grids are sized in multiples of it
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// 16 bytes at an address that is aligned to the element only: global memory takes such loads and stores whole, so a row
+// that starts anywhere costs the lines it touches and no variant of its own
+struct __attribute__((packed, aligned(2))) Raw16a2 { uint32_t w[4]; };
+struct __attribute__((packed, aligned(4))) Raw16a4 { uint32_t w[4]; };
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {       // round to nearest even, NaN stays NaN
+  const f32x2_t f = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
+}
+
+// a row element type: V elements fill 16 bytes
+struct F32 {
+  typedef float T;
+  static constexpr int V = 4;
+  __device__ static __forceinline__ void unpack(const uint32_t (&r)[4], float (&f)[V]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(r[j]);
+  }
+  __device__ static __forceinline__ void pack(const float (&f)[V], uint32_t (&r)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = __float_as_uint(f[j]);
+  }
+  __device__ static __forceinline__ float one(const T* p) { return *p; }
+  __device__ static __forceinline__ void put(T* p, float f) { *p = f; }
+  typedef Raw16a4 Raw;
+};
+struct Bf16 {
+  typedef uint16_t T;
+  static constexpr int V = 8;
+  __device__ static __forceinline__ void unpack(const uint32_t (&r)[4], float (&f)[V]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f[2 * j] = __uint_as_float(r[j] << 16);
+      f[2 * j + 1] = __uint_as_float(r[j] & 0xFFFF0000u);
+    }
+  }
+  __device__ static __forceinline__ void pack(const float (&f)[V], uint32_t (&r)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = pack_bf16(f[2 * j], f[2 * j + 1]);
+  }
+  __device__ static __forceinline__ float one(const T* p) { return __uint_as_float((uint32_t)*p << 16); }
+  __device__ static __forceinline__ void put(T* p, float f) { *p = (uint16_t)pack_bf16(f, 0.f); }
+  typedef Raw16a2 Raw;
+};
+
+// the 16 bytes of elements e0 .. e0+V-1 of a row of n; elements at n and beyond read as zero
+template <class E>
+__device__ __forceinline__ void load16(const typename E::T* row, int64_t e0, int64_t n, uint32_t (&r)[4]) {
+  if (e0 + E::V <= n) {
+    const typename E::Raw v = *reinterpret_cast<const typename E::Raw*>(row + e0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = v.w[j];
+  } else {
+    float f[E::V];
+#pragma unroll
+    for (int j = 0; j < E::V; ++j) f[j] = e0 + j < n ? E::one(row + e0 + j) : 0.f;
+    E::pack(f, r);
+  }
+}
+template <class E>
+__device__ __forceinline__ void store16(typename E::T* row, int64_t e0, int64_t n, const float (&f)[E::V]) {
+  if (e0 + E::V <= n) {
+    typename E::Raw v;
+    E::pack(f, v.w);
+    *reinterpret_cast<typename E::Raw*>(row + e0) = v;
+  } else {
+#pragma unroll
+    for (int j = 0; j < E::V; ++j)
+      if (e0 + j < n) E::put(row + e0 + j, f[j]);
+  }
+}
+// V floats of a parameter row (4-byte aligned)
+template <int V>
+__device__ __forceinline__ void load_floats(const float* row, int64_t e0, int64_t n, float fill, float (&f)[V]) {
+  if (e0 + V <= n) {
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+      const Raw16a4 v = *reinterpret_cast<const Raw16a4*>(row + e0 + 4 * q);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[4 * q + j] = __uint_as_float(v.w[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = e0 + j < n ? row[e0 + j] : fill;
+  }
+}
+
+// sum over the TPR consecutive threads that share a row, to all of them; TPR > 64: the whole block of TPR threads
+// (`lds`: 2 * TPR/64 floats; `turn` alternates between calls so that one barrier a call is enough)
+template <int TPR>
+__device__ __forceinline__ float row_sum(float x, float* lds, int& turn) {
+#pragma unroll
+  for (int off = 1; off < (TPR < 64 ? TPR : 64); off <<= 1) x += __shfl_xor(x, off);
+  if constexpr (TPR > 64) {
+    constexpr int W = TPR / 64;
+    float* at = lds + turn * W;
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = at[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) x += at[w];
+  }
+  return x;
+}
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ---- layer norm (dw_norm.hip) ----------------------------------------------------------------------------------------
+struct Rows { const void* p; int64_t ld, stride; };        // element (w, r, j) at p + w*stride + r*ld + j, in elements
+struct RowsOut { void* p; int64_t ld, stride; };
+
+struct NormArgs {
+  Rows x, dy;
+  RowsOut out;                                             // y, or dx
+  const float* gamma; const float* beta; int64_t param_stride;
+  float* mean; float* rstd;                                // [k][rows]
+  float* dgamma; float* dbeta; int64_t grad_stride;
+  float* part;                                             // backward: [k][strips][2][n]
+  int k, strips;
+  int64_t rows, n;
+  float eps;
+};
+hipError_t launch_layer_norm(const NormArgs& a, int dtype, hipStream_t s);
+hipError_t launch_layer_norm_grad(const NormArgs& a, bool sums, int dtype, hipStream_t s);
+int layer_norm_grad_strips(int k, int64_t rows, int64_t n, int dtype);
+
+}  // namespace dw

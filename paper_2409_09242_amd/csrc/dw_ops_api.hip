@@ -1,0 +1,103 @@
+// Host side of the operators for training steps that the caller puts together: argument checks and the order of their launches.  Nothing is
+// enqueued when an argument is refused.
+#include <cmath>
+
+#include "dw_ops.h"
+
+using namespace dw;
+
+namespace {
+
+#define DW_HIP(expr)                                          \
+  do {                                                        \
+    hipError_t e__ = (expr);                                  \
+    if (e__ != hipSuccess) return note_hip_error(e__);        \
+  } while (0)
+
+inline bool is_type(int dtype) { return dtype == DW_F32 || dtype == DW_BF16; }
+inline int64_t type_bytes(int dtype) { return dtype == DW_BF16 ? 2 : 4; }
+inline bool aligned(const void* p, int64_t a) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(a - 1)) == 0; }
+
+constexpr int64_t kMaxRows = 1ll << 31;                     // rows of a worker
+constexpr int64_t kMaxStride = 1ll << 48;                   // elements: a byte offset stays in 64 bits for every worker
+
+// rows of n at p that are only read
+inline bool in_ok(const void* p, int64_t ld, int64_t stride, int64_t rows, int64_t n, int64_t bytes) {
+  return aligned(p, bytes) && (rows <= 1 || ld >= n) && ld >= 0 && ld <= kMaxStride / (rows > 0 ? rows : 1) && stride >= 0 && stride <= kMaxStride;
+}
+// rows that are written: no two of them share an element
+inline bool out_ok(const void* p, int64_t ld, int64_t stride, int k, int64_t rows, int64_t n, int64_t bytes) {
+  return in_ok(p, ld, stride, rows, n, bytes) && (k == 1 || rows == 0 || stride >= (rows - 1) * ld + n);
+}
+inline bool params_ok(const float* p, int64_t stride) { return aligned(p, 4) && stride >= 0 && stride <= kMaxStride; }
+inline bool grads_ok(const float* p, int64_t stride, int k, int64_t n) { return params_ok(p, stride) && (k == 1 || stride >= n); }
+
+inline bool norm_shape_ok(int k, int64_t rows, int64_t n) {
+  return rows >= 0 && rows < kMaxRows && n >= 1 && n <= DW_MAX_NORM;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dw_layer_norm(const void* d_x, int64_t x_ld, int64_t x_stride, const float* d_gamma, const float* d_beta,
+                  int64_t param_stride, int k, int64_t rows, int64_t n, int dtype, float eps, void* d_y, int64_t y_ld,
+                  int64_t y_stride, float* d_mean, float* d_rstd, void* stream) {
+  if (k < 1 || k > DW_MAX_K || !is_type(dtype)) return DW_ERR_CONFIG;
+  if (!norm_shape_ok(k, rows, n)) return DW_ERR_ARG;
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return DW_ERR_HYPER;
+  if (rows == 0) return DW_OK;
+  if (!d_x || !d_y) return DW_ERR_NULL;
+  const int64_t b = type_bytes(dtype);
+  if (d_y == d_x || !in_ok(d_x, x_ld, x_stride, rows, n, b) || !out_ok(d_y, y_ld, y_stride, k, rows, n, b)) return DW_ERR_ARG;
+  if (!params_ok(d_gamma, param_stride) || !params_ok(d_beta, param_stride)) return DW_ERR_ARG;
+  if (!aligned(d_mean, 4) || !aligned(d_rstd, 4)) return DW_ERR_ARG;
+  NormArgs a = {};
+  a.x = {d_x, x_ld, x_stride};
+  a.out = {d_y, y_ld, y_stride};
+  a.gamma = d_gamma; a.beta = d_beta; a.param_stride = param_stride;
+  a.mean = d_mean; a.rstd = d_rstd;
+  a.k = k; a.rows = rows; a.n = n; a.eps = eps;
+  DW_HIP(launch_layer_norm(a, dtype, (hipStream_t)stream));
+  return DW_OK;
+}
+
+size_t dw_layer_norm_grad_scratch_bytes(int k, int64_t rows, int64_t n, int dtype) {
+  if (k < 1 || k > DW_MAX_K || !is_type(dtype) || !norm_shape_ok(k, rows, n)) return 0;
+  return (size_t)k * layer_norm_grad_strips(k, rows, n, dtype) * 2 * n * sizeof(float);
+}
+
+int dw_layer_norm_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const void* d_x, int64_t x_ld, int64_t x_stride,
+                       const float* d_gamma, int64_t param_stride, const float* d_mean, const float* d_rstd, int k,
+                       int64_t rows, int64_t n, int dtype, void* d_dx, int64_t dx_ld, int64_t dx_stride, float* d_dgamma,
+                       float* d_dbeta, int64_t grad_stride, void* d_scratch, size_t scratch_bytes, void* stream) {
+  if (k < 1 || k > DW_MAX_K || !is_type(dtype)) return DW_ERR_CONFIG;
+  if (!norm_shape_ok(k, rows, n)) return DW_ERR_ARG;
+  const bool sums = d_dgamma || d_dbeta;
+  if (!d_dx && !sums) return DW_OK;
+  if (sums && (!grads_ok(d_dgamma, grad_stride, k, n) || !grads_ok(d_dbeta, grad_stride, k, n) || d_dgamma == d_dbeta)) return DW_ERR_ARG;
+  if (rows == 0 && !sums) return DW_OK;
+  const int64_t b = type_bytes(dtype);
+  if (rows > 0) {
+    if (!d_dy || !d_x || !d_mean || !d_rstd) return DW_ERR_NULL;
+    if (!in_ok(d_dy, dy_ld, dy_stride, rows, n, b) || !in_ok(d_x, x_ld, x_stride, rows, n, b)) return DW_ERR_ARG;
+    if (d_dx && (d_dx == d_dy || d_dx == d_x || !out_ok(d_dx, dx_ld, dx_stride, k, rows, n, b))) return DW_ERR_ARG;
+    if (!params_ok(d_gamma, param_stride) || !aligned(d_mean, 4) || !aligned(d_rstd, 4)) return DW_ERR_ARG;
+    if (sums && (!d_scratch || !aligned(d_scratch, 256) || scratch_bytes < dw_layer_norm_grad_scratch_bytes(k, rows, n, dtype)))
+      return DW_ERR_WORKSPACE;
+  }
+  NormArgs a = {};
+  a.x = {d_x, x_ld, x_stride};
+  a.dy = {d_dy, dy_ld, dy_stride};
+  a.out = {d_dx, dx_ld, dx_stride};
+  a.gamma = d_gamma; a.param_stride = param_stride;
+  a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
+  a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.grad_stride = grad_stride;
+  a.part = sums ? static_cast<float*>(d_scratch) : nullptr;
+  a.k = k; a.rows = rows; a.n = n;
+  a.strips = layer_norm_grad_strips(k, rows, n, dtype);
+  DW_HIP(launch_layer_norm_grad(a, sums, dtype, (hipStream_t)stream));
+  return DW_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,152 @@
+"""Operators of a language model's training step on the GPU, for k worker replicas in one call: thin wrappers over the
+library's handle-free entry points (include/dw.h).
+
+Tensors of activations are [k][rows][n] with contiguous rows (any row and worker stride, so views of wider buffers do),
+float32 or bfloat16; parameters and their gradients are float32.  Outputs and scratch are allocated by torch on the
+current stream of the tensors' device, where the work is enqueued; nothing is synchronised.  As with any torch operator,
+a tensor made on another stream has to be waited for, and recorded, by the caller.  Wrong shapes, types or layouts raise
+ValueError, what the library refuses DwError; there is no CPU path.
+"""
+from __future__ import annotations
+
+import contextlib
+from typing import Optional, Tuple
+
+import torch
+
+from . import binding as B
+
+_TYPES = {torch.float32: B.DW_F32, torch.bfloat16: B.DW_BF16}
+_NO_GUARD = contextlib.nullcontext()
+
+
+def _check(status: int, where: str) -> None:
+    if status < 0:
+        raise B.DwError(int(status), where)
+
+
+def _type(t: torch.Tensor, name: str) -> int:
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise ValueError("%s has type %s: float32 or bfloat16 is wanted" % (name, t.dtype))
+    return code
+
+
+def _on(device: torch.device):
+    """The stream to enqueue on, and a guard for the case that the tensors' device is not the current one."""
+    if device.type != "cuda":
+        raise ValueError("tensors on a GPU are wanted: got %s" % device)
+    stream = torch.cuda.current_stream(device).cuda_stream
+    return stream, (_NO_GUARD if device.index == torch.cuda.current_device() else torch.cuda.device(device))
+
+
+def _matrix(t: torch.Tensor, name: str, shape=None, dtype=None, device=None) -> Tuple[int, int, int]:
+    """(address, row stride, worker stride) of a [k][rows][n] tensor."""
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise ValueError("%s has shape %s: %s is wanted" % (name, tuple(t.shape), "[k][rows][n]" if shape is None else tuple(shape)))
+    if (dtype is not None and t.dtype != dtype) or (device is not None and t.device != device):
+        raise ValueError("%s is %s on %s: %s on %s is wanted" % (name, t.dtype, t.device, dtype or t.dtype, device or t.device))
+    k, rows, n = t.shape
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and n > 1:
+        raise ValueError("the rows of %s are not contiguous" % name)
+    if rows <= 1:
+        s1 = n
+    return t.data_ptr(), s1, (rows * s1 if k <= 1 else s0)
+
+
+def _param(t: Optional[torch.Tensor], name: str, k: int, n: int, device) -> Tuple[Optional[int], int]:
+    """(address, worker stride) of a float32 [k][n] tensor, such as a view of flat parameter vectors."""
+    if t is None:
+        return None, n
+    if t.shape != (k, n) or t.dtype != torch.float32 or t.device != device:
+        raise ValueError("%s is %s %s on %s: float32 [%d][%d] on %s is wanted" % (name, t.dtype, tuple(t.shape), t.device, k, n, device))
+    if n > 1 and t.stride(1) != 1:
+        raise ValueError("the rows of %s are not contiguous" % name)
+    return t.data_ptr(), (n if k == 1 else t.stride(0))
+
+
+def _values(t: Optional[torch.Tensor], name: str, shape, dtype, device) -> Optional[int]:
+    """Address of a contiguous tensor of that shape and type."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError("%s is %s %s on %s: a contiguous %s %s on %s is wanted" % (
+            name, t.dtype, tuple(t.shape), t.device, dtype, tuple(shape), device))
+    return t.data_ptr()
+
+
+def _scratch(nbytes: int, device) -> Tuple[Optional[torch.Tensor], Optional[int]]:
+    """Scratch memory (torch's allocations start at multiples of 256 and more) that lives until the work on the current
+    stream that was enqueued with it is done."""
+    if nbytes == 0:
+        return None, None
+    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if t.data_ptr() % 256:
+        t = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+    return t, (t.data_ptr() + 255) // 256 * 256
+
+
+# ---- layer norm ------------------------------------------------------------------------------------------------------
+
+def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, out=None, stats: bool = True):
+    """y = (x - mean) * rstd * gamma + beta over the last axis of x [k][rows][n]; gamma, beta: float32 [k][n] or None.
+
+    Returns (y, mean, rstd), the latter float32 [k][rows] for layer_norm_grad, or None both with stats=False (a served
+    model).  out: a tensor like x for y."""
+    code = _type(x, "x")
+    xp, x_ld, x_st = _matrix(x, "x")
+    k, rows, n = x.shape
+    dev = x.device
+    stream, guard = _on(dev)
+    if gamma is not None and beta is not None and k > 1 and gamma.stride(0) != beta.stride(0):
+        raise ValueError("gamma and beta have different worker strides")
+    gp, p_st = _param(gamma, "gamma", k, n, dev)
+    bp, b_st = _param(beta, "beta", k, n, dev)
+    if out is None:
+        out = torch.empty((k, rows, n), dtype=x.dtype, device=dev)
+    yp, y_ld, y_st = _matrix(out, "out", x.shape, x.dtype, dev)
+    mean = torch.empty((k, rows), dtype=torch.float32, device=dev) if stats else None
+    rstd = torch.empty((k, rows), dtype=torch.float32, device=dev) if stats else None
+    with guard:
+        _check(B.lib().dw_layer_norm(xp, x_ld, x_st, gp, bp, p_st if gp is not None else b_st, k, rows, n, code, eps, yp, y_ld,
+                                     y_st, mean.data_ptr() if stats else None, rstd.data_ptr() if stats else None, stream),
+               "dw_layer_norm")
+    return out, mean, rstd
+
+
+def layer_norm_grad(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, want_dx: bool = True, want_params: bool = True):
+    """(dx, dgamma, dbeta) of layer_norm from dy, its input and the statistics it returned.  dx, dgamma, dbeta: tensors to
+    write into (float32 [k][n] for the latter two, such as views of the flat gradient of Handle.update_only); what is not
+    wanted is returned as None."""
+    code = _type(x, "x")
+    xp, x_ld, x_st = _matrix(x, "x")
+    k, rows, n = x.shape
+    dev = x.device
+    stream, guard = _on(dev)
+    dyp, dy_ld, dy_st = _matrix(dy, "dy", x.shape, x.dtype, dev)
+    gp, p_st = _param(gamma, "gamma", k, n, dev)
+    mp = _values(mean, "mean", (k, rows), torch.float32, dev)
+    rp = _values(rstd, "rstd", (k, rows), torch.float32, dev)
+    dxp, dx_ld, dx_st = None, n, rows * n
+    if want_dx:
+        if dx is None:
+            dx = torch.empty((k, rows, n), dtype=x.dtype, device=dev)
+        dxp, dx_ld, dx_st = _matrix(dx, "dx", x.shape, x.dtype, dev)
+    dgp = dbp = scratch = sp = None
+    g_st, nbytes = n, 0
+    if want_params:
+        if dgamma is None:
+            dgamma = torch.empty((k, n), dtype=torch.float32, device=dev)
+        if dbeta is None:
+            dbeta = torch.empty((k, n), dtype=torch.float32, device=dev)
+        dgp, g_st = _param(dgamma, "dgamma", k, n, dev)
+        dbp, b_st = _param(dbeta, "dbeta", k, n, dev)
+        if b_st != g_st:
+            raise ValueError("dgamma and dbeta have different worker strides")
+        nbytes = B.lib().dw_layer_norm_grad_scratch_bytes(k, rows, n, code)
+        scratch, sp = _scratch(nbytes, dev)
+    with guard:
+        _check(B.lib().dw_layer_norm_grad(dyp, dy_ld, dy_st, xp, x_ld, x_st, gp, p_st, mp, rp, k, rows, n, code, dxp, dx_ld,
+                                          dx_st, dgp, dbp, g_st, sp, nbytes, stream), "dw_layer_norm_grad")
+    return (dx if want_dx else None), (dgamma if want_params else None), (dbeta if want_params else None)
