@@ -316,6 +316,33 @@ int dw_layer_norm_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const
                        float* d_dbeta, int64_t grad_stride, void* d_scratch, size_t scratch_bytes, void* stream);
 
 /*
+ * Log probability of the chosen token of every row of logits: d_logp[w][r] = z_y - log sum_j exp(z_j), y = d_target[w][r]
+ * (both [k][rows], contiguous).  A target outside [0, vocab) gives 0, a row of -inf alone -inf.
+ */
+#define DW_MAX_VOCAB (1 << 24)
+int dw_token_logp(const void* d_logits, int64_t ld, int64_t stride, const int32_t* d_target, int k, int64_t rows,
+                  int64_t vocab, int dtype, float* d_logp, void* stream);
+
+/*
+ * Clipped policy loss with a KL term, and its gradient.  For a row with lp as above, q = exp(lp - old):
+ *   l = -min(q A, clip(q, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(ref - lp) - (ref - lp) - 1)
+ *   loss of a worker = sum over its rows of weight l,    grad_j = weight dl/dlp ([j = y] - softmax(z)_j)
+ * (where both terms of the minimum are equal the derivative is that of q A).
+ *   d_old_logp, d_ref_logp, d_advantage   [k][rows] floats; d_ref_logp may be NULL when kl_coef is 0
+ *   d_weight    [k][rows] floats, the mask and the average in one: 0 = the row is not read, adds nothing and has gradient 0
+ *               and log probability 0, as has a row whose target lies outside [0, vocab); NULL: 1/rows each
+ *   d_loss      [k] floats; d_logp [k][rows] floats; d_grad logits' type; each may be NULL.  d_grad may be d_logits itself
+ *               with the same ld and stride.
+ * A row of -inf alone has no token to choose: log probability -inf, no loss, gradient 0.
+ * 0 <= clip_low <= 1, 0 <= clip_high.
+ */
+size_t dw_policy_loss_scratch_bytes(int k, int64_t rows);
+int dw_policy_loss(const void* d_logits, int64_t ld, int64_t stride, const int32_t* d_target, const float* d_old_logp,
+                   const float* d_ref_logp, const float* d_advantage, const float* d_weight, int k, int64_t rows,
+                   int64_t vocab, int dtype, float clip_low, float clip_high, float kl_coef, float* d_loss, float* d_logp,
+                   void* d_grad, int64_t grad_ld, int64_t grad_stride, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Per-kernel timing for benchmarks (not part of the method).  While enabled, every kernel the handle launches
  * is bracketed by two HIP events on the caller's stream.  dw_profile_read synchronises the stream and returns,
  * per kernel class, the number of launches and their summed duration in milliseconds since the last read

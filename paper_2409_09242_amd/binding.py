@@ -28,7 +28,8 @@ DW_S_ACT = 16
 EXPORTS = ("dw_strerror", "dw_last_hip_error", "dw_param_count", "dw_workspace_bytes", "dw_init", "dw_destroy",
            "dw_worker_step", "dw_update_only", "dw_elastic_sync", "dw_get_state", "dw_set_state",
            "dw_profile", "dw_profile_read", "dw_partition_scratch_bytes", "dw_overlap_partition", "dw_draw_batch",
-           "dw_overlap_partition_static", "dw_layer_norm", "dw_layer_norm_grad_scratch_bytes", "dw_layer_norm_grad")
+           "dw_overlap_partition_static", "dw_layer_norm", "dw_layer_norm_grad_scratch_bytes", "dw_layer_norm_grad",
+           "dw_token_logp", "dw_policy_loss_scratch_bytes", "dw_policy_loss")
 KERNEL_CLASSES = ("rademacher", "gemm_fwd", "head", "gemm_wgrad", "gemm_dgrad", "update", "weights", "pull", "gather", "step")
 
 
@@ -95,6 +96,13 @@ def lib() -> C.CDLL:
     L.dw_layer_norm_grad.restype = i32
     L.dw_layer_norm_grad.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, vp, vp, i32, i64, i64, i32, vp, i64, i64, vp, vp,
                                      i64, vp, sz, vp]
+    L.dw_token_logp.restype = i32
+    L.dw_token_logp.argtypes = [vp, i64, i64, vp, i32, i64, i64, i32, vp, vp]
+    L.dw_policy_loss_scratch_bytes.restype = sz
+    L.dw_policy_loss_scratch_bytes.argtypes = [i32, i64]
+    L.dw_policy_loss.restype = i32
+    L.dw_policy_loss.argtypes = [vp, i64, i64, vp, vp, vp, vp, vp, i32, i64, i64, i32, f32, f32, f32, vp, vp, vp, i64, i64,
+                                 vp, sz, vp]
     _LIB = L
     return L
 

@@ -28,6 +28,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {       // rou
 struct F32 {
   typedef float T;
   static constexpr int V = 4;
+  static constexpr uint32_t kMinusInf = 0xFF800000u;
   __device__ static __forceinline__ void unpack(const uint32_t (&r)[4], float (&f)[V]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(r[j]);
@@ -43,6 +44,7 @@ struct F32 {
 struct Bf16 {
   typedef uint16_t T;
   static constexpr int V = 8;
+  static constexpr uint32_t kMinusInf = 0xFF80FF80u;
   __device__ static __forceinline__ void unpack(const uint32_t (&r)[4], float (&f)[V]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -59,6 +61,19 @@ struct Bf16 {
   typedef Raw16a2 Raw;
 };
 
+// 16 bytes of whole elements
+template <class E>
+__device__ __forceinline__ void load_piece(const typename E::T* p, uint32_t (&r)[4]) {
+  const typename E::Raw v = *reinterpret_cast<const typename E::Raw*>(p);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r[j] = v.w[j];
+}
+template <class E>
+__device__ __forceinline__ void store_piece(typename E::T* p, const float (&f)[E::V]) {
+  typename E::Raw v;
+  E::pack(f, v.w);
+  *reinterpret_cast<typename E::Raw*>(p) = v;
+}
 // the 16 bytes of elements e0 .. e0+V-1 of a row of n; elements at n and beyond read as zero
 template <class E>
 __device__ __forceinline__ void load16(const typename E::T* row, int64_t e0, int64_t n, uint32_t (&r)[4]) {
@@ -140,5 +155,21 @@ struct NormArgs {
 hipError_t launch_layer_norm(const NormArgs& a, int dtype, hipStream_t s);
 hipError_t launch_layer_norm_grad(const NormArgs& a, bool sums, int dtype, hipStream_t s);
 int layer_norm_grad_strips(int k, int64_t rows, int64_t n, int dtype);
+
+
+// ---- policy loss (dw_policy.hip) -------------------------------------------------------------------------------------
+struct PolicyArgs {
+  Rows logits;
+  RowsOut grad;                                            // p = nullptr: not wanted
+  const int32_t* target;                                   // [k][rows], as the others
+  const float* old_logp; const float* ref_logp; const float* advantage;      // old_logp = nullptr: log probabilities alone
+  const float* weight; float mean_weight;                  // weight = nullptr: mean_weight for every row
+  float q_min, q_max, kl_coef;
+  float* logp; float* part;                                // part: a row's share of the loss
+  float* loss;                                             // [k]
+  int k;
+  int64_t rows, vocab;
+};
+hipError_t launch_policy(const PolicyArgs& a, int dtype, hipStream_t s);
 
 }  // namespace dw

@@ -100,4 +100,59 @@ int dw_layer_norm_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const
   return DW_OK;
 }
 
+int dw_token_logp(const void* d_logits, int64_t ld, int64_t stride, const int32_t* d_target, int k, int64_t rows,
+                  int64_t vocab, int dtype, float* d_logp, void* stream) {
+  if (k < 1 || k > DW_MAX_K || !is_type(dtype)) return DW_ERR_CONFIG;
+  if (rows < 0 || rows >= kMaxRows || vocab < 1 || vocab > DW_MAX_VOCAB) return DW_ERR_ARG;
+  if (rows == 0) return DW_OK;
+  if (!d_logits || !d_target || !d_logp) return DW_ERR_NULL;
+  if (!in_ok(d_logits, ld, stride, rows, vocab, type_bytes(dtype)) || !aligned(d_target, 4) || !aligned(d_logp, 4)) return DW_ERR_ARG;
+  PolicyArgs a = {};
+  a.logits = {d_logits, ld, stride};
+  a.target = d_target;
+  a.mean_weight = 1.f;
+  a.logp = d_logp;
+  a.k = k; a.rows = rows; a.vocab = vocab;
+  DW_HIP(launch_policy(a, dtype, (hipStream_t)stream));
+  return DW_OK;
+}
+
+size_t dw_policy_loss_scratch_bytes(int k, int64_t rows) {
+  if (k < 1 || k > DW_MAX_K || rows < 0 || rows >= kMaxRows) return 0;
+  return (size_t)k * rows * sizeof(float);
+}
+
+int dw_policy_loss(const void* d_logits, int64_t ld, int64_t stride, const int32_t* d_target, const float* d_old_logp,
+                   const float* d_ref_logp, const float* d_advantage, const float* d_weight, int k, int64_t rows,
+                   int64_t vocab, int dtype, float clip_low, float clip_high, float kl_coef, float* d_loss, float* d_logp,
+                   void* d_grad, int64_t grad_ld, int64_t grad_stride, void* d_scratch, size_t scratch_bytes, void* stream) {
+  if (k < 1 || k > DW_MAX_K || !is_type(dtype)) return DW_ERR_CONFIG;
+  if (rows < 0 || rows >= kMaxRows || vocab < 1 || vocab > DW_MAX_VOCAB) return DW_ERR_ARG;
+  if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f) || !std::isfinite(clip_high) || !std::isfinite(kl_coef)) return DW_ERR_HYPER;
+  if (!aligned(d_loss, 4) || !aligned(d_logp, 4)) return DW_ERR_ARG;
+  if (rows > 0) {
+    if (!d_logits || !d_target || !d_old_logp || !d_advantage || (kl_coef != 0.f && !d_ref_logp)) return DW_ERR_NULL;
+    const int64_t b = type_bytes(dtype);
+    if (!in_ok(d_logits, ld, stride, rows, vocab, b) || !aligned(d_target, 4)) return DW_ERR_ARG;
+    if (!aligned(d_old_logp, 4) || !aligned(d_ref_logp, 4) || !aligned(d_advantage, 4) || !aligned(d_weight, 4)) return DW_ERR_ARG;
+    if (d_grad && !out_ok(d_grad, grad_ld, grad_stride, k, rows, vocab, b)) return DW_ERR_ARG;
+    if (d_grad == d_logits && (grad_ld != ld || (k > 1 && grad_stride != stride))) return DW_ERR_ARG;      // in place: the same rows
+    if (d_loss && (!d_scratch || !aligned(d_scratch, 256) || scratch_bytes < dw_policy_loss_scratch_bytes(k, rows))) return DW_ERR_WORKSPACE;
+  }
+  PolicyArgs a = {};
+  a.logits = {d_logits, ld, stride};
+  a.grad = {d_grad, grad_ld, grad_stride};
+  a.target = d_target;
+  a.old_logp = d_old_logp; a.ref_logp = d_ref_logp; a.advantage = d_advantage;
+  a.weight = d_weight;
+  a.mean_weight = rows > 0 ? 1.f / (float)rows : 0.f;
+  a.q_min = 1.f - clip_low; a.q_max = 1.f + clip_high; a.kl_coef = kl_coef;
+  a.logp = d_logp;
+  a.part = d_loss ? static_cast<float*>(d_scratch) : nullptr;
+  a.loss = d_loss;
+  a.k = k; a.rows = rows; a.vocab = vocab;
+  DW_HIP(launch_policy(a, dtype, (hipStream_t)stream));
+  return DW_OK;
+}
+
 }  // extern "C"

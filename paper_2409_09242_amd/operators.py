@@ -150,3 +150,53 @@ def layer_norm_grad(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, 
         _check(B.lib().dw_layer_norm_grad(dyp, dy_ld, dy_st, xp, x_ld, x_st, gp, p_st, mp, rp, k, rows, n, code, dxp, dx_ld,
                                           dx_st, dgp, dbp, g_st, sp, nbytes, stream), "dw_layer_norm_grad")
     return (dx if want_dx else None), (dgamma if want_params else None), (dbeta if want_params else None)
+
+
+# ---- policy loss -----------------------------------------------------------------------------------------------------
+
+def token_logp(logits, target, out=None):
+    """Log probabilities, float32 [k][rows], of the tokens target (int32 [k][rows]) under logits [k][rows][vocab]; 0 where
+    the target lies outside the vocabulary."""
+    code = _type(logits, "logits")
+    zp, ld, st = _matrix(logits, "logits")
+    k, rows, vocab = logits.shape
+    dev = logits.device
+    stream, guard = _on(dev)
+    tp = _values(target, "target", (k, rows), torch.int32, dev)
+    if out is None:
+        out = torch.empty((k, rows), dtype=torch.float32, device=dev)
+    op = _values(out, "out", (k, rows), torch.float32, dev)
+    with guard:
+        _check(B.lib().dw_token_logp(zp, ld, st, tp, k, rows, vocab, code, op, stream), "dw_token_logp")
+    return out
+
+
+def policy_loss(logits, target, old_logp, advantage, weight=None, ref_logp=None, clip_low: float = 0.2, clip_high: float = 0.2,
+                kl_coef: float = 0.0, grad=None, want_grad: bool = True):
+    """(loss [k], logp [k][rows], gradient of the logits) of the clipped policy loss with a KL term; see dw_policy_loss.
+
+    weight (float32 [k][rows], None: 1/rows): mask and average in one, the loss is the weighted sum; rows of weight 0 are
+    not read.  grad: a tensor like logits to write into, the logits themselves among them; want_grad=False: None."""
+    code = _type(logits, "logits")
+    zp, ld, st = _matrix(logits, "logits")
+    k, rows, vocab = logits.shape
+    dev = logits.device
+    stream, guard = _on(dev)
+    tp = _values(target, "target", (k, rows), torch.int32, dev)
+    if old_logp is None or advantage is None:
+        raise ValueError("old_logp and advantage are wanted")
+    op, ap, wp, rp = (_values(t, name, (k, rows), torch.float32, dev) for t, name in (
+        (old_logp, "old_logp"), (advantage, "advantage"), (weight, "weight"), (ref_logp, "ref_logp")))
+    gp, g_ld, g_st = None, vocab, rows * vocab
+    if want_grad:
+        if grad is None:
+            grad = torch.empty((k, rows, vocab), dtype=logits.dtype, device=dev)
+        gp, g_ld, g_st = _matrix(grad, "grad", logits.shape, logits.dtype, dev)
+    loss = torch.empty(k, dtype=torch.float32, device=dev)
+    logp = torch.empty((k, rows), dtype=torch.float32, device=dev)
+    nbytes = B.lib().dw_policy_loss_scratch_bytes(k, rows)
+    scratch, sp = _scratch(nbytes, dev)
+    with guard:
+        _check(B.lib().dw_policy_loss(zp, ld, st, tp, op, rp, ap, wp, k, rows, vocab, code, clip_low, clip_high, kl_coef,
+                                      loss.data_ptr(), logp.data_ptr(), gp, g_ld, g_st, sp, nbytes, stream), "dw_policy_loss")
+    return loss, logp, (grad if want_grad else None)
