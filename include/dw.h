@@ -343,6 +343,26 @@ int dw_policy_loss(const void* d_logits, int64_t ld, int64_t stride, const int32
                    void* d_grad, int64_t grad_ld, int64_t grad_stride, void* d_scratch, size_t scratch_bytes, void* stream);
 
 /*
+ * Global gradient norm of every worker over its tensors, and clipping:
+ *   norm = sqrt(sum g^2),  c = min(1, max_norm / (norm + 1e-6)),  g' = c g
+ * The workers are replicas of one model: tensor j has h_count[j] elements for each of them.
+ *   h_grad    host array of k*n_tensors device addresses, worker w's tensor j at w*n_tensors + j; contiguous tensors at any
+ *             multiple of their element size; not read (and may be NULL) where the count is 0
+ *   h_dtype   [n_tensors] types, or NULL: all are `dtype`
+ *   d_out     NULL: clipped in place (a worker whose norm is within max_norm is only read).  Otherwise the gradients stay
+ *             and g' goes to [k] vectors of floats, worker w's at w*out_stride, its tensors one behind the other in their
+ *             order: the d_g of dw_update_only when out_stride = P.
+ *   d_norm    [k] floats: the norms before clipping
+ *   max_norm  > 0; infinity: the norms (and copies) alone
+ * Squares are added in 64 bits.  Where a norm is not finite that worker's gradients are left as they are (c = 1).
+ */
+#define DW_MAX_TENSORS (1 << 20)
+size_t dw_clip_grads_scratch_bytes(int k, int n_tensors, const int64_t* h_count);
+int dw_clip_grads(const void* const* h_grad, const int64_t* h_count, const int32_t* h_dtype, int k, int n_tensors, int dtype,
+                  float max_norm, float* d_out, int64_t out_stride, float* d_norm, void* d_scratch, size_t scratch_bytes,
+                  void* stream);
+
+/*
  * Per-kernel timing for benchmarks (not part of the method).  While enabled, every kernel the handle launches
  * is bracketed by two HIP events on the caller's stream.  dw_profile_read synchronises the stream and returns,
  * per kernel class, the number of launches and their summed duration in milliseconds since the last read

@@ -172,4 +172,43 @@ struct PolicyArgs {
 };
 hipError_t launch_policy(const PolicyArgs& a, int dtype, hipStream_t s);
 
+// ---- gradient norm and clipping (dw_clip.hip) ------------------------------------------------------------------------
+// Arguments of one launch: tensors j < n of `workers` workers.  The table holds n + 1 places (in elements, from the launch's first
+// tensor), the tensors' addresses (workers by n), then n first chunks and their types, two to a word.
+struct ClipTable {
+  static constexpr int kWords = 470;                       // 64-bit words; all arguments stay below 4 KB
+  uint64_t word[kWords];
+  int n, workers, chunks, worker0;
+  int64_t chunk, elements;                                 // elements of a chunk, and of the launch's tensors (of one worker)
+  double* part; int parts, part0;                          // partial sums [k][parts], this launch's first
+  float* norm; float max_norm;
+  float* out; int64_t out_stride, out0;                    // nullptr: in place; out0: elements of a worker before this launch's
+  // most tensors of one launch for so many workers
+  static int tensors(int workers) { return (kWords - 1) * 2 / (2 * workers + 3); }
+  __host__ __device__ int64_t first_of(int j) const { return (int64_t)word[j]; }
+  __host__ __device__ const void* address(int w, int j) const { return reinterpret_cast<const void*>(word[n + 1 + w * n + j]); }
+  __host__ __device__ int chunk_word(int j) const {
+    const uint64_t v = word[n + 1 + workers * n + (j >> 1)];
+    return (int)(uint32_t)(j & 1 ? v >> 32 : v);
+  }
+  __host__ __device__ int chunk_of(int j) const { return chunk_word(j) & 0x7FFFFFFF; }
+  __host__ __device__ bool is_bf16(int j) const { return chunk_word(j) < 0; }
+  void set_first(int j, int64_t v) { word[j] = (uint64_t)v; }
+  void set_address(int w, int j, const void* p) { word[n + 1 + w * n + j] = reinterpret_cast<uint64_t>(p); }
+  void set_chunk(int j, int32_t c) {
+    uint64_t& v = word[n + 1 + workers * n + (j >> 1)];
+    v = j & 1 ? (v & 0xFFFFFFFFull) | (uint64_t)(uint32_t)c << 32 : (uint64_t)(uint32_t)c;
+  }
+  void set_type(int j, bool bf16) {
+    if (bf16) word[n + 1 + workers * n + (j >> 1)] |= j & 1 ? 1ull << 63 : 1ull << 31;
+  }
+};
+static_assert(sizeof(ClipTable) <= 4096, "kernel arguments");
+int64_t clip_chunk(int64_t elements_of_all_workers);
+void clip_table_fill(ClipTable& t, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int dtype, int per_worker,
+                     int j0, int w0);
+hipError_t launch_grad_squares(const ClipTable& t, hipStream_t s);
+hipError_t launch_grad_norm(const double* part, int parts, float* norm, int k, hipStream_t s);
+hipError_t launch_clip(const ClipTable& t, hipStream_t s);
+
 }  // namespace dw

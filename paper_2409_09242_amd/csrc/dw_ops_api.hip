@@ -36,6 +36,24 @@ inline bool norm_shape_ok(int k, int64_t rows, int64_t n) {
   return rows >= 0 && rows < kMaxRows && n >= 1 && n <= DW_MAX_NORM;
 }
 
+struct ClipSizes { int64_t elements, chunk; int parts; };   // of one worker
+int clip_sizes(int k, int n_tensors, const int64_t* h_count, ClipSizes* z) {
+  if (k < 1 || k > DW_MAX_K) return DW_ERR_CONFIG;
+  if (n_tensors < 0 || n_tensors > DW_MAX_TENSORS) return DW_ERR_ARG;
+  if (!h_count && n_tensors > 0) return DW_ERR_NULL;
+  z->elements = 0;
+  for (int j = 0; j < n_tensors; ++j) {
+    if (h_count[j] < 0 || h_count[j] > (1ll << 40)) return DW_ERR_ARG;
+    z->elements += h_count[j];
+  }
+  if (z->elements > (1ll << 40)) return DW_ERR_ARG;
+  z->chunk = clip_chunk(z->elements * k);
+  int64_t parts = 0;
+  for (int j = 0; j < n_tensors; ++j) parts += ceil_div(h_count[j], z->chunk);
+  z->parts = (int)parts;                                    // at most 4096 + DW_MAX_TENSORS
+  return DW_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -152,6 +170,56 @@ int dw_policy_loss(const void* d_logits, int64_t ld, int64_t stride, const int32
   a.loss = d_loss;
   a.k = k; a.rows = rows; a.vocab = vocab;
   DW_HIP(launch_policy(a, dtype, (hipStream_t)stream));
+  return DW_OK;
+}
+
+size_t dw_clip_grads_scratch_bytes(int k, int n_tensors, const int64_t* h_count) {
+  ClipSizes z;
+  if (clip_sizes(k, n_tensors, h_count, &z) != DW_OK) return 0;
+  return (size_t)k * z.parts * sizeof(double);
+}
+
+int dw_clip_grads(const void* const* h_grad, const int64_t* h_count, const int32_t* h_dtype, int k, int n_tensors, int dtype,
+                  float max_norm, float* d_out, int64_t out_stride, float* d_norm, void* d_scratch, size_t scratch_bytes,
+                  void* stream) {
+  ClipSizes z;
+  const int st = clip_sizes(k, n_tensors, h_count, &z);
+  if (st != DW_OK) return st;
+  if (!h_dtype && !is_type(dtype)) return DW_ERR_CONFIG;
+  for (int j = 0; h_dtype && j < n_tensors; ++j)
+    if (!is_type(h_dtype[j])) return DW_ERR_CONFIG;
+  if (!(max_norm > 0.f)) return DW_ERR_HYPER;
+  if (!d_norm || (!h_grad && z.elements > 0)) return DW_ERR_NULL;
+  if (!aligned(d_norm, 4) || (d_out && !grads_ok(d_out, out_stride, k, z.elements))) return DW_ERR_ARG;
+  for (int64_t i = 0; i < (int64_t)k * n_tensors; ++i) {
+    const int j = (int)(i % n_tensors);
+    if (h_count[j] == 0) continue;
+    if (!h_grad[i]) return DW_ERR_NULL;
+    if (!aligned(h_grad[i], type_bytes(h_dtype ? h_dtype[j] : dtype))) return DW_ERR_ARG;
+  }
+  if (z.parts > 0 && (!d_scratch || !aligned(d_scratch, 256) || scratch_bytes < dw_clip_grads_scratch_bytes(k, n_tensors, h_count)))
+    return DW_ERR_WORKSPACE;
+  const hipStream_t s = (hipStream_t)stream;
+  double* part = static_cast<double*>(d_scratch);
+  const bool writes = z.parts > 0 && (d_out || std::isfinite(max_norm));
+  // first pass over all tensors, then the second: both in launches of as many tensors as the arguments hold
+  for (int pass = 0; pass < (writes ? 2 : 1); ++pass) {
+    ClipTable t;
+    t.chunk = z.chunk;
+    t.part = part; t.parts = z.parts; t.part0 = 0;
+    t.norm = d_norm; t.max_norm = max_norm;
+    t.out = d_out; t.out_stride = out_stride; t.out0 = 0;
+    t.worker0 = 0; t.workers = k;
+    const int most = ClipTable::tensors(k);
+    for (int j0 = 0; j0 < n_tensors; j0 += most) {
+      t.n = n_tensors - j0 < most ? n_tensors - j0 : most;
+      clip_table_fill(t, h_grad, h_count, h_dtype, dtype, n_tensors, j0, 0);
+      DW_HIP(pass == 0 ? launch_grad_squares(t, s) : launch_clip(t, s));
+      t.part0 += t.chunks;
+      t.out0 += t.elements;
+    }
+  }
+  if (!writes) DW_HIP(launch_grad_norm(part, z.parts, d_norm, k, s));
   return DW_OK;
 }
 

@@ -10,6 +10,7 @@ ValueError, what the library refuses DwError; there is no CPU path.
 from __future__ import annotations
 
 import contextlib
+import ctypes as C
 from typing import Optional, Tuple
 
 import torch
@@ -200,3 +201,51 @@ def policy_loss(logits, target, old_logp, advantage, weight=None, ref_logp=None,
         _check(B.lib().dw_policy_loss(zp, ld, st, tp, op, rp, ap, wp, k, rows, vocab, code, clip_low, clip_high, kl_coef,
                                       loss.data_ptr(), logp.data_ptr(), gp, g_ld, g_st, sp, nbytes, stream), "dw_policy_loss")
     return loss, logp, (grad if want_grad else None)
+
+
+# ---- gradient norm and clipping --------------------------------------------------------------------------------------
+
+def _clip(grads, max_norm: float, workers: int, out, where: str):
+    if workers < 1 or len(grads) % workers:
+        raise ValueError("%d tensors for %d workers" % (len(grads), workers))
+    per = len(grads) // workers
+    if per == 0:
+        raise ValueError("no tensors")
+    dev = grads[0].device
+    stream, guard = _on(dev)
+    counts, types = [g.numel() for g in grads], [_TYPES.get(g.dtype, -1) for g in grads]
+    if any(g.device != dev for g in grads) or -1 in types:
+        raise ValueError("float32 or bfloat16 tensors on one device are wanted")
+    if not all(g.is_contiguous() for g in grads):
+        raise ValueError("a gradient is not contiguous")
+    for w in range(1, workers):
+        if counts[w * per:(w + 1) * per] != counts[:per] or types[w * per:(w + 1) * per] != types[:per]:
+            raise ValueError("worker %d has tensors of other sizes or types than worker 0" % w)
+    total = sum(counts[:per])
+    op, o_st = None, total
+    if out is not None:
+        op, o_st = _param(out, "out", workers, total, dev)
+    addresses = (C.c_void_p * len(grads))(*[g.data_ptr() for g in grads])
+    sizes = (C.c_int64 * per)(*counts[:per])
+    kinds = None if types[:per] == [types[0]] * per else (C.c_int32 * per)(*types[:per])
+    norm = torch.empty(workers, dtype=torch.float32, device=dev)
+    nbytes = B.lib().dw_clip_grads_scratch_bytes(workers, per, sizes)
+    scratch, sp = _scratch(nbytes, dev)
+    with guard:
+        _check(B.lib().dw_clip_grads(addresses, sizes, kinds, workers, per, types[0], max_norm, op, o_st, norm.data_ptr(), sp, nbytes,
+                                     stream), where)
+    return norm
+
+
+def clip_grads(grads, max_norm: float, workers: int = 1, out=None):
+    """Clip every worker's gradients to a global 2-norm of at most max_norm; returns the norms before, float32 [workers].
+
+    grads: the tensors of worker 0, then those of worker 1 in the same order and so on (contiguous, float32 or bfloat16).
+    They are scaled in place, or left alone with out, float32 [workers][total]: the clipped gradients one behind the other,
+    as Handle.update_only takes them."""
+    return _clip(grads, max_norm, workers, out, "dw_clip_grads")
+
+
+def grad_norm(grads, workers: int = 1):
+    """The global 2-norm of every worker's gradients, float32 [workers]; grads as for clip_grads."""
+    return _clip(grads, float("inf"), workers, None, "dw_clip_grads")
