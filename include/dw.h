@@ -363,6 +363,42 @@ int dw_clip_grads(const void* const* h_grad, const int64_t* h_count, const int32
                   void* stream);
 
 /*
+ * Matrices in 8 bits: rows of e4m3 numbers (4 bits of exponent, 3 of mantissa, largest 448, no infinities) with one scale
+ * for each block of 128 along the row, a power of two kept as the byte e + 127.  The matrix instruction applies such
+ * scales by itself; e4m3 is a floating format, so against a scale of full precision nothing is lost but up to one of its
+ * binades at the small end.  A row of n numbers takes DW_FP8_ROW(n) bytes (zeros behind the n-th) and DW_FP8_SCALES(n) bytes of
+ * scales; rows follow each other without gaps, workers too.
+ *
+ * dw_fp8_quantize makes them from x [k][rows][n]: e is the least integer (at least -126) for which the block's largest
+ * magnitude is at most 448 2^e, a block of zeros has e = 0, and x 2^-e is rounded to nearest, ties to even.  A block that
+ * holds an infinity or NaN is all NaN.
+ *   square      0: blocks of 128 along the row of the matrix that is written.  1: squares of 128 x 128 of x share a scale
+ *               (it is written for each of their rows), so that q and qt hold the same numbers
+ *   d_q, d_scale       the matrix [k][rows], rows of n; NULL both: not wanted
+ *   d_qt, d_scale_t    the transposed matrix [k][n], rows of `rows`; NULL both: not wanted
+ * Numbers' addresses are multiples of 16, the scales' of 4.
+ */
+#define DW_MAX_FP8 (1 << 24)  /* rows, columns and contraction */
+#define DW_FP8_ROW(n) (((n) + 127) / 128 * 128)
+#define DW_FP8_SCALES(n) (((n) + 511) / 512 * 4)
+int dw_fp8_quantize(const void* d_x, int64_t x_ld, int64_t x_stride, int k, int64_t rows, int64_t n, int dtype, int square,
+                    uint8_t* d_q, uint8_t* d_scale, uint8_t* d_qt, uint8_t* d_scale_t, void* stream);
+
+/*
+ * C = A B^T (+ bias) of such matrices, for every worker: A [m] rows and B [n] rows of `contraction` numbers, C [m][n] in
+ * `dtype`.  In DW_F32 the sums are those of fp32.  In DW_BF16 the products run at the 8-bit rate, whose instruction adds eight
+ * neighbouring products at a time with bits down to 2^-13 of the largest (about 1e-5 of a sum of random terms, a hundredth
+ * of the rounding to bf16), and the eights in fp32.  With x, W and dy quantised along the axis that is summed:
+ * y = x W^T, dx = dy (W^T)^T, dW = dy^T (x^T)^T.
+ *   d_bias      [k] rows of n floats, worker w's at w*bias_stride; NULL: none
+ * An empty contraction gives the bias, or zeros (the operands may then be NULL).
+ */
+size_t dw_fp8_matmul_scratch_bytes(int k, int64_t m, int64_t n, int64_t contraction);
+int dw_fp8_matmul(const uint8_t* d_a, const uint8_t* d_a_scale, const uint8_t* d_b, const uint8_t* d_b_scale, const float* d_bias,
+                  int64_t bias_stride, int k, int64_t m, int64_t n, int64_t contraction, int dtype, void* d_c, int64_t c_ld,
+                  int64_t c_stride, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Per-kernel timing for benchmarks (not part of the method).  While enabled, every kernel the handle launches
  * is bracketed by two HIP events on the caller's stream.  dw_profile_read synchronises the stream and returns,
  * per kernel class, the number of launches and their summed duration in milliseconds since the last read

@@ -29,7 +29,8 @@ EXPORTS = ("dw_strerror", "dw_last_hip_error", "dw_param_count", "dw_workspace_b
            "dw_worker_step", "dw_update_only", "dw_elastic_sync", "dw_get_state", "dw_set_state",
            "dw_profile", "dw_profile_read", "dw_partition_scratch_bytes", "dw_overlap_partition", "dw_draw_batch",
            "dw_overlap_partition_static", "dw_layer_norm", "dw_layer_norm_grad_scratch_bytes", "dw_layer_norm_grad",
-           "dw_token_logp", "dw_policy_loss_scratch_bytes", "dw_policy_loss", "dw_clip_grads_scratch_bytes", "dw_clip_grads")
+           "dw_token_logp", "dw_policy_loss_scratch_bytes", "dw_policy_loss", "dw_clip_grads_scratch_bytes", "dw_clip_grads",
+           "dw_fp8_quantize", "dw_fp8_matmul_scratch_bytes", "dw_fp8_matmul")
 KERNEL_CLASSES = ("rademacher", "gemm_fwd", "head", "gemm_wgrad", "gemm_dgrad", "update", "weights", "pull", "gather", "step")
 
 
@@ -107,6 +108,12 @@ def lib() -> C.CDLL:
     L.dw_clip_grads_scratch_bytes.argtypes = [i32, i32, vp]
     L.dw_clip_grads.restype = i32
     L.dw_clip_grads.argtypes = [vp, vp, vp, i32, i32, i32, f32, vp, i64, vp, vp, sz, vp]
+    L.dw_fp8_quantize.restype = i32
+    L.dw_fp8_quantize.argtypes = [vp, i64, i64, i32, i64, i64, i32, i32, vp, vp, vp, vp, vp]
+    L.dw_fp8_matmul_scratch_bytes.restype = sz
+    L.dw_fp8_matmul_scratch_bytes.argtypes = [i32, i64, i64, i64]
+    L.dw_fp8_matmul.restype = i32
+    L.dw_fp8_matmul.argtypes = [vp, vp, vp, vp, vp, i64, i32, i64, i64, i64, i32, vp, i64, i64, vp, sz, vp]
     _LIB = L
     return L
 

@@ -1,0 +1,194 @@
+// Numbers in e4m3 with one power-of-two scale per block of 128 (gfx950, wave64).
+//
+// A block of 128 along a row (square: of 128 x 128) with largest magnitude m gets the least e with m <= 448 2^e (448 is
+// the largest number of e4m3), its elements are x 2^-e rounded to nearest, ties to even, and the scale is kept as the byte
+// e + 127 (at least 1).  2^-e is a power of two, so the product is exact and the only rounding is that to e4m3; e follows
+// from the bits of m: m = 1.f 2^E and 448 = 1.75 2^8, so e = E - 8, and one more where f > 0.75.  The largest magnitude is
+// found on the bits as integers, where a NaN is above infinity and infinity above the rest: a block with one of them is all NaN.
+//
+// Rows alone: 16 lanes share a block, 8 elements each, one pass from registers.  With the transposed form or squares a
+// block of threads takes a tile of 128 x 128, 8 x 8 elements a thread; the transposed bytes leave through LDS so that
+// both forms are written in whole lines while x is read once.
+#include "dw_ops.h"
+
+namespace dw {
+
+namespace {
+
+// elements e0 .. e0+7 of a row of n as fp32 (zero past the end)
+template <class E>
+__device__ __forceinline__ void load8(const typename E::T* row, int64_t e0, int64_t n, float (&f)[8]) {
+#pragma unroll
+  for (int h = 0; h < 8 / E::V; ++h) {
+    uint32_t raw[4];
+    float v[E::V];
+    load16<E>(row, e0 + h * E::V, n, raw);
+    E::unpack(raw, v);
+#pragma unroll
+    for (int j = 0; j < E::V; ++j) f[h * E::V + j] = v[j];
+  }
+}
+
+__device__ __forceinline__ uint32_t magnitude(float f) { return __float_as_uint(f) & 0x7FFFFFFFu; }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+struct Scale { uint32_t byte; float inverse; };
+__device__ __forceinline__ Scale scale_of(uint32_t top) {
+  if (top == 0u) return {127u, 1.f};
+  if (top >= 0x7F800000u) return {127u, __uint_as_float(0x7FC00000u)};
+  int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  e = e < -126 ? -126 : e;
+  return {(uint32_t)(e + 127), __uint_as_float((uint32_t)(127 - e) << 23)};
+}
+
+__device__ __forceinline__ uint2 to_e4m3(const float (&f)[8], float inverse) {
+  int lo = 0, hi = 0;
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * inverse, f[1] * inverse, lo, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * inverse, f[3] * inverse, lo, true);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[4] * inverse, f[5] * inverse, hi, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[6] * inverse, f[7] * inverse, hi, true);
+  return make_uint2((uint32_t)lo, (uint32_t)hi);
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
+  const int w = blockIdx.z, t = threadIdx.x & 15;
+  const int64_t b = blockIdx.x;                             // block of 128 along the row
+  const int64_t r = (int64_t)blockIdx.y * 16 + (threadIdx.x >> 4);
+  const int64_t np = DW_FP8_ROW(a.n), ns = DW_FP8_SCALES(a.n);
+  if (r >= a.rows) return;                                  // (16 lanes at once: those that exchange values stay together)
+  const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride + r * a.x.ld;
+  float f[8];
+  load8<E>(x, b * 128 + t * 8, a.n, f);
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = larger(top, magnitude(f[j]));
+#pragma unroll
+  for (int off = 1; off < 16; off <<= 1) top = larger(top, (uint32_t)__shfl_xor((int)top, off));
+  const Scale s = scale_of(top);
+  const int64_t row = w * a.rows + r;
+  *reinterpret_cast<uint2*>(a.q + row * np + b * 128 + t * 8) = to_e4m3(f, s.inverse);
+  uint8_t* sc = a.scale + row * ns;
+  if (t == 0) sc[b] = (uint8_t)s.byte;
+  if (b == np / 128 - 1 && b + 1 + t < ns) sc[b + 1 + t] = 127;       // a row's scales fill whole words
+}
+
+template <class E, bool SQUARE>
+__global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a) {
+  __shared__ uint32_t tops[16][129];
+  __shared__ __align__(16) uint8_t tile[128][144];          // transposed bytes: [column][row]
+  const int w = blockIdx.z;
+  const int64_t c0 = (int64_t)blockIdx.x * 128, r0 = (int64_t)blockIdx.y * 128;
+  const int tc = threadIdx.x & 15, tr = threadIdx.x >> 4;   // this thread's 8 columns from 8 tc, 8 rows from 8 tr
+  const int64_t np = DW_FP8_ROW(a.n), ns = DW_FP8_SCALES(a.n), rp = DW_FP8_ROW(a.rows), rs = DW_FP8_SCALES(a.rows);
+  const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
+  float f[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = r0 + tr * 8 + i;
+    if (r < a.rows) load8<E>(x + r * a.x.ld, c0 + tc * 8, a.n, f[i]);
+    else
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] = 0.f;
+  }
+  uint32_t row_top[8], col_top[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { row_top[i] = 0; col_top[i] = 0; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t m = magnitude(f[i][j]);
+      row_top[i] = larger(row_top[i], m);
+      col_top[j] = larger(col_top[j], m);
+    }
+  Scale all = {127u, 1.f};
+  if constexpr (SQUARE) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = larger(m, row_top[i]);
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) m = larger(m, (uint32_t)__shfl_xor((int)m, off));
+    if ((threadIdx.x & 63) == 0) tops[0][threadIdx.x >> 6] = m;
+    __syncthreads();
+    all = scale_of(larger(larger(tops[0][0], tops[0][1]), larger(tops[0][2], tops[0][3])));
+  }
+  if (a.q) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      Scale s = all;
+      if constexpr (!SQUARE) {
+        uint32_t m = row_top[i];
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) m = larger(m, (uint32_t)__shfl_xor((int)m, off));
+        s = scale_of(m);
+      }
+      const int64_t r = r0 + tr * 8 + i;
+      if (r < a.rows) {
+        const int64_t row = w * a.rows + r;
+        *reinterpret_cast<uint2*>(a.q + row * np + c0 + tc * 8) = to_e4m3(f[i], s.inverse);
+        uint8_t* sc = a.scale + row * ns;
+        if (tc == 0) sc[blockIdx.x] = (uint8_t)s.byte;
+        if (blockIdx.x == gridDim.x - 1 && blockIdx.x + 1 + tc < ns) sc[blockIdx.x + 1 + tc] = 127;
+      }
+    }
+  }
+  if (!a.qt) return;
+  float inv[8];
+  if constexpr (SQUARE) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) inv[j] = all.inverse;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) tops[tr][tc * 8 + j] = col_top[j];
+    __syncthreads();
+    if (threadIdx.x < 128) {                                // one thread per column finds its scale
+      uint32_t m = 0;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) m = larger(m, tops[q][threadIdx.x]);
+      tops[0][threadIdx.x] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) inv[j] = scale_of(tops[0][tc * 8 + j]).inverse;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float g[8] = {f[0][j], f[1][j], f[2][j], f[3][j], f[4][j], f[5][j], f[6][j], f[7][j]};
+    *reinterpret_cast<uint2*>(&tile[tc * 8 + j][tr * 8]) = to_e4m3(g, inv[j]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {                             // 8 threads a column, 16 rows each
+    const int c = p * 32 + (threadIdx.x >> 3), at = (threadIdx.x & 7) * 16;
+    if (c0 + c < a.n)
+      *reinterpret_cast<uint4*>(a.qt + (w * a.n + c0 + c) * rp + r0 + at) = *reinterpret_cast<const uint4*>(&tile[c][at]);
+  }
+  if (threadIdx.x < 128 && c0 + threadIdx.x < a.n) {
+    uint8_t* sc = a.scale_t + (w * a.n + c0 + threadIdx.x) * rs;
+    sc[blockIdx.y] = (uint8_t)(SQUARE ? all.byte : scale_of(tops[0][threadIdx.x]).byte);
+    if (blockIdx.y == gridDim.y - 1)
+      for (int64_t q = blockIdx.y + 1; q < rs; ++q) sc[q] = 127;
+  }
+}
+
+template <class E>
+hipError_t quantize(const QuantArgs& a, hipStream_t s) {
+  if (!a.square && !a.qt) {
+    const dim3 grid((unsigned)(DW_FP8_ROW(a.n) / 128), (unsigned)ceil_div(a.rows, 16), (unsigned)a.k);
+    hipLaunchKernelGGL(quantize_rows_kernel<E>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  const dim3 grid((unsigned)(DW_FP8_ROW(a.n) / 128), (unsigned)(DW_FP8_ROW(a.rows) / 128), (unsigned)a.k);
+  if (a.square) hipLaunchKernelGGL((quantize_tile_kernel<E, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((quantize_tile_kernel<E, false>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_fp8_quantize(const QuantArgs& a, int dtype, hipStream_t s) {
+  return dtype == DW_BF16 ? quantize<Bf16>(a, s) : quantize<F32>(a, s);
+}
+
+}  // namespace dw

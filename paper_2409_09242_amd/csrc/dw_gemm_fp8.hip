@@ -1,0 +1,362 @@
+// Products of e4m3 matrices with a power-of-two scale per row and block of 128 along the contraction (gfx950, wave64).
+//
+//   C[m][n] = sum over blocks b of 2^(sa[m][b] + sb[n][b]) sum over k in b of a[m][k] b[n][k]   (+ bias[n])
+//
+// v_mfma_scale_f32_32x32x64_f8f6f4 multiplies 32 x 64 by 64 x 32 numbers of 8 bits and applies both scales (one byte per
+// row and 32 numbers) by itself, so scaled blocks cost no more than unscaled ones and are accumulated in fp32 throughout.
+// The contraction runs in steps of 64: a tile of BM + BN rows of 64 bytes goes from memory straight to LDS
+// (global_load_lds, 16 bytes a lane), four steps are in flight or resident, and every wave reads the operands of the next
+// step from LDS while it multiplies the present one.  Rows of 64 bytes lie back to back, so the 16-byte piece q of row r
+// is kept in slot q ^ (r/4 mod 4): the 16 lanes that read at a time then touch all banks once.  A row's scales for 512
+// numbers are one word; words go through LDS too, a group of eight steps at a time.
+//
+// That instruction adds eight neighbouring products at a time and keeps their bits down to 2^-13 of the largest one's power
+// (measured; all 8-bit matrix instructions of this chip do).  On normally distributed numbers the sums are then off by
+// 1.4e-5 of their size, on numbers with one in a hundred a hundred times larger by 7e-5: a fraction of a percent of an
+// output's rounding to bf16 (2e-3), but not fp32.  So outputs in fp32 take another way (EXACT): the same bytes are turned
+// into bf16, scale and all, by one instruction for two numbers, which is exact, and multiplied by v_mfma_f32_32x32x16_bf16 at
+// half the rate, whose sums are right to 24 bits.
+//
+// Operand A of the instruction is the matrix b and operand B is a: a lane then holds one row of C and groups of four
+// consecutive columns, which leave through a piece of LDS of the wave's own as whole row pieces of 16 bytes a lane.
+// The accumulators start from the bias.  Rows past the end of a matrix repeat the last one; what they give is not written.
+#include <type_traits>
+
+#include "dw_ops.h"
+
+namespace dw {
+
+namespace fp8 {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void* lds_void;
+typedef __attribute__((address_space(1))) const void* glb_void;
+
+constexpr int BK = 64, STAGES = 4, GROUP = 8;               // bytes of a step, steps in flight, steps per word of scales
+
+// at most N vector-memory operations of this wave outstanding (N < 64), its LDS reads all returned
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (0x7 << 4) | (0x0 << 8));
+}
+
+template <int WTM_, int WTN_, int WM_, int WN_, int PER_CU_>
+struct Config {
+  static constexpr int WTM = WTM_, WTN = WTN_, WM = WM_, WN = WN_, PER_CU = PER_CU_;
+  static constexpr int NW = WM * WN, NT = NW * 64;
+  static constexpr int BM = WM * WTM * 32, BN = WN * WTN * 32;
+  static constexpr int A_B = BM * BK, STAGE_B = (BM + BN) * BK;
+  static constexpr int CPW = STAGE_B / 1024 / NW;           // 1 KB pieces a wave moves per step
+  static constexpr int OFF_S = STAGE_B * STAGES;            // two groups of scale words, (BM + BN) each
+  static constexpr int LDS = OFF_S + 2 * (BM + BN) * 4;
+  static_assert(STAGE_B % (1024 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0, "whole pieces");
+};
+
+__device__ __forceinline__ int swizzle(int row) { return (row >> 2) & 3; }
+
+// eight numbers of 8 bits as bf16, times 2^(scale - 127)
+__device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
+  struct { bf16x2_t v[4]; } r;
+  r.v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  r.v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  r.v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  r.v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return __builtin_bit_cast(bf16x8, r);
+}
+__device__ __forceinline__ float power(int word) { return __uint_as_float(((unsigned)word & 255u) << 23); }
+
+template <class C, bool EXACT, bool SLICE>
+__global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
+  const int tiles_m = (int)((a.m + C::BM - 1) / C::BM), tiles_n = (int)((a.n + C::BN - 1) / C::BN);
+  const int tiles = tiles_m * tiles_n;
+  // consecutive blocks go to the eight dies in turn: each die gets a run of neighbouring tiles
+  const int per_xcd = gridDim.x >> 3;
+  const int logical = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  const int w = logical / tiles, tile = logical - w * tiles;
+  if (w >= a.k) return;
+  const int64_t row0 = (int64_t)(tile % tiles_m) * C::BM, col0 = (int64_t)(tile / tiles_m) * C::BN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm0 = (wave % C::WM) * C::WTM * 32, wn0 = (wave / C::WM) * C::WTN * 32;
+  const int l32 = lane & 31, half = lane >> 5;
+
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+
+  const int64_t kp = a.kp;
+  const uint8_t* A = a.a + w * a.m * kp;
+  const uint8_t* Bm = a.b + w * a.n * kp;
+  const uint8_t* sA = a.sa + w * a.m * a.ks;
+  const uint8_t* sB = a.sb + w * a.n * a.ks;
+  // steps of this block: all, or one slice of the contraction (slices begin at whole words of scales)
+  const int all_steps = (int)(kp / BK);
+  const int step0 = SLICE ? (int)blockIdx.y * a.slice_steps : 0;
+  const int steps = SLICE ? (all_steps - step0 < a.slice_steps ? all_steps - step0 : a.slice_steps) : all_steps;
+
+  // where the pieces this wave moves come from (step 0): piece c holds rows 16c .. 16c+15 of A's and then B's tile
+  const uint8_t* src[C::CPW];
+#pragma unroll
+  for (int c = 0; c < C::CPW; ++c) {
+    const int row = (wave * C::CPW + c) * 16 + (lane >> 2), q = (lane & 3) ^ swizzle(row);
+    int64_t r;
+    if (row < C::BM) { r = row0 + row; src[c] = A + (r < a.m ? r : a.m - 1) * kp + q * 16; }
+    else { r = col0 + row - C::BM; src[c] = Bm + (r < a.n ? r : a.n - 1) * kp + q * 16; }
+    src[c] += (int64_t)step0 * BK;
+  }
+  // scale words: 64 rows at a time, the waves in turn
+  constexpr int SP = (C::BM + C::BN) / 64, SPW = (SP + C::NW - 1) / C::NW;
+  const uint8_t* ssrc[SPW];
+#pragma unroll
+  for (int c = 0; c < SPW; ++c) {
+    int p = wave + c * C::NW; p = p < SP ? p : SP - 1;
+    const int row = p * 64 + lane;
+    int64_t r;
+    if (row < C::BM) { r = row0 + row; ssrc[c] = sA + (r < a.m ? r : a.m - 1) * a.ks; }
+    else { r = col0 + row - C::BM; ssrc[c] = sB + (r < a.n ? r : a.n - 1) * a.ks; }
+    ssrc[c] += step0 / 2;
+  }
+  auto issue = [&](int t, int st) {
+#pragma unroll
+    for (int c = 0; c < C::CPW; ++c)
+      __builtin_amdgcn_global_load_lds((glb_void)(src[c] + (int64_t)t * BK),
+                                       (lds_void)(smem + st * C::STAGE_B + (wave * C::CPW + c) * 1024), 16, 0, 0);
+  };
+  auto issue_scales = [&](int g) {
+#pragma unroll
+    for (int c = 0; c < SPW; ++c)
+      if (wave + c * C::NW < SP)
+        __builtin_amdgcn_global_load_lds((glb_void)(ssrc[c] + g * 4),
+                                         (lds_void)(smem + C::OFF_S + (g & 1) * (C::BM + C::BN) * 4 + (wave + c * C::NW) * 256), 4, 0, 0);
+  };
+
+  f32x16 acc[C::WTM][C::WTN];
+#pragma unroll
+  for (int j = 0; j < C::WTN; ++j) {
+    f32x16 start;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) start[r] = 0.f;
+    if (!SLICE && a.bias) {                                  // register r of a lane is column 8 (r/4) + 4 half + r%4 of the tile
+      const float* bias = a.bias + w * a.bias_stride;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int64_t n = col0 + wn0 + j * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
+        start[r] = bias[n < a.n ? n : a.n - 1];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < C::WTM; ++i) acc[i][j] = start;
+  }
+
+  struct Frags { i32x8 x[C::WTM], y[C::WTN]; };
+  auto frag = [&](const char* base, int row) {               // 32 numbers of a row: the lane's half of the step
+    const char* p = base + row * BK;
+    const int s = swizzle(row);
+    const uint4 lo = *reinterpret_cast<const uint4*>(p + (((half * 2) ^ s) << 4));
+    const uint4 hi = *reinterpret_cast<const uint4*>(p + (((half * 2 + 1) ^ s) << 4));
+    i32x8 v = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+    return v;
+  };
+  auto read_frags = [&](Frags& f, int st) {
+    const char* base = smem + st * C::STAGE_B;
+#pragma unroll
+    for (int i = 0; i < C::WTM; ++i) f.x[i] = frag(base, wm0 + i * 32 + l32);
+#pragma unroll
+    for (int j = 0; j < C::WTN; ++j) f.y[j] = frag(base + C::A_B, wn0 + j * 32 + l32);
+  };
+  int sx[C::WTM], sy[C::WTN], nx[C::WTM], ny[C::WTN];        // scale words: of the present steps, of the next group
+  auto read_scales = [&](int g) {
+    const char* base = smem + C::OFF_S + (g & 1) * (C::BM + C::BN) * 4;
+#pragma unroll
+    for (int i = 0; i < C::WTM; ++i) nx[i] = *reinterpret_cast<const int*>(base + (wm0 + i * 32 + l32) * 4);
+#pragma unroll
+    for (int j = 0; j < C::WTN; ++j) ny[j] = *reinterpret_cast<const int*>(base + (C::BM + wn0 + j * 32 + l32) * 4);
+  };
+  auto take_scales = [&]() {
+#pragma unroll
+    for (int i = 0; i < C::WTM; ++i) sx[i] = nx[i];
+#pragma unroll
+    for (int j = 0; j < C::WTN; ++j) sy[j] = ny[j];
+  };
+  auto next_scales = [&](int t) {                            // after step t, an odd one: the block of 128 is done
+    if (((t + 1) & (GROUP - 1)) == 0) { take_scales(); return; }
+#pragma unroll
+    for (int i = 0; i < C::WTM; ++i) sx[i] = (int)((unsigned)sx[i] >> 8);
+#pragma unroll
+    for (int j = 0; j < C::WTN; ++j) sy[j] = (int)((unsigned)sy[j] >> 8);
+  };
+  auto multiply = [&](Frags& f) {
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {                          // 8 of the lane's 32 numbers: any four eights, the same of both
+        bf16x8 x[C::WTM], y[C::WTN];
+#pragma unroll
+        for (int i = 0; i < C::WTM; ++i) x[i] = widen(f.x[i][2 * q], f.x[i][2 * q + 1], power(sx[i]));
+#pragma unroll
+        for (int j = 0; j < C::WTN; ++j) y[j] = widen(f.y[j][2 * q], f.y[j][2 * q + 1], power(sy[j]));
+#pragma unroll
+        for (int i = 0; i < C::WTM; ++i)
+#pragma unroll
+          for (int j = 0; j < C::WTN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[j], x[i], acc[i][j], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < C::WTM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::WTN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.y[j], f.x[i], acc[i][j], 0, 0, 0, sy[j], 0, sx[i]);
+    }
+  };
+
+  issue_scales(0);
+#pragma unroll
+  for (int t = 0; t < STAGES; ++t)
+    if (t < steps) issue(t, t);
+  if (steps >= STAGES) wait_vm<C::CPW * (STAGES - 1)>();
+  else wait_vm<0>();
+  __syncthreads();
+  Frags f0, f1;
+  read_scales(0);
+  take_scales();
+  read_frags(f0, 0);
+
+  // Step t: its operands are in registers.  After the barrier every wave has read stage t, which is then loaded anew, and
+  // step t + 1 has arrived.  The counts leave the loads of the two steps behind it in flight; loads of scale words, which are
+  // not counted, only make a wait longer.
+  auto step = [&](Frags& now, Frags& next, int t, auto more) {
+    constexpr bool MORE = decltype(more)::value;             // step t + STAGES exists
+    if constexpr (MORE) wait_vm<C::CPW * (STAGES - 2)>();
+    else wait_vm<0>();
+    __syncthreads();
+    if constexpr (MORE) {
+      if (((t + STAGES) & (GROUP - 1)) == 0) issue_scales((t + STAGES) / GROUP);
+      issue(t + STAGES, t & (STAGES - 1));
+    }
+    if (t + 1 < steps) {
+      if (((t + 1) & (GROUP - 1)) == 0) read_scales((t + 1) / GROUP);
+      read_frags(next, (t + 1) & (STAGES - 1));
+    }
+    multiply(now);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int t = 0;
+  for (; t + STAGES < steps; t += 2) {                       // the number of steps is even
+    step(f0, f1, t, std::true_type{});
+    step(f1, f0, t + 1, std::true_type{});
+    next_scales(t + 1);
+  }
+  for (; t < steps; t += 2) {
+    step(f0, f1, t, std::false_type{});
+    step(f1, f0, t + 1, std::false_type{});
+    next_scales(t + 1);
+  }
+
+  __syncthreads();                                           // the stages are free: each wave stages its rows in its share
+  const int64_t rows_left = a.m - row0 - wm0, cols_left = a.n - col0 - wn0;
+  if constexpr (SLICE || EXACT) {
+    constexpr int RS = C::WTN * 128 + 16, LPR = C::WTN * 8, RPP = 64 / LPR;
+    static_assert(C::NW * 32 * RS <= C::OFF_S, "staging fits the stages");
+    char* wl = smem + wave * 32 * RS;
+    float* out = SLICE ? a.part + (((int64_t)blockIdx.y * a.k + w) * a.m + row0 + wm0) * a.n + col0 + wn0
+                       : reinterpret_cast<float*>(a.c) + w * a.c_stride + (row0 + wm0) * a.ldc + col0 + wn0;
+    const int64_t ld = SLICE ? a.n : a.ldc;
+#pragma unroll
+    for (int i = 0; i < C::WTM; ++i) {
+#pragma unroll
+      for (int j = 0; j < C::WTN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<float4*>(wl + l32 * RS + (j * 32 + g * 8 + half * 4) * 4) =
+              make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+#pragma unroll
+      for (int p = 0; p < 32 / RPP; ++p) {
+        const int row = p * RPP + lane / LPR, ch = lane % LPR;
+        const float4 v = *reinterpret_cast<const float4*>(wl + row * RS + ch * 16);
+        if (i * 32 + row < rows_left) {
+          const float f[4] = {v.x, v.y, v.z, v.w};
+          store16<F32>(out + (i * 32 + row) * ld, ch * 4, cols_left, f);
+        }
+      }
+    }
+  } else {
+    constexpr int RS = C::WTN * 64 + 16, LPR = C::WTN * 4, RPP = 64 / LPR;
+    char* wl = smem + wave * 32 * RS;
+    uint16_t* out = reinterpret_cast<uint16_t*>(a.c) + w * a.c_stride + (row0 + wm0) * a.ldc + col0 + wn0;
+#pragma unroll
+    for (int i = 0; i < C::WTM; ++i) {
+#pragma unroll
+      for (int j = 0; j < C::WTN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<uint2*>(wl + l32 * RS + (j * 32 + g * 8 + half * 4) * 2) =
+              make_uint2(pack_bf16(acc[i][j][4 * g], acc[i][j][4 * g + 1]), pack_bf16(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]));
+#pragma unroll
+      for (int p = 0; p < 32 / RPP; ++p) {
+        const int row = p * RPP + lane / LPR, ch = lane % LPR;
+        const uint4 v = *reinterpret_cast<const uint4*>(wl + row * RS + ch * 16);
+        if (i * 32 + row < rows_left) {
+          uint16_t* o = out + (int64_t)(i * 32 + row) * a.ldc;
+          if (ch * 8 + 8 <= cols_left) {
+            *reinterpret_cast<Raw16a2*>(o + ch * 8) = Raw16a2{{v.x, v.y, v.z, v.w}};
+          } else {
+            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (ch * 8 + e < cols_left) o[ch * 8 + e] = (uint16_t)(u[e >> 1] >> (16 * (e & 1)));
+          }
+        }
+      }
+    }
+  }
+}
+
+// an empty contraction: the bias, or zeros
+__global__ __launch_bounds__(256) void bias_rows_kernel(Fp8Args a) {
+  const int w = blockIdx.z;
+  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (n >= a.n) return;
+  const float v = a.bias ? a.bias[w * a.bias_stride + n] : 0.f;
+  for (int64_t m = blockIdx.y; m < a.m; m += gridDim.y) {
+    const int64_t at = w * a.c_stride + m * a.ldc + n;
+    if (a.dtype == DW_F32) F32::put(reinterpret_cast<float*>(a.c) + at, v);
+    else Bf16::put(reinterpret_cast<uint16_t*>(a.c) + at, v);
+  }
+}
+
+using Large = Config<4, 4, 2, 2, 1>;                         // 256 x 256, a wave 128 x 128
+using Middle = Config<2, 2, 2, 2, 2>;                        // 128 x 128
+using Small = Config<1, 1, 2, 2, 2>;                         // 64 x 64
+
+template <class C, bool EXACT>
+hipError_t launch_one(const Fp8Args& a, hipStream_t s) {
+  const int64_t tiles = ceil_div(a.m, C::BM) * ceil_div(a.n, C::BN) * a.k;
+  auto kern = gemm_fp8_kernel<C, EXACT, false>;
+  static LdsLimitOnce lds_limit;
+  const hipError_t e = lds_limit.raise(reinterpret_cast<const void*>(kern), C::LDS);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(tiles, 8) * 8)), dim3(C::NT), C::LDS, s, a);
+  return hipGetLastError();
+}
+
+template <class C>
+hipError_t launch(const Fp8Args& a, hipStream_t s) {
+  return a.dtype == DW_F32 ? launch_one<C, true>(a, s) : launch_one<C, false>(a, s);
+}
+
+int64_t tiles_of(const Fp8Args& a, int b) { return ceil_div(a.m, b) * ceil_div(a.n, b) * a.k; }
+
+}  // namespace fp8
+
+hipError_t launch_fp8_matmul(const Fp8Args& a, hipStream_t s) {
+  if (a.kp == 0) {
+    const dim3 grid((unsigned)ceil_div(a.n, 256), (unsigned)(a.m < 1024 ? a.m : 1024), (unsigned)a.k);
+    hipLaunchKernelGGL(fp8::bias_rows_kernel, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  if (fp8::tiles_of(a, 256) >= kCus) return fp8::launch<fp8::Large>(a, s);
+  if (fp8::tiles_of(a, 128) >= kCus) return fp8::launch<fp8::Middle>(a, s);
+  return fp8::launch<fp8::Small>(a, s);
+}
+
+}  // namespace dw

@@ -211,4 +211,25 @@ hipError_t launch_grad_squares(const ClipTable& t, hipStream_t s);
 hipError_t launch_grad_norm(const double* part, int parts, float* norm, int k, hipStream_t s);
 hipError_t launch_clip(const ClipTable& t, hipStream_t s);
 
+// ---- 8-bit block products (dw_fp8_quant.hip, dw_gemm_fp8.hip) ----------------------------------------------------------
+struct QuantArgs {
+  Rows x;
+  int k, square;
+  int64_t rows, n;
+  uint8_t* q; uint8_t* scale;                              // [k][rows][DW_FP8_ROW(n)], [k][rows][DW_FP8_SCALES(n)], or nullptr
+  uint8_t* qt; uint8_t* scale_t;                           // [k][n][DW_FP8_ROW(rows)], [k][n][DW_FP8_SCALES(rows)], or nullptr
+};
+hipError_t launch_fp8_quantize(const QuantArgs& a, int dtype, hipStream_t s);
+
+struct Fp8Args {
+  const uint8_t* a; const uint8_t* sa;                     // [k][m][kp], [k][m][ks]
+  const uint8_t* b; const uint8_t* sb;                     // [k][n][kp], [k][n][ks]
+  const float* bias; int64_t bias_stride;                  // [k] rows of n, or nullptr
+  void* c; int64_t ldc, c_stride;
+  int k, dtype;
+  int64_t m, n, kp, ks;                                    // kp: padded contraction; ks: scale bytes of a row
+  float* part; int slice_steps;                            // slices of the contraction: [slices][k][m][n], steps of 64 each
+};
+hipError_t launch_fp8_matmul(const Fp8Args& a, hipStream_t s);
+
 }  // namespace dw

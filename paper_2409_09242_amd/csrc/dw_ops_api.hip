@@ -223,4 +223,44 @@ int dw_clip_grads(const void* const* h_grad, const int64_t* h_count, const int32
   return DW_OK;
 }
 
+int dw_fp8_quantize(const void* d_x, int64_t x_ld, int64_t x_stride, int k, int64_t rows, int64_t n, int dtype, int square,
+                    uint8_t* d_q, uint8_t* d_scale, uint8_t* d_qt, uint8_t* d_scale_t, void* stream) {
+  if (k < 1 || k > DW_MAX_K || !is_type(dtype)) return DW_ERR_CONFIG;
+  if (rows < 0 || rows > DW_MAX_FP8 || n < 1 || n > DW_MAX_FP8 || (square != 0 && square != 1)) return DW_ERR_ARG;
+  if (rows == 0) return DW_OK;                              // rows of the transposed matrix are empty too
+  if (!d_x || (d_q && !d_scale) || (d_qt && !d_scale_t) || (!d_q && !d_qt)) return DW_ERR_NULL;
+  if (!in_ok(d_x, x_ld, x_stride, rows, n, type_bytes(dtype))) return DW_ERR_ARG;
+  if (!aligned(d_q, 16) || !aligned(d_qt, 16) || !aligned(d_scale, 4) || !aligned(d_scale_t, 4)) return DW_ERR_ARG;
+  QuantArgs a = {};
+  a.x = {d_x, x_ld, x_stride};
+  a.k = k; a.square = square; a.rows = rows; a.n = n;
+  a.q = d_q; a.scale = d_scale; a.qt = d_qt; a.scale_t = d_scale_t;
+  DW_HIP(launch_fp8_quantize(a, dtype, (hipStream_t)stream));
+  return DW_OK;
+}
+
+size_t dw_fp8_matmul_scratch_bytes(int k, int64_t m, int64_t n, int64_t contraction) {
+  return 0;
+}
+
+int dw_fp8_matmul(const uint8_t* d_a, const uint8_t* d_a_scale, const uint8_t* d_b, const uint8_t* d_b_scale, const float* d_bias,
+                  int64_t bias_stride, int k, int64_t m, int64_t n, int64_t contraction, int dtype, void* d_c, int64_t c_ld,
+                  int64_t c_stride, void* d_scratch, size_t scratch_bytes, void* stream) {
+  if (k < 1 || k > DW_MAX_K || !is_type(dtype)) return DW_ERR_CONFIG;
+  if (m < 0 || m > DW_MAX_FP8 || n < 1 || n > DW_MAX_FP8 || contraction < 0 || contraction > DW_MAX_FP8) return DW_ERR_ARG;
+  if (m == 0) return DW_OK;
+  if (!d_c || (contraction > 0 && (!d_a || !d_a_scale || !d_b || !d_b_scale))) return DW_ERR_NULL;
+  if (!aligned(d_a, 16) || !aligned(d_b, 16) || !aligned(d_a_scale, 4) || !aligned(d_b_scale, 4)) return DW_ERR_ARG;
+  if (!params_ok(d_bias, bias_stride) || !out_ok(d_c, c_ld, c_stride, k, m, n, type_bytes(dtype))) return DW_ERR_ARG;
+  if (ceil_div(m, 64) * ceil_div(n, 64) * k > (1 << 22)) return DW_ERR_TOO_LARGE;
+  Fp8Args a = {};
+  a.a = d_a; a.sa = d_a_scale; a.b = d_b; a.sb = d_b_scale;
+  a.bias = d_bias; a.bias_stride = bias_stride;
+  a.c = d_c; a.ldc = c_ld; a.c_stride = c_stride;
+  a.k = k; a.dtype = dtype; a.m = m; a.n = n;
+  a.kp = DW_FP8_ROW(contraction); a.ks = DW_FP8_SCALES(contraction);
+  DW_HIP(launch_fp8_matmul(a, (hipStream_t)stream));
+  return DW_OK;
+}
+
 }  // extern "C"

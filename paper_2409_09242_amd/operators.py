@@ -249,3 +249,64 @@ def clip_grads(grads, max_norm: float, workers: int = 1, out=None):
 def grad_norm(grads, workers: int = 1):
     """The global 2-norm of every worker's gradients, float32 [workers]; grads as for clip_grads."""
     return _clip(grads, float("inf"), workers, None, "dw_clip_grads")
+
+
+# ---- products in 8 bits ----------------------------------------------------------------------------------------------
+
+class Fp8Matrix:
+    """[k][rows] rows of n numbers in e4m3, each row padded with zeros to whole blocks of 128, and their scales.
+
+    q: float8_e4m3fn [k][rows][padded n]; scale: uint8 [k][rows][blocks, to a multiple of 4], 2^(scale - 127)."""
+
+    __slots__ = ("q", "scale", "n")
+
+    def __init__(self, k: int, rows: int, n: int, device):
+        self.n = n
+        self.q = torch.empty((k, rows, (n + 127) // 128 * 128), dtype=torch.float8_e4m3fn, device=device)
+        self.scale = torch.empty((k, rows, (n + 511) // 512 * 4), dtype=torch.uint8, device=device)
+
+    @property
+    def shape(self):
+        return (self.q.shape[0], self.q.shape[1], self.n)
+
+
+def fp8_quantize(x, square: bool = False, transposed: bool = False):
+    """x [k][rows][n] in 8 bits with a scale per block of 128 along its rows (square: per 128 x 128), an Fp8Matrix.
+    transposed=True: (that, the same of x^T): [k][n] rows of `rows`, its blocks along those."""
+    code = _type(x, "x")
+    xp, x_ld, x_st = _matrix(x, "x")
+    k, rows, n = x.shape
+    dev = x.device
+    stream, guard = _on(dev)
+    m = Fp8Matrix(k, rows, n, dev)
+    t = Fp8Matrix(k, n, rows, dev) if transposed else None
+    with guard:
+        _check(B.lib().dw_fp8_quantize(xp, x_ld, x_st, k, rows, n, code, int(square), m.q.data_ptr(), m.scale.data_ptr(),
+                                       t.q.data_ptr() if t else None, t.scale.data_ptr() if t else None, stream), "dw_fp8_quantize")
+    return (m, t) if transposed else m
+
+
+def fp8_matmul(a: Fp8Matrix, b: Fp8Matrix, bias=None, dtype=torch.bfloat16, out=None):
+    """a b^T (+ bias) per worker: a [k][m] and b [k][n] rows of the same length; [k][m][n] in dtype, or into out."""
+    k, m, length = a.shape
+    if b.shape[0] != k or b.n != length or b.q.device != a.q.device:
+        raise ValueError("operands of %s and %s" % (a.shape, b.shape))
+    n, dev = b.shape[1], a.q.device
+    stream, guard = _on(dev)
+    bp, b_st = _param(bias, "bias", k, n, dev)
+    if out is None:
+        out = torch.empty((k, m, n), dtype=dtype, device=dev)
+    code = _type(out, "out")
+    cp, c_ld, c_st = _matrix(out, "out", (k, m, n), None, dev)
+    L = B.lib()
+    nbytes = L.dw_fp8_matmul_scratch_bytes(k, m, n, length)
+    scratch, sp = _scratch(nbytes, dev)
+    with guard:
+        _check(L.dw_fp8_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), bp, b_st, k, m, n, length,
+                               code, cp, c_ld, c_st, sp, nbytes, stream), "dw_fp8_matmul")
+    return out
+
+
+def fp8_linear(x, weight: Fp8Matrix, bias=None, out=None):
+    """x W^T (+ bias) with x [k][rows][n] quantised on the way and W kept in 8 bits; [k][rows][W's rows] in x's type."""
+    return fp8_matmul(fp8_quantize(x), weight, bias, dtype=x.dtype, out=out)
