@@ -31,8 +31,7 @@ namespace fp8 {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) void* lds_void;
-typedef __attribute__((address_space(1))) const void* glb_void;
+typedef __attribute__((address_space(3))) const char* lds_char;
 
 constexpr int BK = 64, STAGES = 4, GROUP = 8;               // bytes of a step, steps in flight, steps per word of scales
 
@@ -41,6 +40,25 @@ template <int N>
 __device__ __forceinline__ void wait_vm() {
   static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (0x7 << 4) | (0x0 << 8));
+}
+
+// Each lane's N bytes at base + offset go to LDS at `to` + N * lane; no register receives anything.  Written as assembly
+// because behind the builtin the compiler waits for every load in flight before each read of LDS: it cannot tell that the
+// read is of another stage.  The waits are the kernel's own (wait_vm before the barrier that precedes a stage's reads).
+// m0 holds the place in LDS; nothing else in these kernels uses it.
+template <int N>
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint32_t to) {
+#if defined(__HIP_DEVICE_COMPILE__)                          // (the host's pass does not know the constraint "s")
+  if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base));
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base));
+#endif
+}
+
+// an address that is the same in all lanes, in scalar registers
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const uint8_t*>((uint64_t)hi << 32 | lo);
 }
 
 template <int WTM_, int WTN_, int WM_, int WN_, int PER_CU_>
@@ -53,6 +71,7 @@ struct Config {
   static constexpr int OFF_S = STAGE_B * STAGES;            // two groups of scale words, (BM + BN) each
   static constexpr int LDS = OFF_S + 2 * (BM + BN) * 4;
   static_assert(STAGE_B % (1024 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0, "whole pieces");
+  static_assert(BM == BN && NW % 2 == 0, "half of the waves load A's tile, the others B's");
 };
 
 __device__ __forceinline__ int swizzle(int row) { return (row >> 2) & 3; }
@@ -66,7 +85,7 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
   r.v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return __builtin_bit_cast(bf16x8, r);
 }
-__device__ __forceinline__ float power(int word) { return __uint_as_float(((unsigned)word & 255u) << 23); }
+__device__ __forceinline__ float power(int byte) { return __uint_as_float((unsigned)byte << 23); }
 
 template <class C, bool EXACT, bool SLICE>
 __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
@@ -95,40 +114,43 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   const int step0 = SLICE ? (int)blockIdx.y * a.slice_steps : 0;
   const int steps = SLICE ? (all_steps - step0 < a.slice_steps ? all_steps - step0 : a.slice_steps) : all_steps;
 
-  // where the pieces this wave moves come from (step 0): piece c holds rows 16c .. 16c+15 of A's and then B's tile
-  const uint8_t* src[C::CPW];
+  // The pieces this wave moves: the first half of the waves A's tile, the others B's; piece c holds rows 16c .. 16c+15.  A
+  // uniform base that advances by a step, and a lane's offset from it (a tile's rows span less than 2^32 bytes).
+  const bool of_a = wave < C::NW / 2;
+  const int first = (of_a ? wave : wave - C::NW / 2) * C::CPW;
+  const int64_t tile0 = of_a ? row0 : col0, all_rows = of_a ? a.m : a.n;
+  const uint8_t* base = (of_a ? A : Bm) + tile0 * kp + (int64_t)step0 * BK;
+  uint32_t off[C::CPW];
 #pragma unroll
   for (int c = 0; c < C::CPW; ++c) {
-    const int row = (wave * C::CPW + c) * 16 + (lane >> 2), q = (lane & 3) ^ swizzle(row);
-    int64_t r;
-    if (row < C::BM) { r = row0 + row; src[c] = A + (r < a.m ? r : a.m - 1) * kp + q * 16; }
-    else { r = col0 + row - C::BM; src[c] = Bm + (r < a.n ? r : a.n - 1) * kp + q * 16; }
-    src[c] += (int64_t)step0 * BK;
+    const int row = (first + c) * 16 + (lane >> 2), q = (lane & 3) ^ swizzle(row);
+    const int64_t r = tile0 + row < all_rows ? row : all_rows - 1 - tile0;
+    off[c] = (uint32_t)(r * kp + q * 16);
   }
-  // scale words: 64 rows at a time, the waves in turn
-  constexpr int SP = (C::BM + C::BN) / 64, SPW = (SP + C::NW - 1) / C::NW;
-  const uint8_t* ssrc[SPW];
+  // scale words, 64 rows at a time: the same halves
+  constexpr int SP = C::BM / 64, SPW = (SP + C::NW / 2 - 1) / (C::NW / 2);
+  const int sfirst = of_a ? wave : wave - C::NW / 2;
+  const uint8_t* sbase = (of_a ? sA : sB) + tile0 * a.ks + step0 / 2;
+  uint32_t soff[SPW];
 #pragma unroll
   for (int c = 0; c < SPW; ++c) {
-    int p = wave + c * C::NW; p = p < SP ? p : SP - 1;
-    const int row = p * 64 + lane;
-    int64_t r;
-    if (row < C::BM) { r = row0 + row; ssrc[c] = sA + (r < a.m ? r : a.m - 1) * a.ks; }
-    else { r = col0 + row - C::BM; ssrc[c] = sB + (r < a.n ? r : a.n - 1) * a.ks; }
-    ssrc[c] += step0 / 2;
+    const int row = (sfirst + c * (C::NW / 2)) * 64 + lane;
+    soff[c] = (uint32_t)((tile0 + row < all_rows ? row : all_rows - 1 - tile0) * a.ks);
   }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char)smem;
+  const uint32_t lds_tile = __builtin_amdgcn_readfirstlane(lds0 + (of_a ? 0 : C::A_B) + first * 1024);
+  const uint32_t lds_scale = __builtin_amdgcn_readfirstlane(lds0 + C::OFF_S + (of_a ? 0 : C::BM * 4));
   auto issue = [&](int t, int st) {
+    const uint8_t* from = uniform(base + (int64_t)t * BK);
 #pragma unroll
-    for (int c = 0; c < C::CPW; ++c)
-      __builtin_amdgcn_global_load_lds((glb_void)(src[c] + (int64_t)t * BK),
-                                       (lds_void)(smem + st * C::STAGE_B + (wave * C::CPW + c) * 1024), 16, 0, 0);
+    for (int c = 0; c < C::CPW; ++c) load_to_lds<16>(from, off[c], lds_tile + st * C::STAGE_B + c * 1024);
   };
   auto issue_scales = [&](int g) {
+    const uint8_t* from = uniform(sbase + g * 4);
 #pragma unroll
     for (int c = 0; c < SPW; ++c)
-      if (wave + c * C::NW < SP)
-        __builtin_amdgcn_global_load_lds((glb_void)(ssrc[c] + g * 4),
-                                         (lds_void)(smem + C::OFF_S + (g & 1) * (C::BM + C::BN) * 4 + (wave + c * C::NW) * 256), 4, 0, 0);
+      if (sfirst + c * (C::NW / 2) < SP)
+        load_to_lds<4>(from, soff[c], lds_scale + (g & 1) * (C::BM + C::BN) * 4 + (sfirst + c * (C::NW / 2)) * 256);
   };
 
   f32x16 acc[C::WTM][C::WTN];
@@ -150,8 +172,8 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   }
 
   struct Frags { i32x8 x[C::WTM], y[C::WTN]; };
-  auto frag = [&](const char* base, int row) {               // 32 numbers of a row: the lane's half of the step
-    const char* p = base + row * BK;
+  auto frag = [&](const char* rows, int row) {               // 32 numbers of a row: the lane's half of the step
+    const char* p = rows + row * BK;
     const int s = swizzle(row);
     const uint4 lo = *reinterpret_cast<const uint4*>(p + (((half * 2) ^ s) << 4));
     const uint4 hi = *reinterpret_cast<const uint4*>(p + (((half * 2 + 1) ^ s) << 4));
@@ -159,32 +181,25 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
     return v;
   };
   auto read_frags = [&](Frags& f, int st) {
-    const char* base = smem + st * C::STAGE_B;
+    const char* stage = smem + st * C::STAGE_B;
 #pragma unroll
-    for (int i = 0; i < C::WTM; ++i) f.x[i] = frag(base, wm0 + i * 32 + l32);
+    for (int i = 0; i < C::WTM; ++i) f.x[i] = frag(stage, wm0 + i * 32 + l32);
 #pragma unroll
-    for (int j = 0; j < C::WTN; ++j) f.y[j] = frag(base + C::A_B, wn0 + j * 32 + l32);
+    for (int j = 0; j < C::WTN; ++j) f.y[j] = frag(stage + C::A_B, wn0 + j * 32 + l32);
   };
-  int sx[C::WTM], sy[C::WTN], nx[C::WTM], ny[C::WTN];        // scale words: of the present steps, of the next group
-  auto read_scales = [&](int g) {
-    const char* base = smem + C::OFF_S + (g & 1) * (C::BM + C::BN) * 4;
+  int sx[C::WTM], sy[C::WTN], nx[C::WTM], ny[C::WTN];        // scale bytes: of the present block of 128, of the next
+  auto read_scales = [&](int blk) {
+    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(smem) + C::OFF_S + ((blk / 4) & 1) * (C::BM + C::BN) * 4 + (blk & 3);
 #pragma unroll
-    for (int i = 0; i < C::WTM; ++i) nx[i] = *reinterpret_cast<const int*>(base + (wm0 + i * 32 + l32) * 4);
+    for (int i = 0; i < C::WTM; ++i) nx[i] = bytes[(wm0 + i * 32 + l32) * 4];
 #pragma unroll
-    for (int j = 0; j < C::WTN; ++j) ny[j] = *reinterpret_cast<const int*>(base + (C::BM + wn0 + j * 32 + l32) * 4);
+    for (int j = 0; j < C::WTN; ++j) ny[j] = bytes[(C::BM + wn0 + j * 32 + l32) * 4];
   };
   auto take_scales = [&]() {
 #pragma unroll
     for (int i = 0; i < C::WTM; ++i) sx[i] = nx[i];
 #pragma unroll
     for (int j = 0; j < C::WTN; ++j) sy[j] = ny[j];
-  };
-  auto next_scales = [&](int t) {                            // after step t, an odd one: the block of 128 is done
-    if (((t + 1) & (GROUP - 1)) == 0) { take_scales(); return; }
-#pragma unroll
-    for (int i = 0; i < C::WTM; ++i) sx[i] = (int)((unsigned)sx[i] >> 8);
-#pragma unroll
-    for (int j = 0; j < C::WTN; ++j) sy[j] = (int)((unsigned)sy[j] >> 8);
   };
   auto multiply = [&](Frags& f) {
     if constexpr (EXACT) {
@@ -223,33 +238,43 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
 
   // Step t: its operands are in registers.  After the barrier every wave has read stage t, which is then loaded anew, and
   // step t + 1 has arrived.  The counts leave the loads of the two steps behind it in flight; loads of scale words, which are
-  // not counted, only make a wait longer.
-  auto step = [&](Frags& now, Frags& next, int t, auto more) {
-    constexpr bool MORE = decltype(more)::value;             // step t + STAGES exists
+  // not counted, only make a wait longer.  A step is one straight line: a read of LDS behind every product, so that
+  // neither waits for all of the other.
+  auto step = [&](Frags& now, Frags& next, int t, auto more, auto odd) {
+    constexpr bool MORE = decltype(more)::value, ODD = decltype(odd)::value;      // MORE: step t + STAGES exists
     if constexpr (MORE) wait_vm<C::CPW * (STAGES - 2)>();
     else wait_vm<0>();
     __syncthreads();
-    if constexpr (MORE) {
+    if constexpr (MORE && !ODD) {
       if (((t + STAGES) & (GROUP - 1)) == 0) issue_scales((t + STAGES) / GROUP);
-      issue(t + STAGES, t & (STAGES - 1));
     }
-    if (t + 1 < steps) {
-      if (((t + 1) & (GROUP - 1)) == 0) read_scales((t + 1) / GROUP);
+    if constexpr (MORE) issue(t + STAGES, t & (STAGES - 1));
+    if (MORE || !ODD || t + 1 < steps) {                     // (the number of steps is even)
       read_frags(next, (t + 1) & (STAGES - 1));
+      if constexpr (ODD) read_scales((t + 1) / 2);
     }
     multiply(now);
+    if constexpr (!EXACT) {
+      constexpr int PRODUCTS = C::WTM * C::WTN, READS = 2 * (C::WTM + C::WTN) + (ODD ? C::WTM + C::WTN : 0);
+#pragma unroll
+      for (int q = 0; q < PRODUCTS; ++q) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, (READS + PRODUCTS - 1) / PRODUCTS, 0);
+      }
+    }
+    if constexpr (ODD) take_scales();
     __builtin_amdgcn_sched_barrier(0);
   };
+  using yes = std::true_type;
+  using no = std::false_type;
   int t = 0;
-  for (; t + STAGES < steps; t += 2) {                       // the number of steps is even
-    step(f0, f1, t, std::true_type{});
-    step(f1, f0, t + 1, std::true_type{});
-    next_scales(t + 1);
+  for (; t + STAGES < steps; t += 2) {
+    step(f0, f1, t, yes{}, no{});
+    step(f1, f0, t + 1, yes{}, yes{});
   }
   for (; t < steps; t += 2) {
-    step(f0, f1, t, std::false_type{});
-    step(f1, f0, t + 1, std::false_type{});
-    next_scales(t + 1);
+    step(f0, f1, t, no{}, no{});
+    step(f1, f0, t + 1, no{}, yes{});
   }
 
   __syncthreads();                                           // the stages are free: each wave stages its rows in its share
