@@ -21,6 +21,7 @@
 // consecutive columns, which leave through a piece of LDS of the wave's own as whole row pieces of 16 bytes a lane.
 // The accumulators start from the bias.  Rows past the end of a matrix repeat the last one; what they give is not written.
 #include <type_traits>
+#include <utility>
 
 #include "dw_ops.h"
 
@@ -53,6 +54,12 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset
   else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(offset), "s"(base));
 #endif
 }
+
+// f(0) .. f(N - 1) with the index as a constant: the products of a step and what is dealt out among them have to unroll
+template <int FROM, int... I, class F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, FROM + I>{}), ...); }
+template <int FROM, int TO, class F>
+__device__ __forceinline__ void each(F f) { each_of<FROM>(std::make_integer_sequence<int, (TO > FROM ? TO - FROM : 0)>{}, f); }
 
 // an address that is the same in all lanes, in scalar registers
 __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
@@ -140,11 +147,7 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char)smem;
   const uint32_t lds_tile = __builtin_amdgcn_readfirstlane(lds0 + (of_a ? 0 : C::A_B) + first * 1024);
   const uint32_t lds_scale = __builtin_amdgcn_readfirstlane(lds0 + C::OFF_S + (of_a ? 0 : C::BM * 4));
-  auto issue = [&](int t, int st) {
-    const uint8_t* from = uniform(base + (int64_t)t * BK);
-#pragma unroll
-    for (int c = 0; c < C::CPW; ++c) load_to_lds<16>(from, off[c], lds_tile + st * C::STAGE_B + c * 1024);
-  };
+  auto issue = [&](const uint8_t* from, int st, int c) { load_to_lds<16>(from, off[c], lds_tile + st * C::STAGE_B + c * 1024); };
   auto issue_scales = [&](int g) {
     const uint8_t* from = uniform(sbase + g * 4);
 #pragma unroll
@@ -171,21 +174,20 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
     for (int i = 0; i < C::WTM; ++i) acc[i][j] = start;
   }
 
-  struct Frags { i32x8 x[C::WTM], y[C::WTN]; };
-  auto frag = [&](const char* rows, int row) {               // 32 numbers of a row: the lane's half of the step
-    const char* p = rows + row * BK;
-    const int s = swizzle(row);
-    const uint4 lo = *reinterpret_cast<const uint4*>(p + (((half * 2) ^ s) << 4));
-    const uint4 hi = *reinterpret_cast<const uint4*>(p + (((half * 2 + 1) ^ s) << 4));
-    i32x8 v = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-    return v;
-  };
-  auto read_frags = [&](Frags& f, int st) {
+  // the 32 numbers of a lane's half of a step, for each row of the wave's tile; read in halves of 16
+  struct Frags { uint4 x[C::WTM][2], y[C::WTN][2]; };
+  constexpr int READS = 2 * (C::WTM + C::WTN);
+  uint32_t at_x[2], at_y[2];                                 // where row 0 of the lane's rows lies in a stage
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {                              // (rows 32 apart are swizzled alike)
+    at_x[h] = (wm0 + l32) * BK + (((half * 2 + h) ^ swizzle(wm0 + l32)) << 4);
+    at_y[h] = C::A_B + (wn0 + l32) * BK + (((half * 2 + h) ^ swizzle(wn0 + l32)) << 4);
+  }
+  auto read_one = [&](Frags& f, int st, int r) {
     const char* stage = smem + st * C::STAGE_B;
-#pragma unroll
-    for (int i = 0; i < C::WTM; ++i) f.x[i] = frag(stage, wm0 + i * 32 + l32);
-#pragma unroll
-    for (int j = 0; j < C::WTN; ++j) f.y[j] = frag(stage + C::A_B, wn0 + j * 32 + l32);
+    const int h = r & 1, i = r >> 1;
+    if (i < C::WTM) f.x[i][h] = *reinterpret_cast<const uint4*>(stage + at_x[h] + i * 32 * BK);
+    else f.y[i - C::WTM][h] = *reinterpret_cast<const uint4*>(stage + at_y[h] + (i - C::WTM) * 32 * BK);
   };
   int sx[C::WTM], sy[C::WTN], nx[C::WTM], ny[C::WTN];        // scale bytes: of the present block of 128, of the next
   auto read_scales = [&](int blk) {
@@ -201,45 +203,42 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
 #pragma unroll
     for (int j = 0; j < C::WTN; ++j) sy[j] = ny[j];
   };
-  auto multiply = [&](Frags& f) {
-    if constexpr (EXACT) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {                          // 8 of the lane's 32 numbers: any four eights, the same of both
-        bf16x8 x[C::WTM], y[C::WTN];
-#pragma unroll
-        for (int i = 0; i < C::WTM; ++i) x[i] = widen(f.x[i][2 * q], f.x[i][2 * q + 1], power(sx[i]));
-#pragma unroll
-        for (int j = 0; j < C::WTN; ++j) y[j] = widen(f.y[j][2 * q], f.y[j][2 * q + 1], power(sy[j]));
-#pragma unroll
-        for (int i = 0; i < C::WTM; ++i)
-#pragma unroll
-          for (int j = 0; j < C::WTN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[j], x[i], acc[i][j], 0, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < C::WTM; ++i)
-#pragma unroll
-        for (int j = 0; j < C::WTN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.y[j], f.x[i], acc[i][j], 0, 0, 0, sy[j], 0, sx[i]);
-    }
+  // what multiplies operand row i of a by row j of b: both halves at once, or (EXACT) eight numbers, q of four, widened before
+  auto whole = [](const uint4 (&v)[2]) {
+    const i32x8 r = {(int)v[0].x, (int)v[0].y, (int)v[0].z, (int)v[0].w, (int)v[1].x, (int)v[1].y, (int)v[1].z, (int)v[1].w};
+    return r;
+  };
+  auto eight = [](const uint4 (&v)[2], int q, int scale) {
+    const uint4 u = v[q >> 1];
+    return q & 1 ? widen((int)u.z, (int)u.w, power(scale)) : widen((int)u.x, (int)u.y, power(scale));
+  };
+  struct Wide { bf16x8 x[C::WTM], y[C::WTN]; };
+  auto widen_one = [&](Wide& d, const Frags& f, int q, int i) {
+    if (i < C::WTM) d.x[i] = eight(f.x[i], q, sx[i]);
+    else d.y[i - C::WTM] = eight(f.y[i - C::WTM], q, sy[i - C::WTM]);
   };
 
   issue_scales(0);
 #pragma unroll
   for (int t = 0; t < STAGES; ++t)
-    if (t < steps) issue(t, t);
+    if (t < steps) {
+      const uint8_t* from = uniform(base + (int64_t)t * BK);
+#pragma unroll
+      for (int c = 0; c < C::CPW; ++c) issue(from, t, c);
+    }
   if (steps >= STAGES) wait_vm<C::CPW * (STAGES - 1)>();
   else wait_vm<0>();
   __syncthreads();
   Frags f0, f1;
   read_scales(0);
   take_scales();
-  read_frags(f0, 0);
+#pragma unroll
+  for (int r = 0; r < READS; ++r) read_one(f0, 0, r);
 
   // Step t: its operands are in registers.  After the barrier every wave has read stage t, which is then loaded anew, and
   // step t + 1 has arrived.  The counts leave the loads of the two steps behind it in flight; loads of scale words, which are
-  // not counted, only make a wait longer.  A step is one straight line: a read of LDS behind every product, so that
-  // neither waits for all of the other.
+  // not counted, only make a wait longer.  Loads and reads are dealt out among the products and kept there: the four waves
+  // come from the barrier together, and a load put in front of the products would hold them all up.
   auto step = [&](Frags& now, Frags& next, int t, auto more, auto odd) {
     constexpr bool MORE = decltype(more)::value, ODD = decltype(odd)::value;      // MORE: step t + STAGES exists
     if constexpr (MORE) wait_vm<C::CPW * (STAGES - 2)>();
@@ -248,22 +247,32 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
     if constexpr (MORE && !ODD) {
       if (((t + STAGES) & (GROUP - 1)) == 0) issue_scales((t + STAGES) / GROUP);
     }
-    if constexpr (MORE) issue(t + STAGES, t & (STAGES - 1));
-    if (MORE || !ODD || t + 1 < steps) {                     // (the number of steps is even)
-      read_frags(next, (t + 1) & (STAGES - 1));
-      if constexpr (ODD) read_scales((t + 1) / 2);
-    }
-    multiply(now);
-    if constexpr (!EXACT) {
-      constexpr int PRODUCTS = C::WTM * C::WTN, READS = 2 * (C::WTM + C::WTN) + (ODD ? C::WTM + C::WTN : 0);
+    const bool reads = MORE || !ODD || t + 1 < steps;        // (the number of steps is even)
+    const uint8_t* from = uniform(base + (int64_t)(t + STAGES) * BK);
+    constexpr int Q = EXACT ? 4 : 1, PRODUCTS = C::WTM * C::WTN * Q, OPERANDS = C::WTM + C::WTN;
+    Wide wide[2];
+    if constexpr (EXACT) {
 #pragma unroll
-      for (int q = 0; q < PRODUCTS; ++q) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, (READS + PRODUCTS - 1) / PRODUCTS, 0);
-      }
+      for (int i = 0; i < OPERANDS; ++i) widen_one(wide[0], now, 0, i);
     }
-    if constexpr (ODD) take_scales();
     __builtin_amdgcn_sched_barrier(0);
+    each<0, PRODUCTS>([&](auto p_) {
+      constexpr int PN = C::WTM * C::WTN, p = decltype(p_)::value, q = p / PN, ij = p % PN, i = ij / C::WTN, j = ij % C::WTN;
+      if constexpr (EXACT) {
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[q & 1].y[j], wide[q & 1].x[i], acc[i][j], 0, 0, 0);
+        if constexpr (q + 1 < Q)
+          each<ij * OPERANDS / PN, (ij + 1) * OPERANDS / PN>([&](auto o) { widen_one(wide[(q + 1) & 1], now, q + 1, o); });
+      } else {
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(now.y[j]), whole(now.x[i]), acc[i][j], 0, 0, 0, sy[j], 0, sx[i]);
+      }
+      if constexpr (MORE) each<p * C::CPW / PRODUCTS, (p + 1) * C::CPW / PRODUCTS>([&](auto c) { issue(from, t & (STAGES - 1), c); });
+      if (reads) {
+        each<p * READS / PRODUCTS, (p + 1) * READS / PRODUCTS>([&](auto r) { read_one(next, (t + 1) & (STAGES - 1), r); });
+        if constexpr (ODD && p == PRODUCTS / 2) read_scales((t + 1) / 2);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (ODD) take_scales();
   };
   using yes = std::true_type;
   using no = std::false_type;
