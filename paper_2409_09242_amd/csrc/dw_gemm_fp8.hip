@@ -4,11 +4,11 @@
 //
 // v_mfma_scale_f32_32x32x64_f8f6f4 multiplies 32 x 64 by 64 x 32 numbers of 8 bits and applies both scales (one byte per
 // row and 32 numbers) by itself, so scaled blocks cost no more than unscaled ones and are accumulated in fp32 throughout.
-// The contraction runs in steps of 64: a tile of BM + BN rows of 64 bytes goes from memory straight to LDS
-// (global_load_lds, 16 bytes a lane), four steps are in flight or resident, and every wave reads the operands of the next
-// step from LDS while it multiplies the present one.  Rows of 64 bytes lie back to back, so the 16-byte piece q of row r
-// is kept in slot q ^ (r/4 mod 4): the 16 lanes that read at a time then touch all banks once.  A row's scales for 512
-// numbers are one word; words go through LDS too, a group of eight steps at a time.
+// The contraction runs in blocks of 128, two steps of 64 each: a tile of BM + BN rows of 128 bytes, whole lines, goes from
+// memory straight to LDS (global_load_lds, 16 bytes a lane), the next blocks are in flight, and every wave reads the operands
+// of the next step from LDS while it multiplies the present one.  Rows lie back to back, so the 16-byte piece q of row r
+// is kept in slot q ^ (r/2 mod 8): the 16 lanes that read at a time then touch all banks once.  A row's scales for 512
+// numbers are one word; words go through LDS too, four blocks at a time.
 //
 // That instruction adds eight neighbouring products at a time and keeps their bits down to 2^-13 of the largest one's power
 // (measured; all 8-bit matrix instructions of this chip do).  On normally distributed numbers the sums are then off by
@@ -34,7 +34,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) const char* lds_char;
 
-constexpr int BK = 64, STAGES = 4, GROUP = 8;               // bytes of a step, steps in flight, steps per word of scales
+constexpr int BK = 128, GROUP = 4;                          // bytes of a block, blocks per word of scales
 
 // at most N vector-memory operations of this wave outstanding (N < 64), its LDS reads all returned
 template <int N>
@@ -68,20 +68,21 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
   return reinterpret_cast<const uint8_t*>((uint64_t)hi << 32 | lo);
 }
 
-template <int WTM_, int WTN_, int WM_, int WN_, int PER_CU_>
+template <int WTM_, int WTN_, int WM_, int WN_, int PER_CU_, int STAGES_>
 struct Config {
-  static constexpr int WTM = WTM_, WTN = WTN_, WM = WM_, WN = WN_, PER_CU = PER_CU_;
+  static constexpr int WTM = WTM_, WTN = WTN_, WM = WM_, WN = WN_, PER_CU = PER_CU_, STAGES = STAGES_;
   static constexpr int NW = WM * WN, NT = NW * 64;
   static constexpr int BM = WM * WTM * 32, BN = WN * WTN * 32;
   static constexpr int A_B = BM * BK, STAGE_B = (BM + BN) * BK;
-  static constexpr int CPW = STAGE_B / 1024 / NW;           // 1 KB pieces a wave moves per step
+  static constexpr int CPW = STAGE_B / 1024 / NW;           // 1 KB pieces a wave moves per block
   static constexpr int OFF_S = STAGE_B * STAGES;            // two groups of scale words, (BM + BN) each
   static constexpr int LDS = OFF_S + 2 * (BM + BN) * 4;
   static_assert(STAGE_B % (1024 * NW) == 0 && BM % 64 == 0 && BN % 64 == 0, "whole pieces");
   static_assert(BM == BN && NW % 2 == 0, "half of the waves load A's tile, the others B's");
+  static_assert(STAGES >= 2 && STAGES <= GROUP && (STAGES & (STAGES - 1)) == 0, "a group of scales is read before it is loaded anew");
 };
 
-__device__ __forceinline__ int swizzle(int row) { return (row >> 2) & 3; }
+__device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 
 // eight numbers of 8 bits as bf16, times 2^(scale - 127)
 __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
@@ -116,28 +117,28 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   const uint8_t* Bm = a.b + w * a.n * kp;
   const uint8_t* sA = a.sa + w * a.m * a.ks;
   const uint8_t* sB = a.sb + w * a.n * a.ks;
-  // steps of this block: all, or one slice of the contraction (slices begin at whole words of scales)
-  const int all_steps = (int)(kp / BK);
-  const int step0 = SLICE ? (int)blockIdx.y * a.slice_steps : 0;
-  const int steps = SLICE ? (all_steps - step0 < a.slice_steps ? all_steps - step0 : a.slice_steps) : all_steps;
+  // blocks of 128 of this tile: all, or one slice of the contraction (slices begin at whole words of scales)
+  const int all_blocks = (int)(kp / BK);
+  const int block0 = SLICE ? (int)blockIdx.y * a.slice_blocks : 0;
+  const int blocks = SLICE ? (all_blocks - block0 < a.slice_blocks ? all_blocks - block0 : a.slice_blocks) : all_blocks;
 
-  // The pieces this wave moves: the first half of the waves A's tile, the others B's; piece c holds rows 16c .. 16c+15.  A
-  // uniform base that advances by a step, and a lane's offset from it (a tile's rows span less than 2^32 bytes).
+  // The pieces this wave moves: the first half of the waves A's tile, the others B's; piece c holds rows 8c .. 8c+7.  A
+  // uniform base that advances by a block, and a lane's offset from it (a tile's rows span less than 2^32 bytes).
   const bool of_a = wave < C::NW / 2;
   const int first = (of_a ? wave : wave - C::NW / 2) * C::CPW;
   const int64_t tile0 = of_a ? row0 : col0, all_rows = of_a ? a.m : a.n;
-  const uint8_t* base = (of_a ? A : Bm) + tile0 * kp + (int64_t)step0 * BK;
+  const uint8_t* base = (of_a ? A : Bm) + tile0 * kp + (int64_t)block0 * BK;
   uint32_t off[C::CPW];
 #pragma unroll
   for (int c = 0; c < C::CPW; ++c) {
-    const int row = (first + c) * 16 + (lane >> 2), q = (lane & 3) ^ swizzle(row);
+    const int row = (first + c) * 8 + (lane >> 3), q = (lane & 7) ^ swizzle(row);
     const int64_t r = tile0 + row < all_rows ? row : all_rows - 1 - tile0;
     off[c] = (uint32_t)(r * kp + q * 16);
   }
   // scale words, 64 rows at a time: the same halves
   constexpr int SP = C::BM / 64, SPW = (SP + C::NW / 2 - 1) / (C::NW / 2);
   const int sfirst = of_a ? wave : wave - C::NW / 2;
-  const uint8_t* sbase = (of_a ? sA : sB) + tile0 * a.ks + step0 / 2;
+  const uint8_t* sbase = (of_a ? sA : sB) + tile0 * a.ks + block0;
   uint32_t soff[SPW];
 #pragma unroll
   for (int c = 0; c < SPW; ++c) {
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char)smem;
   const uint32_t lds_tile = __builtin_amdgcn_readfirstlane(lds0 + (of_a ? 0 : C::A_B) + first * 1024);
   const uint32_t lds_scale = __builtin_amdgcn_readfirstlane(lds0 + C::OFF_S + (of_a ? 0 : C::BM * 4));
-  auto issue = [&](const uint8_t* from, int st, int c) { load_to_lds<16>(from, off[c], lds_tile + st * C::STAGE_B + c * 1024); };
+  auto issue = [&](const uint8_t* from, int b, int c) { load_to_lds<16>(from, off[c], lds_tile + (b & (C::STAGES - 1)) * C::STAGE_B + c * 1024); };
   auto issue_scales = [&](int g) {
     const uint8_t* from = uniform(sbase + g * 4);
 #pragma unroll
@@ -177,17 +178,18 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   // the 32 numbers of a lane's half of a step, for each row of the wave's tile; read in halves of 16
   struct Frags { uint4 x[C::WTM][2], y[C::WTN][2]; };
   constexpr int READS = 2 * (C::WTM + C::WTN);
-  uint32_t at_x[2], at_y[2];                                 // where row 0 of the lane's rows lies in a stage
+  uint32_t at_x[4], at_y[4];                                 // where row 0 of the lane's rows lies in a stage, by step and half
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {                              // (rows 32 apart are swizzled alike)
-    at_x[h] = (wm0 + l32) * BK + (((half * 2 + h) ^ swizzle(wm0 + l32)) << 4);
-    at_y[h] = C::A_B + (wn0 + l32) * BK + (((half * 2 + h) ^ swizzle(wn0 + l32)) << 4);
+  for (int u = 0; u < 4; ++u) {                              // (rows 32 apart are swizzled alike)
+    const int q = (u >> 1) * 4 + half * 2 + (u & 1);
+    at_x[u] = (wm0 + l32) * BK + ((q ^ swizzle(wm0 + l32)) << 4);
+    at_y[u] = C::A_B + (wn0 + l32) * BK + ((q ^ swizzle(wn0 + l32)) << 4);
   }
-  auto read_one = [&](Frags& f, int st, int r) {
-    const char* stage = smem + st * C::STAGE_B;
+  auto read_one = [&](Frags& f, int b, int sub, int r) {     // step `sub` of block b
+    const char* stage = smem + (b & (C::STAGES - 1)) * C::STAGE_B;
     const int h = r & 1, i = r >> 1;
-    if (i < C::WTM) f.x[i][h] = *reinterpret_cast<const uint4*>(stage + at_x[h] + i * 32 * BK);
-    else f.y[i - C::WTM][h] = *reinterpret_cast<const uint4*>(stage + at_y[h] + (i - C::WTM) * 32 * BK);
+    if (i < C::WTM) f.x[i][h] = *reinterpret_cast<const uint4*>(stage + at_x[sub * 2 + h] + i * 32 * BK);
+    else f.y[i - C::WTM][h] = *reinterpret_cast<const uint4*>(stage + at_y[sub * 2 + h] + (i - C::WTM) * 32 * BK);
   };
   int sx[C::WTM], sy[C::WTN], nx[C::WTM], ny[C::WTN];        // scale bytes: of the present block of 128, of the next
   auto read_scales = [&](int blk) {
@@ -220,35 +222,38 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
 
   issue_scales(0);
 #pragma unroll
-  for (int t = 0; t < STAGES; ++t)
-    if (t < steps) {
-      const uint8_t* from = uniform(base + (int64_t)t * BK);
+  for (int b = 0; b < C::STAGES; ++b)
+    if (b < blocks) {
+      const uint8_t* from = uniform(base + (int64_t)b * BK);
 #pragma unroll
-      for (int c = 0; c < C::CPW; ++c) issue(from, t, c);
+      for (int c = 0; c < C::CPW; ++c) issue(from, b, c);
     }
-  if (steps >= STAGES) wait_vm<C::CPW * (STAGES - 1)>();
+  if (blocks >= C::STAGES) wait_vm<C::CPW * (C::STAGES - 1)>();
   else wait_vm<0>();
   __syncthreads();
   Frags f0, f1;
   read_scales(0);
   take_scales();
 #pragma unroll
-  for (int r = 0; r < READS; ++r) read_one(f0, 0, r);
+  for (int r = 0; r < READS; ++r) read_one(f0, 0, 0, r);
 
-  // Step t: its operands are in registers.  After the barrier every wave has read stage t, which is then loaded anew, and
-  // step t + 1 has arrived.  The counts leave the loads of the two steps behind it in flight; loads of scale words, which are
-  // not counted, only make a wait longer.  Loads and reads are dealt out among the products and kept there: the four waves
-  // come from the barrier together, and a load put in front of the products would hold them all up.
-  auto step = [&](Frags& now, Frags& next, int t, auto more, auto odd) {
-    constexpr bool MORE = decltype(more)::value, ODD = decltype(odd)::value;      // MORE: step t + STAGES exists
-    if constexpr (MORE) wait_vm<C::CPW * (STAGES - 2)>();
-    else wait_vm<0>();
-    __syncthreads();
-    if constexpr (MORE && !ODD) {
-      if (((t + STAGES) & (GROUP - 1)) == 0) issue_scales((t + STAGES) / GROUP);
+  // Step SUB of block b: its operands are in registers.  The second step opens with a barrier: every wave has then read all
+  // of block b, whose stage is loaded anew, and block b + 1 has arrived (the counts leave the blocks behind it in flight;
+  // loads of scale words, which are not counted, only make a wait longer).  Loads and reads are dealt out among the products
+  // and kept there: the waves come from the barrier together, and a load put in front of the products would hold them all up.
+  auto step = [&](Frags& now, Frags& next, int b, auto more, auto sub) {
+    constexpr bool MORE = decltype(more)::value;             // block b + STAGES exists
+    constexpr int SUB = decltype(sub)::value;
+    if constexpr (SUB == 1) {
+      if constexpr (MORE) wait_vm<C::CPW * (C::STAGES - 2)>();
+      else wait_vm<0>();
+      __syncthreads();
+      if constexpr (MORE) {
+        if (((b + C::STAGES) & (GROUP - 1)) == 0) issue_scales((b + C::STAGES) / GROUP);
+      }
     }
-    const bool reads = MORE || !ODD || t + 1 < steps;        // (the number of steps is even)
-    const uint8_t* from = uniform(base + (int64_t)(t + STAGES) * BK);
+    const bool reads = SUB == 0 || MORE || b + 1 < blocks;
+    const uint8_t* from = uniform(base + (int64_t)(b + C::STAGES) * BK);
     constexpr int Q = EXACT ? 4 : 1, PRODUCTS = C::WTM * C::WTN * Q, OPERANDS = C::WTM + C::WTN;
     Wide wide[2];
     if constexpr (EXACT) {
@@ -265,25 +270,27 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
       } else {
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(now.y[j]), whole(now.x[i]), acc[i][j], 0, 0, 0, sy[j], 0, sx[i]);
       }
-      if constexpr (MORE) each<p * C::CPW / PRODUCTS, (p + 1) * C::CPW / PRODUCTS>([&](auto c) { issue(from, t & (STAGES - 1), c); });
+      if constexpr (MORE && SUB == 1) each<p * C::CPW / PRODUCTS, (p + 1) * C::CPW / PRODUCTS>([&](auto c) { issue(from, b, c); });
       if (reads) {
-        each<p * READS / PRODUCTS, (p + 1) * READS / PRODUCTS>([&](auto r) { read_one(next, (t + 1) & (STAGES - 1), r); });
-        if constexpr (ODD && p == PRODUCTS / 2) read_scales((t + 1) / 2);
+        each<p * READS / PRODUCTS, (p + 1) * READS / PRODUCTS>([&](auto r) { read_one(next, b + SUB, 1 - SUB, r); });
+        if constexpr (SUB == 1 && p == PRODUCTS / 2) read_scales(b + 1);
       }
       __builtin_amdgcn_sched_barrier(0);
     });
-    if constexpr (ODD) take_scales();
+    if constexpr (SUB == 1) take_scales();
   };
   using yes = std::true_type;
   using no = std::false_type;
-  int t = 0;
-  for (; t + STAGES < steps; t += 2) {
-    step(f0, f1, t, yes{}, no{});
-    step(f1, f0, t + 1, yes{}, yes{});
+  using first_step = std::integral_constant<int, 0>;
+  using second_step = std::integral_constant<int, 1>;
+  int b = 0;
+  for (; b + C::STAGES < blocks; ++b) {
+    step(f0, f1, b, yes{}, first_step{});
+    step(f1, f0, b, yes{}, second_step{});
   }
-  for (; t < steps; t += 2) {
-    step(f0, f1, t, no{}, no{});
-    step(f1, f0, t + 1, no{}, yes{});
+  for (; b < blocks; ++b) {
+    step(f0, f1, b, no{}, first_step{});
+    step(f1, f0, b, no{}, second_step{});
   }
 
   __syncthreads();                                           // the stages are free: each wave stages its rows in its share
@@ -358,9 +365,9 @@ __global__ __launch_bounds__(256) void bias_rows_kernel(Fp8Args a) {
   }
 }
 
-using Large = Config<4, 4, 2, 2, 1>;                         // 256 x 256, a wave 128 x 128
-using Middle = Config<2, 2, 2, 2, 2>;                        // 128 x 128
-using Small = Config<1, 1, 2, 2, 2>;                         // 64 x 64
+using Large = Config<4, 4, 2, 2, 1, 2>;                      // 256 x 256, a wave 128 x 128
+using Middle = Config<2, 2, 2, 2, 2, 2>;                     // 128 x 128
+using Small = Config<1, 1, 2, 2, 2, 4>;                      // 64 x 64
 
 template <class C, bool EXACT>
 hipError_t launch_one(const Fp8Args& a, hipStream_t s) {

@@ -228,7 +228,7 @@ struct Fp8Args {
   void* c; int64_t ldc, c_stride;
   int k, dtype;
   int64_t m, n, kp, ks;                                    // kp: padded contraction; ks: scale bytes of a row
-  float* part; int slice_steps;                            // slices of the contraction: [slices][k][m][n], steps of 64 each
+  float* part; int slice_blocks;                           // slices of the contraction: [slices][k][m][n], blocks of 128 each
 };
 hipError_t launch_fp8_matmul(const Fp8Args& a, hipStream_t s);
 
