@@ -23,44 +23,83 @@ inline int64_t blocks_per_worker(int k, int64_t rows, int groups, int64_t target
   return most < share ? most : share;
 }
 
-template <class E, int TPR, int ITEMS, int BLOCK>
+// A row of n is its whole pieces of 16 bytes, piece i * TPR + t to thread t, and fewer than V elements more, one each to the
+// first threads: every access is in bounds and no piece needs a mask of its own.
+template <class E, int TPR>
+struct Split {
+  int whole, tail;                                         // whole pieces; this thread's element behind them
+  bool has_tail;
+  __device__ __forceinline__ Split(int64_t n, int t) : whole((int)(n / E::V)), tail(whole * E::V + t), has_tail(tail < (int)n) {}
+};
+
+// ITEMS pieces of a row and its odd element, as they are in memory; what a thread has not reads as zero
+template <class E, int TPR, int ITEMS>
+struct RowRegs {
+  uint32_t piece[ITEMS][4];
+  float odd;
+  __device__ __forceinline__ void load(const typename E::T* row, const Split<E, TPR>& s, int t) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      if (i * TPR + t < s.whole) load_piece<E>(row + (i * TPR + t) * E::V, piece[i]);
+      else
+#pragma unroll
+        for (int j = 0; j < 4; ++j) piece[i][j] = 0u;
+    }
+    odd = s.has_tail ? E::one(row + s.tail) : 0.f;
+  }
+};
+
+// FEW: gamma and beta of the thread's columns stay in registers over its rows
+template <class E, int TPR, int ITEMS, int BLOCK, bool FEW>
 __global__ __launch_bounds__(BLOCK) void layer_norm_kernel(NormArgs a) {
   constexpr int V = E::V, GROUPS = BLOCK / TPR;
   __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)];
   int turn = 0;
   const int w = blockIdx.y, t = threadIdx.x % TPR, g = threadIdx.x / TPR;
-  const int64_t n = a.n;
+  const Split<E, TPR> split(a.n, t);
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
   typename E::T* y = reinterpret_cast<typename E::T*>(a.out.p) + w * a.out.stride;
   const float* gamma = a.gamma ? a.gamma + w * a.param_stride : nullptr;
   const float* beta = a.beta ? a.beta + w * a.param_stride : nullptr;
-  const float inv_n = 1.f / (float)n;
+  const float inv_n = 1.f / (float)a.n;
   const int64_t step = (int64_t)gridDim.x * GROUPS;
   // every group of a block goes round the same number of times (the block's barriers are for TPR > 64, where it is one)
-  for (int64_t r = (int64_t)blockIdx.x * GROUPS + g; r < a.rows; r += step) {
-    const typename E::T* xr = x + r * a.x.ld;
+  int64_t r = (int64_t)blockIdx.x * GROUPS + g;
+  RowRegs<E, TPR, ITEMS> next;
+  if (r < a.rows) next.load(x + r * a.x.ld, split, t);     // the first row travels along with gamma and beta
+  float ga[ITEMS][V], be[ITEMS][V], ga_odd = 1.f, be_odd = 0.f;
+  auto param = [&](const float* p, float fill, int i, float (&f)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = fill;
+    if (p && i * TPR + t < split.whole) load_floats<V>(p, (int64_t)(i * TPR + t) * V, a.n, fill, f);
+  };
+  if constexpr (FEW) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) { param(gamma, 1.f, i, ga[i]); param(beta, 0.f, i, be[i]); }
+  }
+  if (split.has_tail) {
+    if (gamma) ga_odd = gamma[split.tail];
+    if (beta) be_odd = beta[split.tail];
+  }
+  for (; r < a.rows; r += step) {
     float v[ITEMS][V];
-    float sum = 0.f;
+    float sum = next.odd;
+    const float odd = next.odd;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      uint32_t raw[4];
-      load16<E>(xr, (int64_t)(i * TPR + t) * V, n, raw);
-      E::unpack(raw, v[i]);
+      E::unpack(next.piece[i], v[i]);
 #pragma unroll
       for (int j = 0; j < V; ++j) sum += v[i][j];
     }
+    if (r + step < a.rows) next.load(x + (r + step) * a.x.ld, split, t);
     const float mean = row_sum<TPR>(sum, red, turn) * inv_n;
-    float sq = 0.f;
+    const float odd_off = odd - mean;
+    float sq = split.has_tail ? odd_off * odd_off : 0.f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int64_t e0 = (int64_t)(i * TPR + t) * V;
-      if (e0 + V <= n) {
+      if (i * TPR + t < split.whole) {
 #pragma unroll
         for (int j = 0; j < V; ++j) { v[i][j] -= mean; sq += v[i][j] * v[i][j]; }
-      } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (e0 + j < n) { v[i][j] -= mean; sq += v[i][j] * v[i][j]; }
       }
     }
     const float var = row_sum<TPR>(sq, red, turn) * inv_n;
@@ -72,18 +111,14 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_kernel(NormArgs a) {
     typename E::T* yr = y + r * a.out.ld;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int64_t e0 = (int64_t)(i * TPR + t) * V;
-      if (e0 < n) {
-        float ga[V], be[V], o[V];
+      if (i * TPR + t < split.whole) {
+        if constexpr (!FEW) { param(gamma, 1.f, i, ga[i]); param(beta, 0.f, i, be[i]); }
 #pragma unroll
-        for (int j = 0; j < V; ++j) { ga[j] = 1.f; be[j] = 0.f; }
-        if (gamma) load_floats<V>(gamma, e0, n, 1.f, ga);
-        if (beta) load_floats<V>(beta, e0, n, 0.f, be);
-#pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = v[i][j] * rstd * ga[j] + be[j];
-        store16<E>(yr, e0, n, o);
+        for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * rstd * ga[i][j] + be[i][j];
+        store_piece<E>(yr + (i * TPR + t) * V, v[i]);
       }
     }
+    if (split.has_tail) E::put(yr + split.tail, odd_off * rstd * ga_odd + be_odd);
   }
 }
 
@@ -138,64 +173,95 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(NormArgs a) {
   }
 }
 
+// Registers hold x, dy and the column sums of a thread's pieces, gamma, and the next row on its way; 1024 threads have half
+// as many each, so there gamma comes from the caches and the next row is not fetched ahead.
 template <class E, int TPR, int ITEMS, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void layer_norm_grad_kernel(NormArgs a) {
   constexpr int V = E::V, GROUPS = BLOCK / TPR;
+  constexpr bool AHEAD = TPR < 1024;
   constexpr int COLS = TPR * ITEMS * V;
-  __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)];
-  __shared__ float cols[GROUPS > 1 ? GROUPS * COLS : 1];
+  __shared__ float red[4 * (TPR > 64 ? TPR / 64 : 1)];
+  __shared__ float cols[GROUPS > 1 ? GROUPS * (COLS + V) : 1];
   int turn = 0;
   const int w = blockIdx.y, t = threadIdx.x % TPR, g = threadIdx.x / TPR;
   const int64_t n = a.n;
+  const Split<E, TPR> split(n, t);
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
   const typename E::T* dy = reinterpret_cast<const typename E::T*>(a.dy.p) + w * a.dy.stride;
   typename E::T* dx = a.out.p ? reinterpret_cast<typename E::T*>(a.out.p) + w * a.out.stride : nullptr;
   const float* gamma = a.gamma ? a.gamma + w * a.param_stride : nullptr;
   const float inv_n = 1.f / (float)n;
-  float dg[ITEMS][V], db[ITEMS][V], ga[ITEMS][V];
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  int64_t r = (int64_t)blockIdx.x * GROUPS + g;
+  RowRegs<E, TPR, ITEMS> next_x, next_dy;
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto fetch = [&](int64_t row) {
+    next_x.load(x + row * a.x.ld, split, t);
+    next_dy.load(dy + row * a.dy.ld, split, t);
+    next_mean = a.mean[w * a.rows + row];
+    next_rstd = a.rstd[w * a.rows + row];
+  };
+  if (AHEAD && r < a.rows) fetch(r);
+  float dg[ITEMS][V], db[ITEMS][V], ga[ITEMS][V], dg_odd = 0.f, db_odd = 0.f, ga_odd = 1.f;
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
 #pragma unroll
     for (int j = 0; j < V; ++j) { dg[i][j] = 0.f; db[i][j] = 0.f; ga[i][j] = 1.f; }
-    if (gamma) load_floats<V>(gamma, (int64_t)(i * TPR + t) * V, n, 0.f, ga[i]);
+    if (AHEAD && gamma && i * TPR + t < split.whole) load_floats<V>(gamma, (int64_t)(i * TPR + t) * V, n, 1.f, ga[i]);
   }
-  const int64_t step = (int64_t)gridDim.x * GROUPS;
-  for (int64_t r = (int64_t)blockIdx.x * GROUPS + g; r < a.rows; r += step) {
-    const float mean = a.mean[w * a.rows + r], rstd = a.rstd[w * a.rows + r];
+  if (gamma && split.has_tail) ga_odd = gamma[split.tail];
+  for (; r < a.rows; r += step) {
+    if constexpr (!AHEAD) fetch(r);
+    const float mean = next_mean, rstd = next_rstd;
     float h[ITEMS][V], v[ITEMS][V];
-    float s1 = 0.f, s2 = 0.f;
+    float s1 = 0.f, s2 = 0.f, h_odd = 0.f, v_odd = 0.f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      uint32_t raw[4];
-      const int64_t e0 = (int64_t)(i * TPR + t) * V;
-      load16<E>(x + r * a.x.ld, e0, n, raw);
-      E::unpack(raw, h[i]);
-      load16<E>(dy + r * a.dy.ld, e0, n, raw);
-      E::unpack(raw, v[i]);
-      if (e0 < n) {
+      E::unpack(next_x.piece[i], h[i]);
+      E::unpack(next_dy.piece[i], v[i]);
+      if (i * TPR + t < split.whole) {
+        float here[V];
+        if (!AHEAD) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) here[j] = 1.f;
+          if (gamma) load_floats<V>(gamma, (int64_t)(i * TPR + t) * V, n, 1.f, here);
+        }
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           h[i][j] = (h[i][j] - mean) * rstd;
           dg[i][j] += v[i][j] * h[i][j];
           db[i][j] += v[i][j];
-          v[i][j] *= ga[i][j];                             // past the end: dy reads as zero
+          v[i][j] *= AHEAD ? ga[i][j] : here[j];
           s1 += v[i][j];
           s2 += v[i][j] * h[i][j];
         }
       }
     }
+    if (split.has_tail) {
+      h_odd = (next_x.odd - mean) * rstd;
+      dg_odd += next_dy.odd * h_odd;
+      db_odd += next_dy.odd;
+      v_odd = next_dy.odd * ga_odd;
+      s1 += v_odd;
+      s2 += v_odd * h_odd;
+    }
+    if (AHEAD && r + step < a.rows) fetch(r + step);
     if (dx) {
-      const float c1 = row_sum<TPR>(s1, red, turn) * inv_n, c2 = row_sum<TPR>(s2, red, turn) * inv_n;
+      float c1, c2;
+      row_sum2<TPR>(s1, s2, red, turn, c1, c2);
+      c1 *= inv_n;
+      c2 *= inv_n;
+      typename E::T* out = dx + r * a.out.ld;
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
-        const int64_t e0 = (int64_t)(i * TPR + t) * V;
-        if (e0 < n) {
+        if (i * TPR + t < split.whole) {
           float o[V];
 #pragma unroll
           for (int j = 0; j < V; ++j) o[j] = rstd * (v[i][j] - c1 - h[i][j] * c2);
-          store16<E>(dx + r * a.out.ld, e0, n, o);
+          store_piece<E>(out + (i * TPR + t) * V, o);
         }
       }
+      if (split.has_tail) E::put(out + split.tail, rstd * (v_odd - c1 - h_odd * c2));
     }
   }
   if (!a.part) return;
@@ -203,24 +269,32 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_grad_kernel(NormArgs a) {
   float* out = a.part + ((int64_t)w * gridDim.x + blockIdx.x) * 2 * n;
   if constexpr (GROUPS == 1) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int64_t e0 = (int64_t)(i * TPR + t) * V;
+    for (int i = 0; i < ITEMS; ++i)
+      if (i * TPR + t < split.whole) {
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (e0 + j < n) { out[e0 + j] = dg[i][j]; out[n + e0 + j] = db[i][j]; }
-    }
+        for (int q = 0; q < V / 4; ++q) {
+          const int64_t e = (int64_t)(i * TPR + t) * V + 4 * q;
+          const float fg[4] = {dg[i][4 * q], dg[i][4 * q + 1], dg[i][4 * q + 2], dg[i][4 * q + 3]};
+          const float fb[4] = {db[i][4 * q], db[i][4 * q + 1], db[i][4 * q + 2], db[i][4 * q + 3]};
+          store_piece<F32>(out + e, fg);
+          store_piece<F32>(out + n + e, fb);
+        }
+      }
+    if (split.has_tail) { out[split.tail] = dg_odd; out[n + split.tail] = db_odd; }
   } else {
     for (int part = 0; part < 2; ++part) {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j) cols[g * COLS + (i * TPR + t) * V + j] = part ? db[i][j] : dg[i][j];
+        for (int j = 0; j < V; ++j) cols[g * (COLS + V) + (i * TPR + t) * V + j] = part ? db[i][j] : dg[i][j];
+      __syncthreads();                                     // (the odd elements' places may be those of a piece that is not there)
+      if (split.has_tail) cols[g * (COLS + V) + split.tail] = part ? db_odd : dg_odd;
       __syncthreads();
       for (int e = threadIdx.x; e < n; e += BLOCK) {
         float s = cols[e];
 #pragma unroll
-        for (int q = 1; q < GROUPS; ++q) s += cols[q * COLS + e];
+        for (int q = 1; q < GROUPS; ++q) s += cols[q * (COLS + V) + e];
         out[part * n + e] = s;
       }
     }
@@ -318,49 +392,68 @@ __global__ __launch_bounds__(1024) void layer_norm_strips_kernel(NormArgs a) {
   }
 }
 
-// threads that share a row and 16-byte pieces a thread holds: the fewest threads whose registers take the row
-struct NormShape { int tpr, items; };
-NormShape norm_shape(int64_t n, int V) {
-  const int64_t pieces = ceil_div(n, V);
-  if (pieces <= 16) return {16, 1};
-  if (pieces <= 64) return {64, 1};
-  if (pieces <= 128) return {64, 2};
-  if (pieces <= 256) return {256, 1};
-  if (pieces <= 512) return {256, 2};
-  if (pieces <= 1024) return {256, 4};
-  if (pieces <= 2048) return {1024, 2};
-  return {0, 0};
+// f.template operator()<TPR, ITEMS>() for a row of `pieces` whole pieces: the fewest threads whose registers take the row
+// in up to two pieces each, then up to four of 512 and (WIDE) of 1024; false: too long
+template <bool WIDE, class F>
+bool for_row(int64_t pieces, F f) {
+  if (pieces <= 16) f.template operator()<16, 1>();
+  else if (pieces <= 64) f.template operator()<64, 1>();
+  else if (pieces <= 128) f.template operator()<64, 2>();
+  else if (pieces <= 256) f.template operator()<256, 1>();
+  else if (pieces <= 512) f.template operator()<256, 2>();
+  else if (pieces <= 1024) f.template operator()<512, 2>();
+  else if (pieces <= 1536) f.template operator()<512, 3>();
+  else if (pieces <= 2048) f.template operator()<512, 4>();
+  else if constexpr (WIDE) {
+    if (pieces > 4096) return false;
+    f.template operator()<1024, 4>();
+  } else return false;
+  return true;
 }
+// the backward pass of bf16 has no registers for eight times as many columns in each of four arrays
+template <class E> constexpr bool kWideGrad = E::V == 4;
+constexpr int block_of(int tpr) { return tpr < 256 ? 256 : tpr; }
 
-template <class E, int TPR, int ITEMS, int BLOCK>
-hipError_t fwd(const NormArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)blocks_per_worker(a.k, a.rows, BLOCK / TPR, 8 * kCus), (unsigned)a.k);
-  hipLaunchKernelGGL((layer_norm_kernel<E, TPR, ITEMS, BLOCK>), grid, dim3(BLOCK), 0, s, a);
-  return hipGetLastError();
-}
+template <class E>
+struct Forward {
+  const NormArgs& a;
+  hipStream_t s;
+  template <int TPR, int ITEMS>
+  void operator()() const {
+    constexpr int BLOCK = block_of(TPR);
+    constexpr bool FEW = ITEMS * E::V <= 16 && TPR < 1024;
+    const dim3 grid((unsigned)blocks_per_worker(a.k, a.rows, BLOCK / TPR, 2048 * (int64_t)kCus / BLOCK), (unsigned)a.k);
+    hipLaunchKernelGGL((layer_norm_kernel<E, TPR, ITEMS, BLOCK, FEW>), grid, dim3(BLOCK), 0, s, a);
+  }
+};
 template <class E>
 hipError_t fwd_any(const NormArgs& a, hipStream_t s) {
-  const NormShape c = norm_shape(a.n, E::V);
-  if (c.tpr == 16) return fwd<E, 16, 1, 256>(a, s);
-  if (c.tpr == 64) return c.items == 1 ? fwd<E, 64, 1, 256>(a, s) : fwd<E, 64, 2, 256>(a, s);
-  if (c.tpr == 256) return c.items == 1 ? fwd<E, 256, 1, 256>(a, s) : c.items == 2 ? fwd<E, 256, 2, 256>(a, s) : fwd<E, 256, 4, 256>(a, s);
-  if (c.tpr == 1024) return fwd<E, 1024, 2, 1024>(a, s);
-  hipLaunchKernelGGL(layer_norm_long_kernel<E>, dim3((unsigned)blocks_per_worker(a.k, a.rows, 1, 4 * kCus), (unsigned)a.k), dim3(1024), 0, s, a);
+  if (!for_row<true>(a.n / E::V, Forward<E>{a, s}))
+    hipLaunchKernelGGL(layer_norm_long_kernel<E>, dim3((unsigned)blocks_per_worker(a.k, a.rows, 1, 4 * kCus), (unsigned)a.k), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
-template <class E, int TPR, int ITEMS, int BLOCK>
-hipError_t bwd(const NormArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((layer_norm_grad_kernel<E, TPR, ITEMS, BLOCK>), dim3((unsigned)a.strips, (unsigned)a.k), dim3(BLOCK), 0, s, a);
-  return hipGetLastError();
-}
+// blocks of the backward pass: as many as run at a time, so that there are few rows of partial sums
+int64_t grad_blocks(int tpr) { return (tpr >= 1024 ? 1 : tpr == 512 ? 2 : 4) * (int64_t)kCus; }
+
+template <class E>
+struct Backward {
+  const NormArgs& a;
+  hipStream_t s;
+  template <int TPR, int ITEMS>
+  void operator()() const {
+    constexpr int BLOCK = block_of(TPR);
+    hipLaunchKernelGGL((layer_norm_grad_kernel<E, TPR, ITEMS, BLOCK>), dim3((unsigned)a.strips, (unsigned)a.k), dim3(BLOCK), 0, s, a);
+  }
+};
+struct Strips {
+  int k; int64_t rows; int* strips;
+  template <int TPR, int ITEMS>
+  void operator()() const { *strips = (int)blocks_per_worker(k, rows, block_of(TPR) / TPR, grad_blocks(TPR)); }
+};
 template <class E>
 hipError_t bwd_any(const NormArgs& a, hipStream_t s) {
-  const NormShape c = norm_shape(a.n, E::V);
-  if (c.tpr == 16) return bwd<E, 16, 1, 256>(a, s);
-  if (c.tpr == 64) return c.items == 1 ? bwd<E, 64, 1, 256>(a, s) : bwd<E, 64, 2, 256>(a, s);
-  if (c.tpr == 256) return c.items == 1 ? bwd<E, 256, 1, 256>(a, s) : c.items == 2 ? bwd<E, 256, 2, 256>(a, s) : bwd<E, 256, 4, 256>(a, s);
-  if (c.tpr == 1024) return bwd<E, 1024, 2, 1024>(a, s);
+  if (for_row<kWideGrad<E>>(a.n / E::V, Backward<E>{a, s})) return hipGetLastError();
   if (a.out.p) {
     hipLaunchKernelGGL(layer_norm_grad_long_kernel<E>, dim3((unsigned)blocks_per_worker(a.k, a.rows, 1, 4 * kCus), (unsigned)a.k), dim3(1024), 0, s, a);
     const hipError_t e = hipGetLastError();
@@ -374,9 +467,10 @@ hipError_t bwd_any(const NormArgs& a, hipStream_t s) {
 }  // namespace
 
 int layer_norm_grad_strips(int k, int64_t rows, int64_t n, int dtype) {
-  const NormShape c = norm_shape(n, dtype == DW_BF16 ? Bf16::V : F32::V);
-  const int groups = c.tpr >= 256 || c.tpr == 0 ? 1 : 256 / c.tpr;
-  return (int)blocks_per_worker(k, rows, groups, c.tpr == 1024 ? kCus : 2 * kCus);
+  int strips = 0;
+  const Strips count{k, rows, &strips};
+  const bool fits = dtype == DW_BF16 ? for_row<kWideGrad<Bf16>>(n / Bf16::V, count) : for_row<kWideGrad<F32>>(n / F32::V, count);
+  return fits ? strips : (int)blocks_per_worker(k, rows, 1, 2 * kCus);
 }
 
 hipError_t launch_layer_norm(const NormArgs& a, int dtype, hipStream_t s) {

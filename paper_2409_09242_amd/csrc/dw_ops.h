@@ -74,6 +74,23 @@ __device__ __forceinline__ void store_piece(typename E::T* p, const float (&f)[E
   E::pack(f, v.w);
   *reinterpret_cast<typename E::Raw*>(p) = v;
 }
+// the same for data that streams through once and must not displace what is read again
+typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+template <class E> struct Streamed { typedef u32x4_a4 T; };
+template <> struct Streamed<Bf16> { typedef u32x4_a2 T; };
+template <class E>
+__device__ __forceinline__ void load_piece_once(const typename E::T* p, uint32_t (&r)[4]) {
+  const auto v = __builtin_nontemporal_load(reinterpret_cast<const typename Streamed<E>::T*>(p));
+  r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
+}
+template <class E>
+__device__ __forceinline__ void store_piece_once(typename E::T* p, const float (&f)[E::V]) {
+  uint32_t r[4];
+  E::pack(f, r);
+  typename Streamed<E>::T v = {r[0], r[1], r[2], r[3]};
+  __builtin_nontemporal_store(v, reinterpret_cast<typename Streamed<E>::T*>(p));
+}
 // the 16 bytes of elements e0 .. e0+V-1 of a row of n; elements at n and beyond read as zero
 template <class E>
 __device__ __forceinline__ void load16(const typename E::T* row, int64_t e0, int64_t n, uint32_t (&r)[4]) {
@@ -133,6 +150,26 @@ __device__ __forceinline__ float row_sum(float x, float* lds, int& turn) {
     for (int w = 1; w < W; ++w) x += at[w];
   }
   return x;
+}
+
+// two such sums with one barrier (`lds`: 4 * TPR/64 floats)
+template <int TPR>
+__device__ __forceinline__ void row_sum2(float x, float y, float* lds, int& turn, float& sx, float& sy) {
+#pragma unroll
+  for (int off = 1; off < (TPR < 64 ? TPR : 64); off <<= 1) { x += __shfl_xor(x, off); y += __shfl_xor(y, off); }
+  if constexpr (TPR > 64) {
+    constexpr int W = TPR / 64;
+    float* at = lds + turn * 2 * W;
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) { at[threadIdx.x >> 6] = x; at[W + (threadIdx.x >> 6)] = y; }
+    __syncthreads();
+    x = at[0];
+    y = at[W];
+#pragma unroll
+    for (int w = 1; w < W; ++w) { x += at[w]; y += at[W + w]; }
+  }
+  sx = x;
+  sy = y;
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
