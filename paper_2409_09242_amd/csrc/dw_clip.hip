@@ -45,18 +45,31 @@ __device__ __forceinline__ double block_sum(double s, double* lds) {
   return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
+constexpr int kAhead = 4;                                   // pieces of a thread in flight
+
 template <class E>
 __device__ __forceinline__ double squares(const void* base, const Chunk& c) {
   const typename E::T* p = reinterpret_cast<const typename E::T*>(base) + c.e0;
   const int n = (int)(c.e1 - c.e0), whole = n / E::V;
   double s = 0.0;
-  for (int q = threadIdx.x; q < whole; q += kThreads) {
-    uint32_t raw[4];
+  auto add = [&](const uint32_t (&raw)[4]) {
     float f[E::V];
-    load_piece<E>(p + q * E::V, raw);
     E::unpack(raw, f);
 #pragma unroll
     for (int j = 0; j < E::V; ++j) s = __builtin_fma((double)f[j], (double)f[j], s);
+  };
+  int q = threadIdx.x;
+  for (; q + (kAhead - 1) * kThreads < whole; q += kAhead * kThreads) {
+    uint32_t raw[kAhead][4];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load_piece<E>(p + (q + i * kThreads) * E::V, raw[i]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) add(raw[i]);
+  }
+  for (; q < whole; q += kThreads) {
+    uint32_t raw[4];
+    load_piece<E>(p + q * E::V, raw);
+    add(raw);
   }
   const int e = whole * E::V + threadIdx.x;
   if (e < n) { const double f = (double)E::one(p + e); s = __builtin_fma(f, f, s); }
@@ -84,49 +97,97 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* part,
   if (threadIdx.x == 0) norm[blockIdx.x] = (float)v;
 }
 
-template <class E, bool PACK>
-__device__ __forceinline__ void scale_chunk(void* base, float* out, const Chunk& c, float factor) {
+// four elements at a time into fp32, so that a wave's stores follow each other without gaps
+template <class E>
+__device__ __forceinline__ void pack_chunk(const void* base, float* out, const Chunk& c, float factor) {
+  typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+  const typename E::T* p = reinterpret_cast<const typename E::T*>(base) + c.e0;
+  const int n = (int)(c.e1 - c.e0), whole = n / 4;
+  struct Four { uint32_t w[E::V == 8 ? 2 : 4]; };
+  auto get = [&](int q) {
+    Four r;
+    if constexpr (E::V == 8) {
+      const u32x2_a2 v = *reinterpret_cast<const u32x2_a2*>(p + q * 4);
+      r.w[0] = v.x; r.w[1] = v.y;
+    } else {
+      load_piece<E>(p + q * 4, r.w);
+    }
+    return r;
+  };
+  auto put = [&](const Four& r, int q) {
+    float f[4];
+    if constexpr (E::V == 8) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(j & 1 ? r.w[j >> 1] & 0xFFFF0000u : r.w[j >> 1] << 16) * factor;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(r.w[j]) * factor;
+    }
+    store_piece_once<F32>(out + q * 4, f);
+  };
+  int q = threadIdx.x;
+  for (; q + (kAhead - 1) * kThreads < whole; q += kAhead * kThreads) {
+    Four r[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) r[i] = get(q + i * kThreads);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) put(r[i], q + i * kThreads);
+  }
+  for (; q < whole; q += kThreads) put(get(q), q);
+  const int e = whole * 4 + threadIdx.x;
+  if (e < n) out[e] = E::one(p + e) * factor;
+}
+
+template <class E>
+__device__ __forceinline__ void scale_chunk(void* base, const Chunk& c, float factor) {
   typename E::T* p = reinterpret_cast<typename E::T*>(base) + c.e0;
   const int n = (int)(c.e1 - c.e0), whole = n / E::V;
-  for (int q = threadIdx.x; q < whole; q += kThreads) {
-    uint32_t raw[4];
+  auto put = [&](const uint32_t (&raw)[4], int q) {
     float f[E::V];
-    load_piece<E>(p + q * E::V, raw);
     E::unpack(raw, f);
 #pragma unroll
     for (int j = 0; j < E::V; ++j) f[j] *= factor;
-    if constexpr (PACK) {
+    store_piece<E>(p + q * E::V, f);
+  };
+  int q = threadIdx.x;
+  for (; q + (kAhead - 1) * kThreads < whole; q += kAhead * kThreads) {
+    uint32_t raw[kAhead][4];
 #pragma unroll
-      for (int h = 0; h < E::V / 4; ++h) {
-        const float g[4] = {f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]};
-        store_piece<F32>(out + q * E::V + 4 * h, g);
-      }
-    } else {
-      store_piece<E>(p + q * E::V, f);
-    }
+    for (int i = 0; i < kAhead; ++i) load_piece<E>(p + (q + i * kThreads) * E::V, raw[i]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) put(raw[i], q + i * kThreads);
+  }
+  for (; q < whole; q += kThreads) {
+    uint32_t raw[4];
+    load_piece<E>(p + q * E::V, raw);
+    put(raw, q);
   }
   const int e = whole * E::V + threadIdx.x;
-  if (e < n) {
-    const float f = E::one(p + e) * factor;
-    if constexpr (PACK) out[e] = f; else E::put(p + e, f);
-  }
+  if (e < n) E::put(p + e, E::one(p + e) * factor);
 }
 
 template <bool PACK>
 __global__ __launch_bounds__(kThreads) void clip_kernel(ClipTable t) {
   __shared__ double lds[4];
-  const int w = t.worker0 + blockIdx.y;
+  // from the last chunk to the first: what the first pass read last is still in the chip's caches
+  const int chunk = gridDim.x - 1 - blockIdx.x, worker = gridDim.y - 1 - blockIdx.y;
+  const int w = t.worker0 + worker;
   const double norm = worker_norm(t.part + (int64_t)w * t.parts, t.parts, lds);
   if (blockIdx.x == 0 && t.part0 == 0 && threadIdx.x == 0) t.norm[w] = (float)norm;
   // a norm that is not finite leaves the gradients as they are: the caller sees it and can leave the step out
   const double c = (double)t.max_norm / (norm + 1e-6);
   const float factor = c < 1.0 && norm <= 1.79769313486231571e308 ? (float)c : 1.f;
   if (!PACK && factor == 1.f) return;
-  const Chunk ch = find_chunk(t, blockIdx.x);
-  void* p = const_cast<void*>(t.address(blockIdx.y, ch.j));
+  const Chunk ch = find_chunk(t, chunk);
+  void* p = const_cast<void*>(t.address(worker, ch.j));
   float* out = PACK ? t.out + (int64_t)w * t.out_stride + t.out0 + t.first_of(ch.j) + ch.e0 : nullptr;
-  if (t.is_bf16(ch.j)) scale_chunk<Bf16, PACK>(p, out, ch, factor);
-  else scale_chunk<F32, PACK>(p, out, ch, factor);
+  if constexpr (PACK) {
+    if (t.is_bf16(ch.j)) pack_chunk<Bf16>(p, out, ch, factor);
+    else pack_chunk<F32>(p, out, ch, factor);
+  } else {
+    if (t.is_bf16(ch.j)) scale_chunk<Bf16>(p, ch, factor);
+    else scale_chunk<F32>(p, ch, factor);
+  }
 }
 
 }  // namespace

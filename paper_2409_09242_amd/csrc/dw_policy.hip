@@ -147,7 +147,7 @@ __global__ __launch_bounds__(BLOCK) void policy_rows_kernel(PolicyArgs a) {
           E::unpack(piece, f);
 #pragma unroll
           for (int j = 0; j < V; ++j) f[j] = scale * exp_fast(f[j] - top);
-          store_piece<E>(out + (int64_t)q * V, f);
+          store_piece_once<E>(out + (int64_t)q * V, f);
         };
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(BLOCK) void policy_rows_kernel(PolicyArgs a) {
         float f[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = 0.f;
-        for (int q = t; q < whole; q += TPR) store_piece<E>(out + (int64_t)q * V, f);
+        for (int q = t; q < whole; q += TPR) store_piece_once<E>(out + (int64_t)q * V, f);
         if (has_tail) E::put(out + tail, 0.f);
       }
     }
@@ -204,6 +204,7 @@ hipError_t rows_any(const PolicyArgs& a, hipStream_t s) {
   if (pieces <= 64) return rows_of<E, 64, 1, 256, false>(a, s);
   if (pieces <= 256) return rows_of<E, 64, 4, 256, false>(a, s);
   if (pieces <= 1024) return rows_of<E, 256, 4, 256, false>(a, s);
+  if (pieces <= 2048) return rows_of<E, 256, 8, 256, false>(a, s);
   if (pieces <= 4096) return rows_of<E, 1024, 4, 1024, false>(a, s);
   if (pieces <= 8192) return rows_of<E, 1024, 8, 1024, false>(a, s);
   if (pieces <= 16384) return rows_of<E, 1024, 16, 1024, false>(a, s);
