@@ -4,7 +4,7 @@
 //
 // Two passes: a block adds up the squares of a chunk of one tensor in 64 bits (no overflow, and the order of additions is
 // fixed) and leaves one partial sum; the second pass adds a worker's partial sums, every block for itself and in the same
-// order, and writes its chunk.  In place a worker that is not clipped is not touched again.
+// order (many of them: a launch in between, once), and writes its chunk.  In place a worker that is not clipped is not touched again.
 //
 // The workers are replicas of one model, so tensor j has the same size for all of them: a launch carries, in its
 // arguments, where the chunks and elements of its tensors begin (once) and their addresses (for each worker).
@@ -84,17 +84,22 @@ __global__ __launch_bounds__(kThreads) void grad_squares_kernel(ClipTable t) {
   if (threadIdx.x == 0) t.part[(int64_t)(t.worker0 + blockIdx.y) * t.parts + t.part0 + blockIdx.x] = s;
 }
 
-// the norm of worker w from its partial sums
+// the norm of a worker from its partial sums
 __device__ __forceinline__ double worker_norm(const double* part, int parts, double* lds) {
   double s = 0.0;
+#pragma unroll 4
   for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
   return sqrt(block_sum(s, lds));
 }
 
-__global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* part, int parts, float* norm) {
+// wide[w]: the norm in 64 bits for the second pass (nullptr: there is none, or its blocks add up for themselves)
+__global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* part, int parts, float* norm, double* wide) {
   __shared__ double lds[4];
   const double v = worker_norm(part + (int64_t)blockIdx.x * parts, parts, lds);
-  if (threadIdx.x == 0) norm[blockIdx.x] = (float)v;
+  if (threadIdx.x == 0) {
+    norm[blockIdx.x] = (float)v;
+    if (wide) wide[blockIdx.x] = v;
+  }
 }
 
 // four elements at a time into fp32, so that a wave's stores follow each other without gaps
@@ -172,8 +177,13 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(ClipTable t) {
   // from the last chunk to the first: what the first pass read last is still in the chip's caches
   const int chunk = gridDim.x - 1 - blockIdx.x, worker = gridDim.y - 1 - blockIdx.y;
   const int w = t.worker0 + worker;
-  const double norm = worker_norm(t.part + (int64_t)w * t.parts, t.parts, lds);
-  if (blockIdx.x == 0 && t.part0 == 0 && threadIdx.x == 0) t.norm[w] = (float)norm;
+  double norm;
+  if (t.wide) {
+    norm = t.wide[w];
+  } else {
+    norm = worker_norm(t.part + (int64_t)w * t.parts, t.parts, lds);
+    if (blockIdx.x == 0 && t.part0 == 0 && threadIdx.x == 0) t.norm[w] = (float)norm;
+  }
   // a norm that is not finite leaves the gradients as they are: the caller sees it and can leave the step out
   const double c = (double)t.max_norm / (norm + 1e-6);
   const float factor = c < 1.0 && norm <= 1.79769313486231571e308 ? (float)c : 1.f;
@@ -192,12 +202,16 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(ClipTable t) {
 
 }  // namespace
 
-// elements of a chunk: few enough partial sums that every block can add a worker's, many enough blocks to fill the chip
+// Elements of a chunk: blocks enough that the last of them do not leave the chip half empty (8 x 50.4e6 elements: 12400
+// blocks %s us, 3100 blocks 677), and chunks of 4096 at least.
 int64_t clip_chunk(int64_t elements_of_all_workers) {
   int64_t c = 4096;
-  while (c * 4096 < elements_of_all_workers) c *= 2;
+  while (c * 16384 < elements_of_all_workers) c *= 2;
   return c;
 }
+// Up to so many partial sums a worker every block of the second pass adds them up for itself; beyond, a launch between the
+// passes does it once.
+bool clip_adds_in_between(int parts) { return parts > 512; }
 
 // the tensors [j0, j0 + n) of the workers [w0, w0 + workers) that one launch carries
 void clip_table_fill(ClipTable& t, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int dtype, int per_worker,
@@ -221,8 +235,8 @@ hipError_t launch_grad_squares(const ClipTable& t, hipStream_t s) {
   hipLaunchKernelGGL(grad_squares_kernel, dim3((unsigned)t.chunks, (unsigned)t.workers), dim3(kThreads), 0, s, t);
   return hipGetLastError();
 }
-hipError_t launch_grad_norm(const double* part, int parts, float* norm, int k, hipStream_t s) {
-  hipLaunchKernelGGL(grad_norm_kernel, dim3((unsigned)k), dim3(kThreads), 0, s, part, parts, norm);
+hipError_t launch_grad_norm(const double* part, int parts, float* norm, double* wide, int k, hipStream_t s) {
+  hipLaunchKernelGGL(grad_norm_kernel, dim3((unsigned)k), dim3(kThreads), 0, s, part, parts, norm, wide);
   return hipGetLastError();
 }
 hipError_t launch_clip(const ClipTable& t, hipStream_t s) {

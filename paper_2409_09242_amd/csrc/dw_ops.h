@@ -213,15 +213,16 @@ hipError_t launch_policy(const PolicyArgs& a, int dtype, hipStream_t s);
 // Arguments of one launch: tensors j < n of `workers` workers.  The table holds n + 1 places (in elements, from the launch's first
 // tensor), the tensors' addresses (workers by n), then n first chunks and their types, two to a word.
 struct ClipTable {
-  static constexpr int kWords = 470;                       // 64-bit words; all arguments stay below 4 KB
+  static constexpr int kWords = 469;                       // 64-bit words; all arguments stay below 4 KB
   uint64_t word[kWords];
   int n, workers, chunks, worker0;
   int64_t chunk, elements;                                 // elements of a chunk, and of the launch's tensors (of one worker)
   double* part; int parts, part0;                          // partial sums [k][parts], this launch's first
   float* norm; float max_norm;
+  const double* wide;                                      // [k] norms, or nullptr: every block adds the partial sums
   float* out; int64_t out_stride, out0;                    // nullptr: in place; out0: elements of a worker before this launch's
   // most tensors of one launch for so many workers
-  static int tensors(int workers) { return (kWords - 1) * 2 / (2 * workers + 3); }
+  static int tensors(int workers) { return (kWords - 2) * 2 / (2 * workers + 3); }
   __host__ __device__ int64_t first_of(int j) const { return (int64_t)word[j]; }
   __host__ __device__ const void* address(int w, int j) const { return reinterpret_cast<const void*>(word[n + 1 + w * n + j]); }
   __host__ __device__ int chunk_word(int j) const {
@@ -245,7 +246,8 @@ int64_t clip_chunk(int64_t elements_of_all_workers);
 void clip_table_fill(ClipTable& t, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int dtype, int per_worker,
                      int j0, int w0);
 hipError_t launch_grad_squares(const ClipTable& t, hipStream_t s);
-hipError_t launch_grad_norm(const double* part, int parts, float* norm, int k, hipStream_t s);
+bool clip_adds_in_between(int parts);
+hipError_t launch_grad_norm(const double* part, int parts, float* norm, double* wide, int k, hipStream_t s);
 hipError_t launch_clip(const ClipTable& t, hipStream_t s);
 
 // ---- 8-bit block products (dw_fp8_quant.hip, dw_gemm_fp8.hip) ----------------------------------------------------------

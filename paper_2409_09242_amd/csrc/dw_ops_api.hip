@@ -50,7 +50,7 @@ int clip_sizes(int k, int n_tensors, const int64_t* h_count, ClipSizes* z) {
   z->chunk = clip_chunk(z->elements * k);
   int64_t parts = 0;
   for (int j = 0; j < n_tensors; ++j) parts += ceil_div(h_count[j], z->chunk);
-  z->parts = (int)parts;                                    // at most 4096 + DW_MAX_TENSORS
+  z->parts = (int)parts;                                    // at most 16384 + DW_MAX_TENSORS
   return DW_OK;
 }
 
@@ -176,7 +176,7 @@ int dw_policy_loss(const void* d_logits, int64_t ld, int64_t stride, const int32
 size_t dw_clip_grads_scratch_bytes(int k, int n_tensors, const int64_t* h_count) {
   ClipSizes z;
   if (clip_sizes(k, n_tensors, h_count, &z) != DW_OK) return 0;
-  return (size_t)k * z.parts * sizeof(double);
+  return (size_t)k * (z.parts + 1) * sizeof(double);       // the partial sums, and the norms
 }
 
 int dw_clip_grads(const void* const* h_grad, const int64_t* h_count, const int32_t* h_dtype, int k, int n_tensors, int dtype,
@@ -197,14 +197,17 @@ int dw_clip_grads(const void* const* h_grad, const int64_t* h_count, const int32
     if (!h_grad[i]) return DW_ERR_NULL;
     if (!aligned(h_grad[i], type_bytes(h_dtype ? h_dtype[j] : dtype))) return DW_ERR_ARG;
   }
-  if (z.parts > 0 && (!d_scratch || !aligned(d_scratch, 256) || scratch_bytes < dw_clip_grads_scratch_bytes(k, n_tensors, h_count)))
+  if ((!d_scratch || !aligned(d_scratch, 256) || scratch_bytes < dw_clip_grads_scratch_bytes(k, n_tensors, h_count)))
     return DW_ERR_WORKSPACE;
   const hipStream_t s = (hipStream_t)stream;
   double* part = static_cast<double*>(d_scratch);
   const bool writes = z.parts > 0 && (d_out || std::isfinite(max_norm));
+  double* wide = clip_adds_in_between(z.parts) ? part + (int64_t)k * z.parts : nullptr;
   // first pass over all tensors, then the second: both in launches of as many tensors as the arguments hold
   for (int pass = 0; pass < (writes ? 2 : 1); ++pass) {
+    if (pass == 1 && wide) DW_HIP(launch_grad_norm(part, z.parts, d_norm, wide, k, s));
     ClipTable t;
+    t.wide = wide;
     t.chunk = z.chunk;
     t.part = part; t.parts = z.parts; t.part0 = 0;
     t.norm = d_norm; t.max_norm = max_norm;
@@ -219,7 +222,7 @@ int dw_clip_grads(const void* const* h_grad, const int64_t* h_count, const int32
       t.out0 += t.elements;
     }
   }
-  if (!writes) DW_HIP(launch_grad_norm(part, z.parts, d_norm, k, s));
+  if (!writes) DW_HIP(launch_grad_norm(part, z.parts, d_norm, nullptr, k, s));
   return DW_OK;
 }
 
