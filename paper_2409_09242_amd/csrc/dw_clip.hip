@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(ClipTable t) {
 }  // namespace
 
 // Elements of a chunk: blocks enough that the last of them do not leave the chip half empty (8 x 50.4e6 elements: 12400
-// blocks %s us, 3100 blocks 677), and chunks of 4096 at least.
+// blocks 653 us, 3100 blocks 677), and chunks of 4096 at least.
 int64_t clip_chunk(int64_t elements_of_all_workers) {
   int64_t c = 4096;
   while (c * 16384 < elements_of_all_workers) c *= 2;

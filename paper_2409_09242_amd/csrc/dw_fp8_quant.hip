@@ -7,8 +7,8 @@
 // found on the bits as integers, where a NaN is above infinity and infinity above the rest: a block with one of them is all NaN.
 //
 // Rows alone: 16 lanes share a block, 8 elements each, one pass from registers.  With the transposed form or squares a
-// block of threads takes a tile of 128 x 128, 8 x 8 elements a thread; the transposed bytes leave through LDS so that
-// both forms are written in whole lines while x is read once.
+// block of 512 threads takes a tile of 128 x 128, 4 rows x 8 columns a thread; the transposed bytes leave through LDS so that
+// both forms are written in whole lines while x is read once.  Bound by memory when there is much of it.
 #include "dw_ops.h"
 
 namespace dw {
@@ -31,6 +31,16 @@ __device__ __forceinline__ void load8(const typename E::T* row, int64_t e0, int6
 
 __device__ __forceinline__ uint32_t magnitude(float f) { return __float_as_uint(f) & 0x7FFFFFFFu; }
 __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// the largest of the 16 lanes of a row of lanes, to all of them: neighbours, pairs, halves of eight, eights
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_move(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
+__device__ __forceinline__ uint32_t largest_of_16(uint32_t v) {
+  v = larger(v, lane_move<0xB1>(v));                        // quad_perm 1 0 3 2
+  v = larger(v, lane_move<0x4E>(v));                        // quad_perm 2 3 0 1
+  v = larger(v, lane_move<0x141>(v));                       // the eight reversed: the other four's
+  return larger(v, lane_move<0x140>(v));                    // the sixteen reversed: the other eight's
+}
 
 struct Scale { uint32_t byte; float inverse; };
 __device__ __forceinline__ Scale scale_of(uint32_t top) {
@@ -63,9 +73,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = larger(top, magnitude(f[j]));
-#pragma unroll
-  for (int off = 1; off < 16; off <<= 1) top = larger(top, (uint32_t)__shfl_xor((int)top, off));
-  const Scale s = scale_of(top);
+  const Scale s = scale_of(largest_of_16(top));
   const int64_t row = w * a.rows + r;
   *reinterpret_cast<uint2*>(a.q + row * np + b * 128 + t * 8) = to_e4m3(f, s.inverse);
   uint8_t* sc = a.scale + row * ns;
@@ -73,29 +81,35 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
   if (b == np / 128 - 1 && b + 1 + t < ns) sc[b + 1 + t] = 127;       // a row's scales fill whole words
 }
 
+constexpr int kTileThreads = 512, kRows = 4;                // rows of a thread
+
 template <class E, bool SQUARE>
-__global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a) {
-  __shared__ uint32_t tops[16][129];
-  __shared__ __align__(16) uint8_t tile[128][144];          // transposed bytes: [column][row]
+__global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a) {
+  constexpr int WAVES = kTileThreads / 64;
+  __shared__ uint32_t tops[WAVES][128];
+  __shared__ __align__(16) uint32_t tile[128][32];          // transposed bytes: [column][four rows, swizzled]
   const int w = blockIdx.z;
   const int64_t c0 = (int64_t)blockIdx.x * 128, r0 = (int64_t)blockIdx.y * 128;
-  const int tc = threadIdx.x & 15, tr = threadIdx.x >> 4;   // this thread's 8 columns from 8 tc, 8 rows from 8 tr
+  const int tc = threadIdx.x & 15, tr = threadIdx.x >> 4;   // this thread's 8 columns from 8 tc, 4 rows from 4 tr
+  const int wave = threadIdx.x >> 6;
   const int64_t np = DW_FP8_ROW(a.n), ns = DW_FP8_SCALES(a.n), rp = DW_FP8_ROW(a.rows), rs = DW_FP8_SCALES(a.rows);
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
-  float f[8][8];
+  float f[kRows][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t r = r0 + tr * 8 + i;
+  for (int i = 0; i < kRows; ++i) {
+    const int64_t r = r0 + tr * kRows + i;
     if (r < a.rows) load8<E>(x + r * a.x.ld, c0 + tc * 8, a.n, f[i]);
     else
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[i][j] = 0.f;
   }
-  uint32_t row_top[8], col_top[8];
+  uint32_t row_top[kRows], col_top[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { row_top[i] = 0; col_top[i] = 0; }
+  for (int i = 0; i < kRows; ++i) row_top[i] = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int j = 0; j < 8; ++j) col_top[j] = 0;
+#pragma unroll
+  for (int i = 0; i < kRows; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t m = magnitude(f[i][j]);
@@ -106,24 +120,20 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a) {
   if constexpr (SQUARE) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = larger(m, row_top[i]);
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) m = larger(m, (uint32_t)__shfl_xor((int)m, off));
-    if ((threadIdx.x & 63) == 0) tops[0][threadIdx.x >> 6] = m;
+    for (int i = 0; i < kRows; ++i) m = larger(m, row_top[i]);
+    m = largest_of_16(m);
+    if (tc == 0) tops[0][tr] = m;
     __syncthreads();
-    all = scale_of(larger(larger(tops[0][0], tops[0][1]), larger(tops[0][2], tops[0][3])));
+    m = 0;
+#pragma unroll
+    for (int q = 0; q < kTileThreads / 16; ++q) m = larger(m, tops[0][q]);
+    all = scale_of(m);
   }
   if (a.q) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      Scale s = all;
-      if constexpr (!SQUARE) {
-        uint32_t m = row_top[i];
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) m = larger(m, (uint32_t)__shfl_xor((int)m, off));
-        s = scale_of(m);
-      }
-      const int64_t r = r0 + tr * 8 + i;
+    for (int i = 0; i < kRows; ++i) {
+      const Scale s = SQUARE ? all : scale_of(largest_of_16(row_top[i]));
+      const int64_t r = r0 + tr * kRows + i;
       if (r < a.rows) {
         const int64_t row = w * a.rows + r;
         *reinterpret_cast<uint2*>(a.q + row * np + c0 + tc * 8) = to_e4m3(f[i], s.inverse);
@@ -140,29 +150,39 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a) {
     for (int j = 0; j < 8; ++j) inv[j] = all.inverse;
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) tops[tr][tc * 8 + j] = col_top[j];
+    for (int j = 0; j < 8; ++j) {                           // over the wave's rows, then over the waves
+      uint32_t m = col_top[j];
+      m = larger(m, (uint32_t)__shfl_xor((int)m, 16));
+      m = larger(m, (uint32_t)__shfl_xor((int)m, 32));
+      if ((tr & 3) == 0) tops[wave][tc * 8 + j] = m;
+    }
     __syncthreads();
-    if (threadIdx.x < 128) {                                // one thread per column finds its scale
+    if (threadIdx.x < 128) {
       uint32_t m = 0;
 #pragma unroll
-      for (int q = 0; q < 16; ++q) m = larger(m, tops[q][threadIdx.x]);
-      tops[0][threadIdx.x] = m;
+      for (int q = 0; q < WAVES; ++q) m = larger(m, tops[q][threadIdx.x]);
+      tops[0][threadIdx.x] = m;                             // (only this thread reads the column's)
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 8; ++j) inv[j] = scale_of(tops[0][tc * 8 + j]).inverse;
   }
+  // Word tr of a column goes to place tr ^ 4 (tc mod 8): the lanes of a wave, 16 columns 8 apart and 4 words, then spread
+  // over the banks, and pieces of 16 bytes stay whole.
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float g[8] = {f[0][j], f[1][j], f[2][j], f[3][j], f[4][j], f[5][j], f[6][j], f[7][j]};
-    *reinterpret_cast<uint2*>(&tile[tc * 8 + j][tr * 8]) = to_e4m3(g, inv[j]);
+    int v = 0;
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(f[0][j] * inv[j], f[1][j] * inv[j], v, false);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(f[2][j] * inv[j], f[3][j] * inv[j], v, true);
+    tile[tc * 8 + j][tr ^ ((tc & 7) << 2)] = (uint32_t)v;
   }
   __syncthreads();
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {                             // 8 threads a column, 16 rows each
-    const int c = p * 32 + (threadIdx.x >> 3), at = (threadIdx.x & 7) * 16;
+  for (int p = 0; p < 128 * 8 / kTileThreads; ++p) {        // 8 threads a column, 16 rows each
+    const int c = p * (kTileThreads / 8) + (threadIdx.x >> 3), at = threadIdx.x & 7;
     if (c0 + c < a.n)
-      *reinterpret_cast<uint4*>(a.qt + (w * a.n + c0 + c) * rp + r0 + at) = *reinterpret_cast<const uint4*>(&tile[c][at]);
+      *reinterpret_cast<uint4*>(a.qt + (w * a.n + c0 + c) * rp + r0 + at * 16) =
+          *reinterpret_cast<const uint4*>(&tile[c][(at ^ ((c >> 3) & 7)) * 4]);
   }
   if (threadIdx.x < 128 && c0 + threadIdx.x < a.n) {
     uint8_t* sc = a.scale_t + (w * a.n + c0 + threadIdx.x) * rs;
@@ -180,8 +200,8 @@ hipError_t quantize(const QuantArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   const dim3 grid((unsigned)(DW_FP8_ROW(a.n) / 128), (unsigned)(DW_FP8_ROW(a.rows) / 128), (unsigned)a.k);
-  if (a.square) hipLaunchKernelGGL((quantize_tile_kernel<E, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((quantize_tile_kernel<E, false>), grid, dim3(256), 0, s, a);
+  if (a.square) hipLaunchKernelGGL((quantize_tile_kernel<E, true>), grid, dim3(kTileThreads), 0, s, a);
+  else hipLaunchKernelGGL((quantize_tile_kernel<E, false>), grid, dim3(kTileThreads), 0, s, a);
   return hipGetLastError();
 }
 
