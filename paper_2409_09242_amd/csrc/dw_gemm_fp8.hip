@@ -352,6 +352,105 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   }
 }
 
+// Few rows of a (a served model's tokens): the product is as fast as b can be read.  A block takes 16 rows of b and all of
+// a, MT tiles of 16 rows; its waves deal the blocks of 128 out among themselves, each reading whole lines of b straight
+// into registers, and add their sums up through LDS in order.  v_mfma_scale_f32_16x16x128_f8f6f4, b as operand A: a lane
+// holds one row of a and four consecutive columns of C.  (EXACT: v_mfma_f32_16x16x32_bf16 on widened numbers, see above.)
+// A lane reads 16 bytes at 16 (lane/16) and 16 at 64 + 16 (lane/16) of a row's 128: any division of the block among the
+// lanes will do as long as it is the same for both operands.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kRowWaves = 8;
+
+template <int MT, bool EXACT>
+__global__ __launch_bounds__(kRowWaves * 64) void gemm_fp8_rows_kernel(Fp8Args a) {
+  constexpr int WAVES = kRowWaves, AHEAD = 4 / MT < 2 ? 2 : 4 / MT;             // blocks of 128 a wave has in flight
+  __shared__ float sums[WAVES][MT][16][17];
+  const int w = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int r16 = lane & 15, part = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int blocks = (int)(a.kp / BK);
+  const int64_t nr = n0 + r16 < a.n ? n0 + r16 : a.n - 1;
+  const uint8_t* pb = a.b + (w * a.n + nr) * a.kp + part * 16;
+  const uint8_t* psb = a.sb + (w * a.n + nr) * a.ks;
+  const uint8_t* pa[MT];
+  const uint8_t* psa[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t mr = i * 16 + r16 < a.m ? i * 16 + r16 : a.m - 1;
+    pa[i] = a.a + (w * a.m + mr) * a.kp + part * 16;
+    psa[i] = a.sa + (w * a.m + mr) * a.ks;
+  }
+  struct Piece { uint4 lo, hi; int scale; };
+  auto read = [](const uint8_t* row, const uint8_t* scales, int b) {
+    return Piece{*reinterpret_cast<const uint4*>(row + (int64_t)b * BK), *reinterpret_cast<const uint4*>(row + (int64_t)b * BK + 64), scales[b]};
+  };
+  auto all = [](const Piece& p) {
+    const i32x8 r = {(int)p.lo.x, (int)p.lo.y, (int)p.lo.z, (int)p.lo.w, (int)p.hi.x, (int)p.hi.y, (int)p.hi.z, (int)p.hi.w};
+    return r;
+  };
+  f32x4 acc[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](const Piece& y, const Piece (&x)[MT]) {
+    if constexpr (EXACT) {
+      const float sy = power(y.scale);
+      const bf16x8 y0 = widen((int)y.lo.x, (int)y.lo.y, sy), y1 = widen((int)y.lo.z, (int)y.lo.w, sy);
+      const bf16x8 y2 = widen((int)y.hi.x, (int)y.hi.y, sy), y3 = widen((int)y.hi.z, (int)y.hi.w, sy);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const float sx = power(x[i].scale);
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y0, widen((int)x[i].lo.x, (int)x[i].lo.y, sx), acc[i], 0, 0, 0);
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y1, widen((int)x[i].lo.z, (int)x[i].lo.w, sx), acc[i], 0, 0, 0);
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y2, widen((int)x[i].hi.x, (int)x[i].hi.y, sx), acc[i], 0, 0, 0);
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y3, widen((int)x[i].hi.z, (int)x[i].hi.w, sx), acc[i], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(all(y), all(x[i]), acc[i], 0, 0, 0, y.scale, 0, x[i].scale);
+    }
+  };
+  // AHEAD blocks at a time, all of their loads before the first product: nothing else hides what a load takes
+  for (int b = wave; b < blocks; b += AHEAD * WAVES) {
+    Piece y[AHEAD], x[AHEAD][MT];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (b + u * WAVES < blocks) {
+        y[u] = read(pb, psb, b + u * WAVES);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x[u][i] = read(pa[i], psa[i], b + u * WAVES);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (b + u * WAVES < blocks) multiply(y[u], x[u]);
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sums[wave][i][r16][part * 4 + r] = acc[i][r];
+  __syncthreads();
+  for (int e = threadIdx.x; e < MT * 256; e += WAVES * 64) {
+    const int m = e >> 4, c = e & 15;
+    if (m >= a.m || n0 + c >= a.n) continue;
+    float s = a.bias ? a.bias[w * a.bias_stride + n0 + c] : 0.f;
+#pragma unroll
+    for (int q = 0; q < WAVES; ++q) s += sums[q][m >> 4][m & 15][c];
+    const int64_t at = w * a.c_stride + m * a.ldc + n0 + c;
+    if constexpr (EXACT) F32::put(reinterpret_cast<float*>(a.c) + at, s);
+    else Bf16::put(reinterpret_cast<uint16_t*>(a.c) + at, s);
+  }
+}
+
+template <int MT>
+hipError_t launch_rows(const Fp8Args& a, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div(a.n, 16), (unsigned)a.k), block(kRowWaves * 64);
+  if (a.dtype == DW_F32) hipLaunchKernelGGL((gemm_fp8_rows_kernel<MT, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((gemm_fp8_rows_kernel<MT, false>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
 // an empty contraction: the bias, or zeros
 __global__ __launch_bounds__(256) void bias_rows_kernel(Fp8Args a) {
   const int w = blockIdx.z;
@@ -369,35 +468,97 @@ using Large = Config<4, 4, 2, 2, 1, 2>;                      // 256 x 256, a wav
 using Middle = Config<2, 2, 2, 2, 2, 2>;                     // 128 x 128
 using Small = Config<1, 1, 2, 2, 2, 4>;                      // 64 x 64
 
-template <class C, bool EXACT>
-hipError_t launch_one(const Fp8Args& a, hipStream_t s) {
+// the slices' sums in their order, and the bias
+template <class E>
+__global__ __launch_bounds__(256) void add_slices_kernel(Fp8Args a, int slices) {
+  const int w = blockIdx.z;
+  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)a.k * a.m * a.n;
+  if (n >= a.n) return;
+  const float bias = a.bias ? a.bias[w * a.bias_stride + n] : 0.f;
+  for (int64_t m = blockIdx.y; m < a.m; m += gridDim.y) {
+    const float* p = a.part + ((int64_t)w * a.m + m) * a.n + n;
+    float s = bias;
+#pragma unroll 4
+    for (int i = 0; i < slices; ++i) s += p[i * step];
+    E::put(reinterpret_cast<typename E::T*>(a.c) + w * a.c_stride + m * a.ldc + n, s);
+  }
+}
+
+template <class C, bool EXACT, bool SLICE>
+hipError_t launch_one(const Fp8Args& a, int slices, hipStream_t s) {
   const int64_t tiles = ceil_div(a.m, C::BM) * ceil_div(a.n, C::BN) * a.k;
-  auto kern = gemm_fp8_kernel<C, EXACT, false>;
+  auto kern = gemm_fp8_kernel<C, EXACT, SLICE>;
   static LdsLimitOnce lds_limit;
   const hipError_t e = lds_limit.raise(reinterpret_cast<const void*>(kern), C::LDS);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(tiles, 8) * 8)), dim3(C::NT), C::LDS, s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(tiles, 8) * 8), (unsigned)slices), dim3(C::NT), C::LDS, s, a);
   return hipGetLastError();
 }
 
 template <class C>
 hipError_t launch(const Fp8Args& a, hipStream_t s) {
-  return a.dtype == DW_F32 ? launch_one<C, true>(a, s) : launch_one<C, false>(a, s);
+  return a.dtype == DW_F32 ? launch_one<C, true, false>(a, 1, s) : launch_one<C, false, false>(a, 1, s);
 }
 
-int64_t tiles_of(const Fp8Args& a, int b) { return ceil_div(a.m, b) * ceil_div(a.n, b) * a.k; }
+int64_t tiles_of(int k, int64_t m, int64_t n, int b) { return ceil_div(m, b) * ceil_div(n, b) * k; }
+
+// Which kernel a product takes.  The rows kernel reads a anew for every 16 rows of b and is held by how fast a compute unit
+// takes in rows of 64 bytes, so its time grows with m and with the contraction a wave goes through; the tiles read 64 rows of a
+// whatever m is and are cut into slices where they are few.  Both sides, us, in bf16 (fp32 alike):
+//   4096 x 4096            m = 1: 5.4, 7.0;  m = 16: 7.6, 7.8;  m = 32: 10.4, 8.5
+//   four of 8192 x 2048    m = 1: 14.7, 16.6;  m = 8: 18, 16;   256 x 1024   m = 1: 2.4, 4.5;  m = 64: 4.8, 4.7
+//   1024 x 8192            m = 1: 8.0, 7.2;  m = 16: 12, 7.6;   8192 x 8192  m = 1: 15, 15;  m = 16: 23, 16
+bool rows_kernel(int k, int64_t m, int64_t n, int64_t kp) {
+  if (kp > 4096 || m > 64 || m * kp > 65536) return false;
+  return m <= 4 || tiles_of(k, m, n, 64) < kCus;
+}
+
+// Slices of the contraction (whole words of scales, 512 numbers) for products with fewer 64 x 64 tiles than compute units,
+// by what they would take: 0.3 us a block of 128 (bf16 0.25, fp32 0.45), and for slices 3.5 us and their sums, written and
+// read, at 2 TB/s.  1024 x 8192, m = 64: 18 us whole, 8.5 in slices; 4096 x 4096, m = 128: 11 whole, 13.4 in two, 15.3 in four.
+int slices_of(int k, int64_t m, int64_t n, int64_t blocks) {
+  const int64_t tiles = tiles_of(k, m, n, 64), words = ceil_div(blocks, GROUP);
+  int best = 1;
+  double least = 0.3 * (double)blocks;
+  for (int64_t s = 2; s <= 16 && s <= words && tiles * s <= 2 * kCus; ++s) {
+    const int64_t per = ceil_div(words, s);
+    if (ceil_div(words, per) != s) continue;                 // (a slice would be empty)
+    const double t = 0.3 * (double)(per * GROUP) + 3.5 + (double)s * (double)(k * m * n) * 8.0 / 2e6;
+    if (t < least) { least = t; best = (int)s; }
+  }
+  return best;
+}
 
 }  // namespace fp8
 
-hipError_t launch_fp8_matmul(const Fp8Args& a, hipStream_t s) {
+size_t fp8_scratch_bytes(int k, int64_t m, int64_t n, int64_t kp) {
+  const int s = fp8::rows_kernel(k, m, n, kp) ? 1 : fp8::slices_of(k, m, n, kp / fp8::BK);
+  return s > 1 ? (size_t)s * k * m * n * sizeof(float) : 0;
+}
+
+hipError_t launch_fp8_matmul(const Fp8Args& a_, hipStream_t s) {
+  Fp8Args a = a_;
   if (a.kp == 0) {
     const dim3 grid((unsigned)ceil_div(a.n, 256), (unsigned)(a.m < 1024 ? a.m : 1024), (unsigned)a.k);
     hipLaunchKernelGGL(fp8::bias_rows_kernel, grid, dim3(256), 0, s, a);
     return hipGetLastError();
   }
-  if (fp8::tiles_of(a, 256) >= kCus) return fp8::launch<fp8::Large>(a, s);
-  if (fp8::tiles_of(a, 128) >= kCus) return fp8::launch<fp8::Middle>(a, s);
-  return fp8::launch<fp8::Small>(a, s);
+  if (fp8::rows_kernel(a.k, a.m, a.n, a.kp)) {
+    if (a.m <= 16) return fp8::launch_rows<1>(a, s);
+    return a.m <= 32 ? fp8::launch_rows<2>(a, s) : fp8::launch_rows<4>(a, s);
+  }
+  if (fp8::tiles_of(a.k, a.m, a.n, 256) >= kCus) return fp8::launch<fp8::Large>(a, s);
+  if (fp8::tiles_of(a.k, a.m, a.n, 128) >= kCus) return fp8::launch<fp8::Middle>(a, s);
+  const int slices = fp8::slices_of(a.k, a.m, a.n, a.kp / fp8::BK);
+  if (slices == 1) return fp8::launch<fp8::Small>(a, s);
+  const int words = (int)ceil_div(a.kp / fp8::BK, fp8::GROUP);
+  a.slice_blocks = (int)ceil_div(words, slices) * fp8::GROUP;    // (the last slice may be shorter, none is empty)
+  const hipError_t e = a.dtype == DW_F32 ? fp8::launch_one<fp8::Small, true, true>(a, slices, s) : fp8::launch_one<fp8::Small, false, true>(a, slices, s);
+  if (e != hipSuccess) return e;
+  const dim3 grid((unsigned)ceil_div(a.n, 256), (unsigned)(a.m < 1024 ? a.m : 1024), (unsigned)a.k);
+  if (a.dtype == DW_F32) hipLaunchKernelGGL(fp8::add_slices_kernel<F32>, grid, dim3(256), 0, s, a, slices);
+  else hipLaunchKernelGGL(fp8::add_slices_kernel<Bf16>, grid, dim3(256), 0, s, a, slices);
+  return hipGetLastError();
 }
 
 }  // namespace dw

@@ -269,6 +269,7 @@ struct Fp8Args {
   int64_t m, n, kp, ks;                                    // kp: padded contraction; ks: scale bytes of a row
   float* part; int slice_blocks;                           // slices of the contraction: [slices][k][m][n], blocks of 128 each
 };
+size_t fp8_scratch_bytes(int k, int64_t m, int64_t n, int64_t kp);
 hipError_t launch_fp8_matmul(const Fp8Args& a, hipStream_t s);
 
 }  // namespace dw

@@ -243,7 +243,8 @@ int dw_fp8_quantize(const void* d_x, int64_t x_ld, int64_t x_stride, int k, int6
 }
 
 size_t dw_fp8_matmul_scratch_bytes(int k, int64_t m, int64_t n, int64_t contraction) {
-  return 0;
+  if (k < 1 || k > DW_MAX_K || m < 1 || m > DW_MAX_FP8 || n < 1 || n > DW_MAX_FP8 || contraction < 1 || contraction > DW_MAX_FP8) return 0;
+  return fp8_scratch_bytes(k, m, n, DW_FP8_ROW(contraction));
 }
 
 int dw_fp8_matmul(const uint8_t* d_a, const uint8_t* d_a_scale, const uint8_t* d_b, const uint8_t* d_b_scale, const float* d_bias,
@@ -256,12 +257,15 @@ int dw_fp8_matmul(const uint8_t* d_a, const uint8_t* d_a_scale, const uint8_t* d
   if (!aligned(d_a, 16) || !aligned(d_b, 16) || !aligned(d_a_scale, 4) || !aligned(d_b_scale, 4)) return DW_ERR_ARG;
   if (!params_ok(d_bias, bias_stride) || !out_ok(d_c, c_ld, c_stride, k, m, n, type_bytes(dtype))) return DW_ERR_ARG;
   if (ceil_div(m, 64) * ceil_div(n, 64) * k > (1 << 22)) return DW_ERR_TOO_LARGE;
+  const size_t need = dw_fp8_matmul_scratch_bytes(k, m, n, contraction);
+  if (need > 0 && (!d_scratch || !aligned(d_scratch, 256) || scratch_bytes < need)) return DW_ERR_WORKSPACE;
   Fp8Args a = {};
   a.a = d_a; a.sa = d_a_scale; a.b = d_b; a.sb = d_b_scale;
   a.bias = d_bias; a.bias_stride = bias_stride;
   a.c = d_c; a.ldc = c_ld; a.c_stride = c_stride;
   a.k = k; a.dtype = dtype; a.m = m; a.n = n;
   a.kp = DW_FP8_ROW(contraction); a.ks = DW_FP8_SCALES(contraction);
+  a.part = static_cast<float*>(d_scratch);
   DW_HIP(launch_fp8_matmul(a, (hipStream_t)stream));
   return DW_OK;
 }
