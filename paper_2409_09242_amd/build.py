@@ -1,4 +1,5 @@
-"""Build libdw.so (the C-ABI library) from csrc/*.hip for gfx950, in-tree.
+"""Build libdw.so (the C-ABI library) from csrc/*.hip for gfx950, and _dw_torch.so (its tensor-level entry, host code) from
+csrc/dw_torch.cpp, in-tree.
 
 Usage:  python -m paper_2409_09242_amd.build
 """
@@ -15,6 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdw.so")
+TORCH_LIB = os.path.join(HERE, "_dw_torch.so")          # imported as paper_2409_09242_amd._dw_torch
 STAMP = os.path.join(HERE, "libdw.sources.sha256")      # digest of the sources the library was built from
 
 FLAGS = [
@@ -44,6 +46,35 @@ def _compile(src: str) -> str:
     if "warning:" in warn:
         sys.stderr.write(warn + "\n")
     return obj
+
+
+def _compile_torch_module() -> str:
+    """csrc/dw_torch.cpp with the host compiler against torch's headers; it is linked once libdw.so is there."""
+    import sysconfig
+    import torch
+    inc = os.path.join(os.path.dirname(torch.__file__), "include")
+    obj = os.path.join(OBJ, "dw_torch.cpp.o")
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-I", os.path.join(ROOT, "include"),
+           "-isystem", inc, "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"],
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+           "-c", os.path.join(CSRC, "dw_torch.cpp"), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed for dw_torch.cpp:\n%s\n%s" % (r.stdout, r.stderr))
+    if "warning:" in r.stderr:
+        sys.stderr.write(r.stderr)
+    return obj
+
+
+def _link_torch_module(obj: str) -> None:
+    import torch
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = [shutil.which("g++") or "g++", "-shared", "-o", TORCH_LIB, obj, "-L", HERE, "-l:" + os.path.basename(LIB),
+           "-L", lib, "-lc10", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))
 
 
 # The data-gradient kernel of dw_gemm_bf16_dma.hip issues its LDS transpose reads from inline assembly, so the
@@ -107,7 +138,7 @@ def check_transposed_reads() -> str:
 def _source_digest() -> str:
     import hashlib
     h = hashlib.sha256()
-    files = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hip", ".h")))
+    files = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hip", ".h", ".cpp")))
     files.append(os.path.join(ROOT, "include", "dw.h"))
     for f in files:
         h.update(os.path.basename(f).encode() + b"\0")
@@ -120,14 +151,17 @@ def build(verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
     digest = _source_digest()
     srcs = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".hip"))
-    with ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:
+    with ThreadPoolExecutor(max_workers=min(8, len(srcs) + 2)) as ex:
         check = ex.submit(check_transposed_reads)
+        torch_obj = ex.submit(_compile_torch_module)
         objs = list(ex.map(_compile, srcs))
         check.result()
+        torch_obj = torch_obj.result()
     cmd = [_hipcc(), "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))
+    _link_torch_module(torch_obj)
     with open(STAMP, "w") as f:
         f.write(digest + "\n")
     if verbose:
@@ -139,7 +173,7 @@ def ensure_built() -> str:
     """Build the library when none is there, or when the sources have changed since the one that is there was built
     (its digest file says so; a library without a digest file is taken as it is).  Tests, the smoke check and the
     benchmark call this.  The binding itself does not: without a library it raises."""
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(TORCH_LIB)):
         return build(verbose=True)
     if os.path.exists(STAMP) and open(STAMP).read().strip() != _source_digest():
         sys.stderr.write("libdw.so is older than its sources: building again\n")
