@@ -68,8 +68,9 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
   return reinterpret_cast<const uint8_t*>((uint64_t)hi << 32 | lo);
 }
 
-template <int WTM_, int WTN_, int WM_, int WN_, int PER_CU_, int STAGES_>
+template <int WTM_, int WTN_, int WM_, int WN_, int PER_CU_, int STAGES_, int LATE_8THS_>
 struct Config {
+  static constexpr int LATE_8THS = LATE_8THS_;              // eighths of a block's loads that are put off by a step
   static constexpr int WTM = WTM_, WTN = WTN_, WM = WM_, WN = WN_, PER_CU = PER_CU_, STAGES = STAGES_;
   static constexpr int NW = WM * WN, NT = NW * 64;
   static constexpr int BM = WM * WTM * 32, BN = WN * WTN * 32;
@@ -241,8 +242,10 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   // of block b, whose stage is loaded anew, and block b + 1 has arrived (the counts leave the blocks behind it in flight;
   // loads of scale words, which are not counted, only make a wait longer).  Loads and reads are dealt out among the products
   // and kept there: the waves come from the barrier together, and a load put in front of the products would hold them all up.
+  // The last LATE pieces of a block are loaded in the first half of the step behind the barrier's.
+  constexpr int LATE = C::CPW * C::LATE_8THS / 8;
   auto step = [&](Frags& now, Frags& next, int b, auto more, auto sub) {
-    constexpr bool MORE = decltype(more)::value;             // block b + STAGES exists
+    constexpr bool MORE = decltype(more)::value;             // SUB 1: block b + STAGES exists; SUB 0: b - 1 + STAGES does, and b > 0
     constexpr int SUB = decltype(sub)::value;
     if constexpr (SUB == 1) {
       if constexpr (MORE) wait_vm<C::CPW * (C::STAGES - 2)>();
@@ -253,7 +256,8 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
       }
     }
     const bool reads = SUB == 0 || MORE || b + 1 < blocks;
-    const uint8_t* from = uniform(base + (int64_t)(b + C::STAGES) * BK);
+    const int loads = SUB == 1 ? b : b - 1;                  // whose stage is loaded anew
+    const uint8_t* from = uniform(base + (int64_t)(loads + C::STAGES) * BK);
     constexpr int Q = EXACT ? 4 : 1, PRODUCTS = C::WTM * C::WTN * Q, OPERANDS = C::WTM + C::WTN;
     Wide wide[2];
     if constexpr (EXACT) {
@@ -270,7 +274,12 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
       } else {
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(now.y[j]), whole(now.x[i]), acc[i][j], 0, 0, 0, sy[j], 0, sx[i]);
       }
-      if constexpr (MORE && SUB == 1) each<p * C::CPW / PRODUCTS, (p + 1) * C::CPW / PRODUCTS>([&](auto c) { issue(from, b, c); });
+      if constexpr (MORE && SUB == 1) {
+        each<p * (C::CPW - LATE) / PRODUCTS, (p + 1) * (C::CPW - LATE) / PRODUCTS>([&](auto c) { issue(from, loads, c); });
+      } else if constexpr (MORE) {
+        constexpr int HALF = PRODUCTS < 2 ? 1 : PRODUCTS / 2, at = p < HALF ? p : HALF, to = p + 1 < HALF ? p + 1 : HALF;
+        each<C::CPW - LATE + at * LATE / HALF, C::CPW - LATE + to * LATE / HALF>([&](auto c) { issue(from, loads, c); });
+      }
       if (reads) {
         each<p * READS / PRODUCTS, (p + 1) * READS / PRODUCTS>([&](auto r) { read_one(next, b + SUB, 1 - SUB, r); });
         if constexpr (SUB == 1 && p == PRODUCTS / 2) read_scales(b + 1);
@@ -283,14 +292,15 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   using no = std::false_type;
   using first_step = std::integral_constant<int, 0>;
   using second_step = std::integral_constant<int, 1>;
+  step(f0, f1, 0, no{}, first_step{});
   int b = 0;
   for (; b + C::STAGES < blocks; ++b) {
-    step(f0, f1, b, yes{}, first_step{});
     step(f1, f0, b, yes{}, second_step{});
+    step(f0, f1, b + 1, yes{}, first_step{});
   }
   for (; b < blocks; ++b) {
-    step(f0, f1, b, no{}, first_step{});
     step(f1, f0, b, no{}, second_step{});
+    if (b + 1 < blocks) step(f0, f1, b + 1, no{}, first_step{});
   }
 
   __syncthreads();                                           // the stages are free: each wave stages its rows in its share
@@ -464,9 +474,9 @@ __global__ __launch_bounds__(256) void bias_rows_kernel(Fp8Args a) {
   }
 }
 
-using Large = Config<4, 4, 2, 2, 1, 2>;                      // 256 x 256, a wave 128 x 128
-using Middle = Config<2, 2, 2, 2, 2, 2>;                     // 128 x 128
-using Small = Config<1, 1, 2, 2, 2, 4>;                      // 64 x 64
+using Large = Config<4, 4, 2, 2, 1, 2, 3>;                      // 256 x 256, a wave 128 x 128
+using Middle = Config<2, 2, 2, 2, 2, 2, 0>;                     // 128 x 128
+using Small = Config<1, 1, 2, 2, 2, 4, 0>;                      // 64 x 64
 
 // the slices' sums in their order, and the bias
 template <class E>
