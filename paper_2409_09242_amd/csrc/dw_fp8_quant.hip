@@ -15,19 +15,40 @@ namespace dw {
 
 namespace {
 
-// elements e0 .. e0+7 of a row of n as fp32 (zero past the end)
+// eight elements of a row as they are in memory
 template <class E>
-__device__ __forceinline__ void load8(const typename E::T* row, int64_t e0, int64_t n, float (&f)[8]) {
+struct Raw8 {
+  uint32_t w[8 / E::V][4];
+  // elements e0 .. e0+7 of a row of n (zero past the end)
+  __device__ __forceinline__ void load(const typename E::T* row, int64_t e0, int64_t n) {
 #pragma unroll
-  for (int h = 0; h < 8 / E::V; ++h) {
-    uint32_t raw[4];
-    float v[E::V];
-    load16<E>(row, e0 + h * E::V, n, raw);
-    E::unpack(raw, v);
-#pragma unroll
-    for (int j = 0; j < E::V; ++j) f[h * E::V + j] = v[j];
+    for (int h = 0; h < 8 / E::V; ++h) load16<E>(row, e0 + h * E::V, n, w[h]);
   }
-}
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int h = 0; h < 8 / E::V; ++h)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[h][j] = 0u;
+  }
+  __device__ __forceinline__ void floats(float (&f)[8]) const {
+#pragma unroll
+    for (int h = 0; h < 8 / E::V; ++h) {
+      float v[E::V];
+      E::unpack(w[h], v);
+#pragma unroll
+      for (int j = 0; j < E::V; ++j) f[h * E::V + j] = v[j];
+    }
+  }
+  __device__ __forceinline__ float one(int j) const {       // (j is a constant where this is used)
+    const uint32_t u = w[j / E::V][E::V == 8 ? j / 2 : j % 4];
+    return __uint_as_float(E::V == 4 ? u : j & 1 ? u & 0xFFFF0000u : u << 16);
+  }
+  // what it holds is unpacked anew where it is used next: registers hold it packed in between
+  __device__ __forceinline__ void keep_packed() {
+#pragma unroll
+    for (int h = 0; h < 8 / E::V; ++h) asm volatile("" : "+v"(w[h][0]), "+v"(w[h][1]), "+v"(w[h][2]), "+v"(w[h][3]));
+  }
+};
 
 __device__ __forceinline__ uint32_t magnitude(float f) { return __float_as_uint(f) & 0x7FFFFFFFu; }
 __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
@@ -69,7 +90,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
   if (r >= a.rows) return;                                  // (16 lanes at once: those that exchange values stay together)
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride + r * a.x.ld;
   float f[8];
-  load8<E>(x, b * 128 + t * 8, a.n, f);
+  Raw8<E> raw;
+  raw.load(x, b * 128 + t * 8, a.n);
+  raw.floats(f);
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = larger(top, magnitude(f[j]));
@@ -94,14 +117,12 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
   const int wave = threadIdx.x >> 6;
   const int64_t np = DW_FP8_ROW(a.n), ns = DW_FP8_SCALES(a.n), rp = DW_FP8_ROW(a.rows), rs = DW_FP8_SCALES(a.rows);
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
-  float f[kRows][8];
+  Raw8<E> raw[kRows];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
     const int64_t r = r0 + tr * kRows + i;
-    if (r < a.rows) load8<E>(x + r * a.x.ld, c0 + tc * 8, a.n, f[i]);
-    else
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[i][j] = 0.f;
+    if (r < a.rows) raw[i].load(x + r * a.x.ld, c0 + tc * 8, a.n);
+    else raw[i].zero();
   }
   uint32_t row_top[kRows], col_top[8];
 #pragma unroll
@@ -109,13 +130,17 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
 #pragma unroll
   for (int j = 0; j < 8; ++j) col_top[j] = 0;
 #pragma unroll
-  for (int i = 0; i < kRows; ++i)
+  for (int i = 0; i < kRows; ++i) {
+    float f[8];
+    raw[i].floats(f);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint32_t m = magnitude(f[i][j]);
+      const uint32_t m = magnitude(f[j]);
       row_top[i] = larger(row_top[i], m);
       col_top[j] = larger(col_top[j], m);
     }
+    raw[i].keep_packed();
+  }
   Scale all = {127u, 1.f};
   if constexpr (SQUARE) {
     uint32_t m = 0;
@@ -136,7 +161,9 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
       const int64_t r = r0 + tr * kRows + i;
       if (r < a.rows) {
         const int64_t row = w * a.rows + r;
-        *reinterpret_cast<uint2*>(a.q + row * np + c0 + tc * 8) = to_e4m3(f[i], s.inverse);
+        float f[8];
+        raw[i].floats(f);
+        *reinterpret_cast<uint2*>(a.q + row * np + c0 + tc * 8) = to_e4m3(f, s.inverse);
         uint8_t* sc = a.scale + row * ns;
         if (tc == 0) sc[blockIdx.x] = (uint8_t)s.byte;
         if (blockIdx.x == gridDim.x - 1 && blockIdx.x + 1 + tc < ns) sc[blockIdx.x + 1 + tc] = 127;
@@ -144,11 +171,9 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
     }
   }
   if (!a.qt) return;
-  float inv[8];
-  if constexpr (SQUARE) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) inv[j] = all.inverse;
-  } else {
+  __shared__ float inverse[128];
+  Scale mine = all;                                         // of column threadIdx.x, for the first 128 threads
+  if constexpr (!SQUARE) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {                           // over the wave's rows, then over the waves
       uint32_t m = col_top[j];
@@ -161,19 +186,21 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
       uint32_t m = 0;
 #pragma unroll
       for (int q = 0; q < WAVES; ++q) m = larger(m, tops[q][threadIdx.x]);
-      tops[0][threadIdx.x] = m;                             // (only this thread reads the column's)
+      mine = scale_of(m);
+      inverse[threadIdx.x] = mine.inverse;
     }
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 8; ++j) inv[j] = scale_of(tops[0][tc * 8 + j]).inverse;
   }
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) raw[i].keep_packed();
   // Word tr of a column goes to place tr ^ 4 (tc mod 8): the lanes of a wave, 16 columns 8 apart and 4 words, then spread
   // over the banks, and pieces of 16 bytes stay whole.
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
+    const float inv = SQUARE ? all.inverse : inverse[tc * 8 + j];
     int v = 0;
-    v = __builtin_amdgcn_cvt_pk_fp8_f32(f[0][j] * inv[j], f[1][j] * inv[j], v, false);
-    v = __builtin_amdgcn_cvt_pk_fp8_f32(f[2][j] * inv[j], f[3][j] * inv[j], v, true);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(raw[0].one(j) * inv, raw[1].one(j) * inv, v, false);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(raw[2].one(j) * inv, raw[3].one(j) * inv, v, true);
     tile[tc * 8 + j][tr ^ ((tc & 7) << 2)] = (uint32_t)v;
   }
   __syncthreads();
@@ -186,7 +213,7 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
   }
   if (threadIdx.x < 128 && c0 + threadIdx.x < a.n) {
     uint8_t* sc = a.scale_t + (w * a.n + c0 + threadIdx.x) * rs;
-    sc[blockIdx.y] = (uint8_t)(SQUARE ? all.byte : scale_of(tops[0][threadIdx.x]).byte);
+    sc[blockIdx.y] = (uint8_t)mine.byte;
     if (blockIdx.y == gridDim.y - 1)
       for (int64_t q = blockIdx.y + 1; q < rs; ++q) sc[q] = 127;
   }
