@@ -399,6 +399,15 @@ int dw_fp8_matmul(const uint8_t* d_a, const uint8_t* d_a_scale, const uint8_t* d
                   int64_t c_stride, void* d_scratch, size_t scratch_bytes, void* stream);
 
 /*
+ * y = x W^T (+ bias) with x [k][m] rows of `contraction` in `dtype`, quantised on the way as dw_fp8_quantize does, W in 8 bits
+ * ([k][n] rows), y [k][m][n] in `dtype`: bit for bit dw_fp8_matmul of the two, for a few rows in one launch.
+ */
+size_t dw_fp8_linear_scratch_bytes(int k, int64_t m, int64_t n, int64_t contraction);
+int dw_fp8_linear(const void* d_x, int64_t x_ld, int64_t x_stride, const uint8_t* d_w, const uint8_t* d_w_scale, const float* d_bias,
+                  int64_t bias_stride, int k, int64_t m, int64_t n, int64_t contraction, int dtype, void* d_y, int64_t y_ld,
+                  int64_t y_stride, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Per-kernel timing for benchmarks (not part of the method).  While enabled, every kernel the handle launches
  * is bracketed by two HIP events on the caller's stream.  dw_profile_read synchronises the stream and returns,
  * per kernel class, the number of launches and their summed duration in milliseconds since the last read

@@ -30,7 +30,8 @@ EXPORTS = ("dw_strerror", "dw_last_hip_error", "dw_param_count", "dw_workspace_b
            "dw_profile", "dw_profile_read", "dw_partition_scratch_bytes", "dw_overlap_partition", "dw_draw_batch",
            "dw_overlap_partition_static", "dw_layer_norm", "dw_layer_norm_grad_scratch_bytes", "dw_layer_norm_grad",
            "dw_token_logp", "dw_policy_loss_scratch_bytes", "dw_policy_loss", "dw_clip_grads_scratch_bytes", "dw_clip_grads",
-           "dw_fp8_quantize", "dw_fp8_matmul_scratch_bytes", "dw_fp8_matmul")
+           "dw_fp8_quantize", "dw_fp8_matmul_scratch_bytes", "dw_fp8_matmul",
+           "dw_fp8_linear_scratch_bytes", "dw_fp8_linear")
 KERNEL_CLASSES = ("rademacher", "gemm_fwd", "head", "gemm_wgrad", "gemm_dgrad", "update", "weights", "pull", "gather", "step")
 
 
@@ -114,6 +115,10 @@ def lib() -> C.CDLL:
     L.dw_fp8_matmul_scratch_bytes.argtypes = [i32, i64, i64, i64]
     L.dw_fp8_matmul.restype = i32
     L.dw_fp8_matmul.argtypes = [vp, vp, vp, vp, vp, i64, i32, i64, i64, i64, i32, vp, i64, i64, vp, sz, vp]
+    L.dw_fp8_linear_scratch_bytes.restype = sz
+    L.dw_fp8_linear_scratch_bytes.argtypes = [i32, i64, i64, i64]
+    L.dw_fp8_linear.restype = i32
+    L.dw_fp8_linear.argtypes = [vp, i64, i64, vp, vp, vp, i64, i32, i64, i64, i64, i32, vp, i64, i64, vp, sz, vp]
     _LIB = L
     return L
 

@@ -23,7 +23,7 @@
 #include <type_traits>
 #include <utility>
 
-#include "dw_ops.h"
+#include "dw_fp8.h"
 
 namespace dw {
 
@@ -370,9 +370,12 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
 // lanes will do as long as it is the same for both operands.
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// E: a is not quantised yet (rows of a.x).  Every block does it for itself, into LDS, while its first loads of b are on their
+// way: that costs less than a launch in front while the rows are few.  Rows in LDS are 16 bytes longer than their numbers, so
+// that 16 of them lie over all banks.
 constexpr int kRowWaves = 8;
 
-template <int MT, bool EXACT>
+template <int MT, bool EXACT, class E>
 __global__ __launch_bounds__(kRowWaves * 64) void gemm_fp8_rows_kernel(Fp8Args a) {
   constexpr int WAVES = kRowWaves, AHEAD = 4 / MT < 2 ? 2 : 4 / MT;             // blocks of 128 a wave has in flight
   __shared__ float sums[WAVES][MT][16][17];
@@ -383,13 +386,16 @@ __global__ __launch_bounds__(kRowWaves * 64) void gemm_fp8_rows_kernel(Fp8Args a
   const int64_t nr = n0 + r16 < a.n ? n0 + r16 : a.n - 1;
   const uint8_t* pb = a.b + (w * a.n + nr) * a.kp + part * 16;
   const uint8_t* psb = a.sb + (w * a.n + nr) * a.ks;
+  constexpr bool RAW = !std::is_void<E>::value;
+  extern __shared__ __attribute__((aligned(16))) uint8_t rows8[];          // RAW: [m][kp + 16] numbers, then [m][blocks] scales
+  uint8_t* scales8 = rows8 + a.m * (a.kp + 16);
   const uint8_t* pa[MT];
   const uint8_t* psa[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const int64_t mr = i * 16 + r16 < a.m ? i * 16 + r16 : a.m - 1;
-    pa[i] = a.a + (w * a.m + mr) * a.kp + part * 16;
-    psa[i] = a.sa + (w * a.m + mr) * a.ks;
+    pa[i] = RAW ? rows8 + mr * (a.kp + 16) + part * 16 : a.a + (w * a.m + mr) * a.kp + part * 16;
+    psa[i] = RAW ? scales8 + mr * blocks : a.sa + (w * a.m + mr) * a.ks;
   }
   struct Piece { uint4 lo, hi; int scale; };
   auto read = [](const uint8_t* row, const uint8_t* scales, int b) {
@@ -422,16 +428,37 @@ __global__ __launch_bounds__(kRowWaves * 64) void gemm_fp8_rows_kernel(Fp8Args a
     }
   };
   // AHEAD blocks at a time, all of their loads before the first product: nothing else hides what a load takes
-  for (int b = wave; b < blocks; b += AHEAD * WAVES) {
+  for (int b = wave; b < blocks || (RAW && b == wave); b += AHEAD * WAVES) {
     Piece y[AHEAD], x[AHEAD][MT];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
+    for (int u = 0; u < AHEAD; ++u)
+      if (b + u * WAVES < blocks) y[u] = read(pb, psb, b + u * WAVES);
+    if constexpr (RAW) {
+      if (b == wave) {                                       // once, and every wave comes by
+        const typename E::T* rows = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
+        const int per_row = blocks * 16, all = (int)a.m * per_row, t = threadIdx.x & 15;
+        for (int e = threadIdx.x; e < all; e += WAVES * 64) {               // 16 lanes a block of 128
+          const int m = e / per_row, blk = (e - m * per_row) >> 4;
+          Raw8<E> raw;
+          float f[8];
+          raw.load(rows + m * a.x.ld, (int64_t)blk * BK + t * 8, a.contraction);
+          raw.floats(f);
+          uint32_t top = 0;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) top = larger(top, magnitude(f[j]));
+          const Scale s = scale_of(largest_of_16(top));
+          *reinterpret_cast<uint2*>(rows8 + m * (a.kp + 16) + blk * BK + t * 8) = to_e4m3(f, s.inverse);
+          if (t == 0) scales8[m * blocks + blk] = (uint8_t)s.byte;
+        }
+        __syncthreads();
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
       if (b + u * WAVES < blocks) {
-        y[u] = read(pb, psb, b + u * WAVES);
 #pragma unroll
         for (int i = 0; i < MT; ++i) x[u][i] = read(pa[i], psa[i], b + u * WAVES);
       }
-    }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
       if (b + u * WAVES < blocks) multiply(y[u], x[u]);
@@ -456,8 +483,18 @@ __global__ __launch_bounds__(kRowWaves * 64) void gemm_fp8_rows_kernel(Fp8Args a
 template <int MT>
 hipError_t launch_rows(const Fp8Args& a, hipStream_t s) {
   const dim3 grid((unsigned)ceil_div(a.n, 16), (unsigned)a.k), block(kRowWaves * 64);
-  if (a.dtype == DW_F32) hipLaunchKernelGGL((gemm_fp8_rows_kernel<MT, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((gemm_fp8_rows_kernel<MT, false>), grid, block, 0, s, a);
+  if (a.dtype == DW_F32) hipLaunchKernelGGL((gemm_fp8_rows_kernel<MT, true, void>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((gemm_fp8_rows_kernel<MT, false, void>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+// Quantised on the way: up to 16 rows whose numbers fill at most 16 KB, as every block goes through all of them (us, against
+// a launch of its own: 4096 x 4096, m = 1: 5.4, 7.7; m = 4: 7.0, 8.2; m = 8: 9.3, 8.5; 256 x 1024, m = 16: 4.4, 4.9)
+constexpr int64_t kFusedRows = 16, kFusedBytes = 16384;
+template <bool EXACT, class E>
+hipError_t launch_fused(const Fp8Args& a, hipStream_t s) {
+  const size_t lds = (size_t)(a.m * (a.kp + 16) + a.m * (a.kp / BK));
+  hipLaunchKernelGGL((gemm_fp8_rows_kernel<1, EXACT, E>), dim3((unsigned)ceil_div(a.n, 16), (unsigned)a.k), dim3(kRowWaves * 64), lds, s, a);
   return hipGetLastError();
 }
 
@@ -544,6 +581,14 @@ int slices_of(int k, int64_t m, int64_t n, int64_t blocks) {
 size_t fp8_scratch_bytes(int k, int64_t m, int64_t n, int64_t kp) {
   const int s = fp8::rows_kernel(k, m, n, kp) ? 1 : fp8::slices_of(k, m, n, kp / fp8::BK);
   return s > 1 ? (size_t)s * k * m * n * sizeof(float) : 0;
+}
+
+bool fp8_linear_fused(int k, int64_t m, int64_t n, int64_t kp) {
+  return kp > 0 && m <= fp8::kFusedRows && m * kp <= fp8::kFusedBytes && fp8::rows_kernel(k, m, n, kp);
+}
+
+hipError_t launch_fp8_linear_fused(const Fp8Args& a, hipStream_t s) {
+  return a.dtype == DW_F32 ? fp8::launch_fused<true, F32>(a, s) : fp8::launch_fused<false, Bf16>(a, s);
 }
 
 hipError_t launch_fp8_matmul(const Fp8Args& a_, hipStream_t s) {

@@ -267,9 +267,12 @@ struct Fp8Args {
   void* c; int64_t ldc, c_stride;
   int k, dtype;
   int64_t m, n, kp, ks;                                    // kp: padded contraction; ks: scale bytes of a row
+  Rows x; int64_t contraction;                             // p != nullptr: operand a is x, to be quantised on the way (type: dtype)
   float* part; int slice_blocks;                           // slices of the contraction: [slices][k][m][n], blocks of 128 each
 };
 size_t fp8_scratch_bytes(int k, int64_t m, int64_t n, int64_t kp);
 hipError_t launch_fp8_matmul(const Fp8Args& a, hipStream_t s);
+bool fp8_linear_fused(int k, int64_t m, int64_t n, int64_t kp);
+hipError_t launch_fp8_linear_fused(const Fp8Args& a, hipStream_t s);
 
 }  // namespace dw

@@ -36,6 +36,8 @@ inline bool norm_shape_ok(int k, int64_t rows, int64_t n) {
   return rows >= 0 && rows < kMaxRows && n >= 1 && n <= DW_MAX_NORM;
 }
 
+inline bool fp8_product_fits(int k, int64_t m, int64_t n) { return ceil_div(m, 64) * ceil_div(n, 64) * k <= (1 << 22); }   // one grid
+
 struct ClipSizes { int64_t elements, chunk; int parts; };   // of one worker
 int clip_sizes(int k, int n_tensors, const int64_t* h_count, ClipSizes* z) {
   if (k < 1 || k > DW_MAX_K) return DW_ERR_CONFIG;
@@ -256,7 +258,7 @@ int dw_fp8_matmul(const uint8_t* d_a, const uint8_t* d_a_scale, const uint8_t* d
   if (!d_c || (contraction > 0 && (!d_a || !d_a_scale || !d_b || !d_b_scale))) return DW_ERR_NULL;
   if (!aligned(d_a, 16) || !aligned(d_b, 16) || !aligned(d_a_scale, 4) || !aligned(d_b_scale, 4)) return DW_ERR_ARG;
   if (!params_ok(d_bias, bias_stride) || !out_ok(d_c, c_ld, c_stride, k, m, n, type_bytes(dtype))) return DW_ERR_ARG;
-  if (ceil_div(m, 64) * ceil_div(n, 64) * k > (1 << 22)) return DW_ERR_TOO_LARGE;
+  if (!fp8_product_fits(k, m, n)) return DW_ERR_TOO_LARGE;
   const size_t need = dw_fp8_matmul_scratch_bytes(k, m, n, contraction);
   if (need > 0 && (!d_scratch || !aligned(d_scratch, 256) || scratch_bytes < need)) return DW_ERR_WORKSPACE;
   Fp8Args a = {};
@@ -268,6 +270,49 @@ int dw_fp8_matmul(const uint8_t* d_a, const uint8_t* d_a_scale, const uint8_t* d
   a.part = static_cast<float*>(d_scratch);
   DW_HIP(launch_fp8_matmul(a, (hipStream_t)stream));
   return DW_OK;
+}
+
+// scratch of dw_fp8_linear: x in 8 bits and its scales, and what the product needs; nothing where it is quantised on the way
+static int64_t linear_q_bytes(int k, int64_t m, int64_t contraction) { return ceil_div(k * m * DW_FP8_ROW(contraction), 256) * 256; }
+static int64_t linear_scale_bytes(int k, int64_t m, int64_t contraction) { return ceil_div(k * m * DW_FP8_SCALES(contraction), 256) * 256; }
+
+size_t dw_fp8_linear_scratch_bytes(int k, int64_t m, int64_t n, int64_t contraction) {
+  if (k < 1 || k > DW_MAX_K || m < 1 || m > DW_MAX_FP8 || n < 1 || n > DW_MAX_FP8 || contraction < 1 || contraction > DW_MAX_FP8) return 0;
+  if (fp8_linear_fused(k, m, n, DW_FP8_ROW(contraction))) return 0;
+  return (size_t)(linear_q_bytes(k, m, contraction) + linear_scale_bytes(k, m, contraction)) + dw_fp8_matmul_scratch_bytes(k, m, n, contraction);
+}
+
+int dw_fp8_linear(const void* d_x, int64_t x_ld, int64_t x_stride, const uint8_t* d_w, const uint8_t* d_w_scale, const float* d_bias,
+                  int64_t bias_stride, int k, int64_t m, int64_t n, int64_t contraction, int dtype, void* d_y, int64_t y_ld,
+                  int64_t y_stride, void* d_scratch, size_t scratch_bytes, void* stream) {
+  if (k < 1 || k > DW_MAX_K || !is_type(dtype)) return DW_ERR_CONFIG;
+  if (m < 0 || m > DW_MAX_FP8 || n < 1 || n > DW_MAX_FP8 || contraction < 1 || contraction > DW_MAX_FP8) return DW_ERR_ARG;
+  if (m == 0) return DW_OK;
+  if (!d_x || !d_w || !d_w_scale || !d_y) return DW_ERR_NULL;
+  const int64_t b = type_bytes(dtype);
+  if (!in_ok(d_x, x_ld, x_stride, m, contraction, b) || !aligned(d_w, 16) || !aligned(d_w_scale, 4)) return DW_ERR_ARG;
+  if (!params_ok(d_bias, bias_stride) || !out_ok(d_y, y_ld, y_stride, k, m, n, b)) return DW_ERR_ARG;
+  if (!fp8_product_fits(k, m, n)) return DW_ERR_TOO_LARGE;
+  const size_t need = dw_fp8_linear_scratch_bytes(k, m, n, contraction);
+  if (need > 0 && (!d_scratch || !aligned(d_scratch, 256) || scratch_bytes < need)) return DW_ERR_WORKSPACE;
+  if (need == 0) {
+    Fp8Args a = {};
+    a.x = {d_x, x_ld, x_stride}; a.contraction = contraction;
+    a.b = d_w; a.sb = d_w_scale;
+    a.bias = d_bias; a.bias_stride = bias_stride;
+    a.c = d_y; a.ldc = y_ld; a.c_stride = y_stride;
+    a.k = k; a.dtype = dtype; a.m = m; a.n = n;
+    a.kp = DW_FP8_ROW(contraction); a.ks = DW_FP8_SCALES(contraction);
+    DW_HIP(launch_fp8_linear_fused(a, (hipStream_t)stream));
+    return DW_OK;
+  }
+  uint8_t* q = static_cast<uint8_t*>(d_scratch);
+  uint8_t* scale = q + linear_q_bytes(k, m, contraction);
+  uint8_t* rest = scale + linear_scale_bytes(k, m, contraction);
+  const int st = dw_fp8_quantize(d_x, x_ld, x_stride, k, m, contraction, dtype, 0, q, scale, nullptr, nullptr, stream);
+  if (st != DW_OK) return st;
+  return dw_fp8_matmul(q, scale, d_w, d_w_scale, d_bias, bias_stride, k, m, n, contraction, dtype, d_y, y_ld, y_stride, rest,
+                       scratch_bytes - (size_t)(rest - q), stream);
 }
 
 }  // extern "C"

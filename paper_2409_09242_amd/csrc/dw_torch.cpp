@@ -325,27 +325,21 @@ Eight make_eight(int64_t k, int64_t rows, int64_t n, at::Device device) {
 }
 uint8_t* bytes(const at::Tensor& t) { return t.defined() ? static_cast<uint8_t*>(t.data_ptr()) : nullptr; }
 
-void quantize(const at::Tensor& x, bool square, const Eight& m, const Eight& t, void* stream) {
-  const int type = type_of(x, "x");
-  const Matrix mx = matrix(x, "x");
-  check(dw_fp8_quantize(mx.p, mx.ld, mx.stride, workers_of(x.size(0)), x.size(1), x.size(2), type, square ? 1 : 0, bytes(m.q), bytes(m.scale),
-                        bytes(t.q), bytes(t.scale), stream),
-        "dw_fp8_quantize");
-}
-
 // x, square, transposed -> (q, scale) or (q, scale, qt, scale_t)
 PyObject* fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   expect(n_args, 3);
   const at::Tensor& x = tensor(a[0], "x");
-  type_of(x, "x");
-  matrix(x, "x");
+  const int type = type_of(x, "x");
+  const Matrix mx = matrix(x, "x");
   On on(x);
   const int64_t k = x.size(0), rows = x.size(1), n = x.size(2);
   const Eight m = make_eight(k, rows, n, x.device());
   Eight t;
   if (a[2] == Py_True) t = make_eight(k, n, rows, x.device());
-  quantize(x, a[1] == Py_True, m, t, on.stream);
+  check(dw_fp8_quantize(mx.p, mx.ld, mx.stride, workers_of(k), rows, n, type, a[1] == Py_True ? 1 : 0, bytes(m.q), bytes(m.scale), bytes(t.q),
+                        bytes(t.scale), on.stream),
+        "dw_fp8_quantize");
   if (t.q.defined()) return tuple(wrap(m.q), wrap(m.scale), wrap(t.q), wrap(t.scale));
   return tuple(wrap(m.q), wrap(m.scale));
   END_HANDLE_TH_ERRORS
@@ -361,21 +355,6 @@ Eight operand(PyObject* q, PyObject* scale, int64_t n, const char* name) {
   return e;
 }
 
-at::Tensor product(const Eight& x, const Eight& w, int64_t n, PyObject* bias, PyObject* out, at::ScalarType type, void* stream) {
-  const at::Device device = x.q.device();
-  const int64_t k = x.q.size(0), m = x.q.size(1), rows = w.q.size(1);
-  TORCH_CHECK_VALUE(w.q.size(0) == k && w.q.device() == device, "operands of ", k, " workers on ", device, " and ", w.q.size(0), " on ", w.q.device());
-  const Param b = param(maybe(bias, "bias"), "bias", k, rows, device);
-  const at::Tensor c = out == Py_None ? make({k, m, rows}, type, device) : tensor(out, "out");
-  const int code = type_of(c, "out");
-  const Matrix mc = matrix_like(c, "out", {k, m, rows}, c.scalar_type(), device);
-  const Scratch scratch(dw_fp8_matmul_scratch_bytes(workers_of(k), m, rows, n), device);
-  check(dw_fp8_matmul(bytes(x.q), bytes(x.scale), bytes(w.q), bytes(w.scale), b.p, b.stride, workers_of(k), m, rows, n, code, mc.p, mc.ld,
-                      mc.stride, scratch.p, scratch.bytes, stream),
-        "dw_fp8_matmul");
-  return c;
-}
-
 // a's numbers, scales, row length, b's, bias, out, bf16 -> c
 PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
@@ -384,7 +363,18 @@ PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   TORCH_CHECK_VALUE(n == whole(a[5]), "operands with rows of ", n, " and ", whole(a[5]));
   const Eight x = operand(a[0], a[1], n, "a"), w = operand(a[3], a[4], n, "b");
   On on(x.q);
-  return wrap(product(x, w, n, a[6], a[7], a[8] == Py_True ? at::kBFloat16 : at::kFloat, on.stream));
+  const at::Device device = x.q.device();
+  const int64_t k = x.q.size(0), m = x.q.size(1), rows = w.q.size(1);
+  TORCH_CHECK_VALUE(w.q.size(0) == k && w.q.device() == device, "operands of ", k, " workers on ", device, " and ", w.q.size(0), " on ", w.q.device());
+  const Param b = param(maybe(a[6], "bias"), "bias", k, rows, device);
+  const at::Tensor c = a[7] == Py_None ? make({k, m, rows}, a[8] == Py_True ? at::kBFloat16 : at::kFloat, device) : tensor(a[7], "out");
+  const int code = type_of(c, "out");
+  const Matrix mc = matrix_like(c, "out", {k, m, rows}, c.scalar_type(), device);
+  const Scratch scratch(dw_fp8_matmul_scratch_bytes(workers_of(k), m, rows, n), device);
+  check(dw_fp8_matmul(bytes(x.q), bytes(x.scale), bytes(w.q), bytes(w.scale), b.p, b.stride, workers_of(k), m, rows, n, code, mc.p, mc.ld,
+                      mc.stride, scratch.p, scratch.bytes, on.stream),
+        "dw_fp8_matmul");
+  return wrap(c);
   END_HANDLE_TH_ERRORS
 }
 
@@ -393,14 +383,23 @@ PyObject* fp8_linear(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   expect(n_args, 6);
   const at::Tensor& x = tensor(a[0], "x");
-  type_of(x, "x");
-  matrix(x, "x");
+  const int type = type_of(x, "x");
+  const Matrix mx = matrix(x, "x");
   On on(x);
-  const int64_t n = whole(a[3]);
+  const at::Device device = x.device();
+  const int64_t n = whole(a[3]), k = x.size(0), m = x.size(1);
   TORCH_CHECK_VALUE(x.size(2) == n, "x has rows of ", x.size(2), ", the weight of ", n);
-  const Eight w = operand(a[1], a[2], n, "the weight"), e = make_eight(x.size(0), x.size(1), n, x.device());
-  quantize(x, false, e, Eight{}, on.stream);
-  return wrap(product(e, w, n, a[4], a[5], x.scalar_type(), on.stream));
+  const Eight w = operand(a[1], a[2], n, "the weight");
+  const int64_t rows = w.q.size(1);
+  TORCH_CHECK_VALUE(w.q.size(0) == k && w.q.device() == device, "x of ", k, " workers on ", device, ", a weight of ", w.q.size(0), " on ", w.q.device());
+  const Param b = param(maybe(a[4], "bias"), "bias", k, rows, device);
+  const at::Tensor y = a[5] == Py_None ? make({k, m, rows}, x.scalar_type(), device) : tensor(a[5], "out");
+  const Matrix my = matrix_like(y, "out", {k, m, rows}, x.scalar_type(), device);
+  const Scratch scratch(dw_fp8_linear_scratch_bytes(workers_of(k), m, rows, n), device);
+  check(dw_fp8_linear(mx.p, mx.ld, mx.stride, bytes(w.q), bytes(w.scale), b.p, b.stride, workers_of(k), m, rows, n, type, my.p, my.ld, my.stride,
+                      scratch.p, scratch.bytes, on.stream),
+        "dw_fp8_linear");
+  return wrap(y);
   END_HANDLE_TH_ERRORS
 }
 

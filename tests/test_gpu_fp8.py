@@ -191,6 +191,27 @@ def test_a_linear_layer_and_its_gradients(dtype):
         within(got, want, bound + out_rounding(got.dtype) * (want.abs() + bound), "linear")
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(1, 1, 64, 128), (1, 1, 4096, 4096), (2, 3, 100, 131), (3, 16, 50, 1000), (1, 5, 17, 7), (2, 9, 300, 2050),
+                                   (1, 17, 64, 300), (2, 100, 130, 500), (1, 4, 96, 9000)])
+def test_a_linear_layer_quantises_on_the_way(shape, dtype):
+    """With few rows in one launch: the same bits as quantiser and product, from any view of x."""
+    k, m, n, length = shape
+    g = _gen(m + length)
+    wq = OPS.fp8_quantize(padded((k, n, length), 0, 0, F32, g), square=True)
+    bias = torch.randn(k, n, generator=g, device=DEV)
+    for pad, lead in ((0, 0), (3, 1)):
+        x = padded((k, m, length), pad, lead, dtype, g, 2.0)
+        x[:, m // 2, :200] = 0
+        out = torch.full((k, m, n + 2), 7.0, dtype=dtype, device=DEV)
+        y = OPS.fp8_linear(x, wq, bias, out=out[..., 1:n + 1])
+        assert torch.equal(y, OPS.fp8_matmul(OPS.fp8_quantize(x), wq, bias, dtype=dtype))
+        assert bool((out[..., 0] == 7).all()) and bool((out[..., -1] == 7).all())
+    x[0, 0, length - 1] = float("nan")
+    y = OPS.fp8_linear(x, wq)
+    assert bool(y[0, 0].isnan().all()) and not bool(y[0, 1:].isnan().any())
+
+
 def test_results_do_not_change_and_other_workers_do_not_matter():
     g = _gen(11)
     a, b = padded((3, 70, 900), 0, 0, BF16, g), padded((3, 300, 900), 0, 0, BF16, g)

@@ -24,7 +24,7 @@ def test_binding_declares_as_many_arguments_as_the_header():
         if name.startswith(("dw_layer", "dw_token", "dw_policy", "dw_clip", "dw_fp8")):
             assert len(getattr(lib, name).argtypes) == want, name
             seen += 1
-    assert seen == 11
+    assert seen == 13
 
 
 def _norm(**kw):
@@ -138,6 +138,19 @@ def test_fp8_matmul(kw, status):
              stream=None)
     a.update(kw)
     assert B.lib().dw_fp8_matmul(*a.values()) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(k=0), CONFIG), (dict(dtype=5), CONFIG), (dict(m=-1), ARG), (dict(length=0), ARG), (dict(x=None), NULL), (dict(w=None), NULL),
+    (dict(sw=None), NULL), (dict(y=None), NULL), (dict(x=P + 2), ARG), (dict(w=P + 8), ARG), (dict(x_ld=255), ARG), (dict(y_ld=99), ARG),
+    (dict(scratch=None), WORKSPACE), (dict(bytes=100), WORKSPACE), (dict(m=0), 0),
+])
+def test_fp8_linear(kw, status):
+    a = dict(x=P, x_ld=256, x_st=25600, w=P, sw=P, bias=None, b_st=100, k=2, m=100, n=100, length=256, dtype=0, y=P, y_ld=100, y_st=10000,
+             scratch=P, bytes=1 << 20, stream=None)
+    a.update(kw)
+    assert B.lib().dw_fp8_linear(*a.values()) == status
+    assert B.lib().dw_fp8_linear_scratch_bytes(1, 1, 4096, 4096) == 0 and B.lib().dw_fp8_linear_scratch_bytes(2, 100, 100, 256) >= 2 * 100 * 260
 
 
 def test_wrappers_want_tensors_on_a_gpu():
