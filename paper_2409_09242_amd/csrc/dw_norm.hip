@@ -40,7 +40,7 @@ struct RowRegs {
   __device__ __forceinline__ void load(const typename E::T* row, const Split<E, TPR>& s, int t) {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      if (i * TPR + t < s.whole) load_piece<E>(row + (i * TPR + t) * E::V, piece[i]);
+      if (i * TPR + t < s.whole) load_piece<E>(at_piece<E>(row, i * TPR + t), piece[i]);
       else
 #pragma unroll
         for (int j = 0; j < 4; ++j) piece[i][j] = 0u;
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_kernel(NormArgs a) {
   constexpr int V = E::V, GROUPS = BLOCK / TPR;
   __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)];
   int turn = 0;
-  const int w = blockIdx.y, t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  const int w = blockIdx.y, t = GROUPS == 1 ? threadIdx.x : threadIdx.x % TPR, g = GROUPS == 1 ? 0 : threadIdx.x / TPR;
   const Split<E, TPR> split(a.n, t);
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
   typename E::T* y = reinterpret_cast<typename E::T*>(a.out.p) + w * a.out.stride;
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_kernel(NormArgs a) {
         if constexpr (!FEW) { param(gamma, 1.f, i, ga[i]); param(beta, 0.f, i, be[i]); }
 #pragma unroll
         for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * rstd * ga[i][j] + be[i][j];
-        store_piece<E>(yr + (i * TPR + t) * V, v[i]);
+        store_piece<E>(at_piece<E>(yr, i * TPR + t), v[i]);
       }
     }
     if (split.has_tail) E::put(yr + split.tail, odd_off * rstd * ga_odd + be_odd);
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_grad_kernel(NormArgs a) {
   __shared__ float red[4 * (TPR > 64 ? TPR / 64 : 1)];
   __shared__ float cols[GROUPS > 1 ? GROUPS * (COLS + V) : 1];
   int turn = 0;
-  const int w = blockIdx.y, t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  const int w = blockIdx.y, t = GROUPS == 1 ? threadIdx.x : threadIdx.x % TPR, g = GROUPS == 1 ? 0 : threadIdx.x / TPR;
   const int64_t n = a.n;
   const Split<E, TPR> split(n, t);
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_grad_kernel(NormArgs a) {
           float o[V];
 #pragma unroll
           for (int j = 0; j < V; ++j) o[j] = rstd * (v[i][j] - c1 - h[i][j] * c2);
-          store_piece<E>(out + (i * TPR + t) * V, o);
+          store_piece<E>(at_piece<E>(out, i * TPR + t), o);
         }
       }
       if (split.has_tail) E::put(out + split.tail, rstd * (v_odd - c1 - h_odd * c2));
@@ -396,7 +396,9 @@ __global__ __launch_bounds__(1024) void layer_norm_strips_kernel(NormArgs a) {
 // in up to two pieces each, then up to four of 512 and (WIDE) of 1024; false: too long
 template <bool WIDE, class F>
 bool for_row(int64_t pieces, F f) {
-  if (pieces <= 16) f.template operator()<16, 1>();
+  if (pieces <= 4) f.template operator()<4, 1>();
+  else if (pieces <= 16) f.template operator()<16, 1>();
+  else if (pieces <= 32) f.template operator()<32, 1>();
   else if (pieces <= 64) f.template operator()<64, 1>();
   else if (pieces <= 128) f.template operator()<64, 2>();
   else if (pieces <= 256) f.template operator()<256, 1>();

@@ -74,6 +74,11 @@ __device__ __forceinline__ void store_piece(typename E::T* p, const float (&f)[E
   E::pack(f, v.w);
   *reinterpret_cast<typename E::Raw*>(p) = v;
 }
+// piece q (16 bytes) of a row: a 32-bit offset from the row's address, which may be in scalar registers
+template <class E, class T>
+__device__ __forceinline__ T* at_piece(T* row, int q) {
+  return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + (uint32_t)q * 16u);
+}
 // the same for data that streams through once and must not displace what is read again
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));

@@ -5,10 +5,15 @@
 //   l' = (0 where the clipped term is the smaller, else -q A) + beta (1 - exp(ref - lp)),
 //   dz_j = w l' ([j = y] - softmax(z)_j)
 //
-// TPR threads share a row and keep its logits in registers as they came (16-byte pieces, ITEMS a thread), so they are read
-// once: the maximum, the sum of exponentials and the gradient all come from there.  Vocabularies beyond 16 pieces of each
-// of 1024 threads read the rest of the row again, from the caches.  Sums over a row are in fp32 (at most 128 terms of a thread,
-// then a tree); the rows' losses go to scratch and a second kernel adds a worker's up in 64 bits in a fixed order.
+// TPR threads share a row, how many follows from the vocabulary alone.  One pass finds the maximum and the sum of exponentials
+// together: a thread keeps both for the pieces (16 bytes) it has seen, the sum relative to its maximum, and the threads'
+// are joined at the end.  For the gradient the pieces stay in registers as they came, so logits are read once; past 16 pieces
+// of each of 1024 threads the rest of the row is read again, from the caches.  Log probabilities alone (no gradient) need no
+// registers for the row, and are the same bits: the same pieces in the same order.  Bound by memory; with the whole row in the
+// registers of one compute unit a block's loads and stores take turns, so rows are shared among as few threads as hold them.
+//
+// Sums over a row are in fp32 (of a thread at most 16 pieces' sums, then a tree); the rows' losses go to scratch and a second kernel
+// adds a worker's up in 64 bits in a fixed order.
 #include "dw_ops.h"
 
 namespace dw {
@@ -34,24 +39,44 @@ __device__ __forceinline__ float row_max(float x, float* lds, int& turn) {
   return x;
 }
 
-// the packed logits are what stays in registers from one pass over them to the next, not their unpacked values
-template <int ITEMS>
-__device__ __forceinline__ void unpack_anew(uint32_t (&raw)[ITEMS][4]) {
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) asm volatile("" : "+v"(raw[i][0]), "+v"(raw[i][1]), "+v"(raw[i][2]), "+v"(raw[i][3]));
-}
-// a thread with 16 pieces has registers for them and for a few values more: its pieces are worked on one at a time
-template <int ITEMS>
-__device__ __forceinline__ void keep_order() {
-  if constexpr (ITEMS >= 16) __builtin_amdgcn_sched_barrier(0);
+// A piece is unpacked where it is worked on, once what came before it is done (`x`, `y`: what that left): all pieces' unpacked
+// values at once, or kept for the second pass, would take twice the registers of the packed ones in bf16.
+__device__ __forceinline__ void in_turn(uint32_t (&piece)[4], float& x, float& y) {
+  asm volatile("" : "+v"(piece[0]), "+v"(piece[1]), "+v"(piece[2]), "+v"(piece[3]), "+v"(x), "+v"(y));
 }
 
+// a maximum to subtract: of -inf alone nothing, so that the sum stays zero (while a NaN, which no maximum takes, shows in it)
+__device__ __forceinline__ float base_of(float m) { return m == -__builtin_huge_valf() ? 0.f : m; }
+
+// the largest of what a thread has seen and the sum of exponentials relative to it
+struct Running {
+  float m = -__builtin_huge_valf(), s = 0.f;
+  template <int V>
+  __device__ __forceinline__ void add(const float (&f)[V]) {
+    float top = f[0];
+#pragma unroll
+    for (int j = 1; j < V; ++j) top = fmaxf(top, f[j]);
+    top = fmaxf(top, m);
+    const float base = base_of(top);
+    float e[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) e[j] = exp_fast(f[j] - base);
+#pragma unroll
+    for (int h = V / 2; h > 0; h /= 2)
+#pragma unroll
+      for (int j = 0; j < h; ++j) e[j] += e[j + h];
+    s = __builtin_fmaf(s, exp_fast(m - base), e[0]);         // (nothing new: times 1 plus 0)
+    m = top;
+  }
+};
+
 template <class E, int TPR, int ITEMS, int BLOCK, bool LONG, bool GRAD>
-__global__ __launch_bounds__(BLOCK) void policy_rows_kernel(PolicyArgs a) {
+__global__ __launch_bounds__(BLOCK, (GRAD && ITEMS >= 16 ? 4 : 1)) void policy_rows_kernel(PolicyArgs a) {      // (waves a SIMD)
   constexpr int V = E::V, GROUPS = BLOCK / TPR;
   __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)];
   int turn = 0;
-  const int w = blockIdx.y, t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  // (one group a block: everything about the row is uniform)
+  const int w = blockIdx.y, t = GROUPS == 1 ? threadIdx.x : threadIdx.x % TPR, g = GROUPS == 1 ? 0 : threadIdx.x / TPR;
   const float ninf = -__builtin_huge_valf();
   // piece i of a thread is piece i * TPR + t of the row's whole ones; what is left of the row (fewer than V elements) goes
   // to the first threads, one each.  A thread without one holds -inf in its place, which changes neither maximum nor sum
@@ -69,52 +94,43 @@ __global__ __launch_bounds__(BLOCK) void policy_rows_kernel(PolicyArgs a) {
     if (y >= 0 && y < (int)a.vocab && weight != 0.f) {      // the same for all threads of the row
       zy = E::one(z + y);
       if (has_tail) zt = E::one(z + tail);
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        if (i * TPR + t < whole) {
-          load_piece<E>(z + (int64_t)(i * TPR + t) * V, raw[i]);
+      Running run;
+      auto take = [&](int i, int q) {                       // piece q into place i
+        if (q < whole) {
+          load_piece<E>(at_piece<E>(z, q), raw[i]);
         } else {
 #pragma unroll
           for (int j = 0; j < 4; ++j) raw[i][j] = E::kMinusInf;
         }
-      }
-      float m = zt;
-      auto highest = [&](const uint32_t (&piece)[4]) {
-        float f[V];
-        E::unpack(piece, f);
-#pragma unroll
-        for (int j = 0; j < V; ++j) m = fmaxf(m, f[j]);
       };
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) { highest(raw[i]); keep_order<ITEMS>(); }
-      if constexpr (LONG) {
-        for (int q = ITEMS * TPR + t; q < whole; q += TPR) {
-          uint32_t more[4];
-          load_piece<E>(z + (int64_t)q * V, more);
-          highest(more);
-        }
-      }
-      m = row_max<TPR>(m, red, turn);
-      unpack_anew(raw);
-      top = m == ninf ? 0.f : m;                            // a row of -inf: the sum stays zero, while a NaN shows in it
-      float sum = exp_fast(zt - top);
       auto add = [&](const uint32_t (&piece)[4]) {
         float f[V];
         E::unpack(piece, f);
-#pragma unroll
-        for (int j = 0; j < V; ++j) sum += exp_fast(f[j] - top);
+        run.add(f);
       };
+      // the gradient's pieces, or (none is wanted) all of them, ITEMS at a time
+      int q0 = t;
+      do {
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i) { add(raw[i]); keep_order<ITEMS>(); }
-      if constexpr (LONG) {
-        for (int q = ITEMS * TPR + t; q < whole; q += TPR) {
+        for (int i = 0; i < ITEMS; ++i) take(i, q0 + i * TPR);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          in_turn(raw[i], run.m, run.s);
+          add(raw[i]);
+        }
+        q0 += ITEMS * TPR;
+      } while (!GRAD && q0 - t < whole);
+      if constexpr (GRAD && LONG) {
+        for (int q = q0; q < whole; q += TPR) {
           uint32_t more[4];
-          load_piece<E>(z + (int64_t)q * V, more);
+          load_piece<E>(at_piece<E>(z, q), more);
           add(more);
         }
       }
-      sum = row_sum<TPR>(sum, red, turn);
-      if constexpr (GRAD) unpack_anew(raw);
+      const float one_more[1] = {zt};
+      run.add(one_more);
+      top = base_of(row_max<TPR>(run.m, red, turn));
+      const float sum = row_sum<TPR>(run.s * exp_fast(run.m - top), red, turn);
       if (sum == 0.f) {                                     // nothing can be chosen: no loss and no gradient
         logp = ninf;
       } else {
@@ -147,17 +163,17 @@ __global__ __launch_bounds__(BLOCK) void policy_rows_kernel(PolicyArgs a) {
           E::unpack(piece, f);
 #pragma unroll
           for (int j = 0; j < V; ++j) f[j] = scale * exp_fast(f[j] - top);
-          store_piece_once<E>(out + (int64_t)q * V, f);
+          store_piece_once<E>(at_piece<E>(out, q), f);
         };
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
+          in_turn(raw[i], scale, top);
           if (i * TPR + t < whole) put(raw[i], i * TPR + t);
-          keep_order<ITEMS>();
         }
         if constexpr (LONG) {
           for (int q = ITEMS * TPR + t; q < whole; q += TPR) {
             uint32_t more[4];
-            load_piece<E>(z + (int64_t)q * V, more);
+            load_piece<E>(at_piece<E>(z, q), more);
             put(more, q);
           }
         }
@@ -168,47 +184,53 @@ __global__ __launch_bounds__(BLOCK) void policy_rows_kernel(PolicyArgs a) {
         float f[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = 0.f;
-        for (int q = t; q < whole; q += TPR) store_piece_once<E>(out + (int64_t)q * V, f);
+        for (int q = t; q < whole; q += TPR) store_piece_once<E>(at_piece<E>(out, q), f);
         if (has_tail) E::put(out + tail, 0.f);
       }
     }
   }
 }
 
-__global__ __launch_bounds__(256) void policy_sum_kernel(const float* part, float* loss, int64_t rows) {
-  __shared__ double waves[4];
+__global__ __launch_bounds__(1024) void policy_sum_kernel(const float* part, float* loss, int64_t rows) {
+  __shared__ double waves[16];
   const float* p = part + (int64_t)blockIdx.x * rows;
   double s = 0.0;
-  for (int64_t r = threadIdx.x; r < rows; r += 256) s += (double)p[r];
+#pragma unroll 4
+  for (int64_t r = threadIdx.x; r < rows; r += 1024) s += (double)p[r];
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) s += __shfl_xor(s, off);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) loss[blockIdx.x] = (float)((waves[0] + waves[1]) + (waves[2] + waves[3]));
+  if (threadIdx.x >= 64) return;
+  s = threadIdx.x < 16 ? waves[threadIdx.x] : 0.0;
+#pragma unroll
+  for (int off = 1; off < 16; off <<= 1) s += __shfl_xor(s, off);
+  if (threadIdx.x == 0) loss[blockIdx.x] = (float)s;
 }
 
-template <class E, int TPR, int ITEMS, int BLOCK, bool LONG>
+// ITEMS: pieces of a thread that the gradient keeps; log probabilities alone take up to eight at a time
+template <class E, int TPR, int ITEMS, bool LONG>
 hipError_t rows_of(const PolicyArgs& a, hipStream_t s) {
+  constexpr int BLOCK = TPR < 256 ? 256 : TPR;
   int64_t blocks = ceil_div(a.rows, BLOCK / TPR);
   if (blocks > 65536) blocks = 65536;
   const dim3 grid((unsigned)blocks, (unsigned)a.k);
   if (a.grad.p) hipLaunchKernelGGL((policy_rows_kernel<E, TPR, ITEMS, BLOCK, LONG, true>), grid, dim3(BLOCK), 0, s, a);
-  else hipLaunchKernelGGL((policy_rows_kernel<E, TPR, ITEMS, BLOCK, LONG, false>), grid, dim3(BLOCK), 0, s, a);
+  else hipLaunchKernelGGL((policy_rows_kernel<E, TPR, (ITEMS < 8 ? ITEMS : 8), BLOCK, false, false>), grid, dim3(BLOCK), 0, s, a);
   return hipGetLastError();
 }
 
-// the fewest threads a row that hold it in few pieces each
 template <class E>
 hipError_t rows_any(const PolicyArgs& a, hipStream_t s) {
   const int64_t pieces = a.vocab / E::V;
-  if (pieces <= 64) return rows_of<E, 64, 1, 256, false>(a, s);
-  if (pieces <= 256) return rows_of<E, 64, 4, 256, false>(a, s);
-  if (pieces <= 1024) return rows_of<E, 256, 4, 256, false>(a, s);
-  if (pieces <= 2048) return rows_of<E, 256, 8, 256, false>(a, s);
-  if (pieces <= 4096) return rows_of<E, 1024, 4, 1024, false>(a, s);
-  if (pieces <= 8192) return rows_of<E, 1024, 8, 1024, false>(a, s);
-  if (pieces <= 16384) return rows_of<E, 1024, 16, 1024, false>(a, s);
-  return rows_of<E, 1024, 16, 1024, true>(a, s);
+  if (pieces <= 64) return rows_of<E, 64, 1, false>(a, s);
+  if (pieces <= 256) return rows_of<E, 64, 4, false>(a, s);
+  if (pieces <= 1024) return rows_of<E, 256, 4, false>(a, s);
+  if (pieces <= 2048) return rows_of<E, 256, 8, false>(a, s);
+  if (pieces <= 4096) return rows_of<E, 512, 8, false>(a, s);
+  if (pieces <= 8192) return rows_of<E, 512, 16, false>(a, s);
+  if (pieces <= 16384) return rows_of<E, 1024, 16, false>(a, s);
+  return rows_of<E, 1024, 16, true>(a, s);
 }
 
 }  // namespace
@@ -219,7 +241,7 @@ hipError_t launch_policy(const PolicyArgs& a, int dtype, hipStream_t s) {
     if (e != hipSuccess || !a.loss) return e;
   }
   if (!a.loss) return hipSuccess;
-  hipLaunchKernelGGL(policy_sum_kernel, dim3((unsigned)a.k), dim3(256), 0, s, a.part, a.loss, a.rows);
+  hipLaunchKernelGGL(policy_sum_kernel, dim3((unsigned)a.k), dim3(1024), 0, s, a.part, a.loss, a.rows);
   return hipGetLastError();
 }
 
