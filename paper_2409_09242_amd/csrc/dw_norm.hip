@@ -17,9 +17,9 @@ namespace dw {
 
 namespace {
 
-// blocks of `groups` rows at a time: enough to fill the chip a few times over, shared among the workers
+// blocks of `groups` rows at a time: `target` of them over all workers at most, so that they run all at once, and one a worker
 inline int64_t blocks_per_worker(int k, int64_t rows, int groups, int64_t target) {
-  const int64_t most = ceil_div(rows, groups), share = ceil_div(target, k);
+  const int64_t most = ceil_div(rows, groups), share = target > k ? target / k : 1;
   return most < share ? most : share;
 }
 
@@ -32,18 +32,22 @@ struct Split {
   __device__ __forceinline__ Split(int64_t n, int t) : whole((int)(n / E::V)), tail(whole * E::V + t), has_tail(tail < (int)n) {}
 };
 
-// ITEMS pieces of a row and its odd element, as they are in memory; what a thread has not reads as zero
-template <class E, int TPR, int ITEMS>
+// ITEMS pieces of a row and its odd element, as they are in memory; what a thread has not reads as zero.  ONCE: with the
+// policy of data that streams through
+template <class E, int TPR, int ITEMS, bool ONCE>
 struct RowRegs {
   uint32_t piece[ITEMS][4];
   float odd;
   __device__ __forceinline__ void load(const typename E::T* row, const Split<E, TPR>& s, int t) {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      if (i * TPR + t < s.whole) load_piece<E>(at_piece<E>(row, i * TPR + t), piece[i]);
-      else
+      if (i * TPR + t < s.whole) {
+        if constexpr (ONCE) load_piece_once<E>(at_piece<E>(row, i * TPR + t), piece[i]);
+        else load_piece<E>(at_piece<E>(row, i * TPR + t), piece[i]);
+      } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) piece[i][j] = 0u;
+      }
     }
     odd = s.has_tail ? E::one(row + s.tail) : 0.f;
   }
@@ -65,7 +69,7 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_kernel(NormArgs a) {
   const int64_t step = (int64_t)gridDim.x * GROUPS;
   // every group of a block goes round the same number of times (the block's barriers are for TPR > 64, where it is one)
   int64_t r = (int64_t)blockIdx.x * GROUPS + g;
-  RowRegs<E, TPR, ITEMS> next;
+  RowRegs<E, TPR, ITEMS, false> next;
   if (r < a.rows) next.load(x + r * a.x.ld, split, t);     // the first row travels along with gamma and beta
   float ga[ITEMS][V], be[ITEMS][V], ga_odd = 1.f, be_odd = 0.f;
   auto param = [&](const float* p, float fill, int i, float (&f)[V]) {
@@ -193,7 +197,9 @@ __global__ __launch_bounds__(BLOCK) void layer_norm_grad_kernel(NormArgs a) {
   const float inv_n = 1.f / (float)n;
   const int64_t step = (int64_t)gridDim.x * GROUPS;
   int64_t r = (int64_t)blockIdx.x * GROUPS + g;
-  RowRegs<E, TPR, ITEMS> next_x, next_dy;
+  // fp32 streams through (8192 x 4096: 74 us, otherwise 84); rows of bf16 share lines with their neighbours more often, which then
+  // come twice (3 x 2731 x 5003: 133 against 113)
+  RowRegs<E, TPR, ITEMS, E::V == 4> next_x, next_dy;
   float next_mean = 0.f, next_rstd = 0.f;
   auto fetch = [&](int64_t row) {
     next_x.load(x + row * a.x.ld, split, t);
@@ -435,8 +441,9 @@ hipError_t fwd_any(const NormArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// blocks of the backward pass: as many as run at a time, so that there are few rows of partial sums
-int64_t grad_blocks(int tpr) { return (tpr >= 1024 ? 1 : tpr == 512 ? 2 : 4) * (int64_t)kCus; }
+// blocks of the backward pass: two a compute unit from 256 threads on, so that there are few rows of partial sums (bf16,
+// 8192 x 4096: 44 us, with four 56)
+int64_t grad_blocks(int tpr) { return (tpr >= 1024 ? 1 : tpr >= 256 ? 2 : 4) * (int64_t)kCus; }
 
 template <class E>
 struct Backward {

@@ -2,7 +2,8 @@
 
 Bounds (U = 2^-24).  With x_j = z_j - max the kernel's exp(x_j) is right to (|x_j| + 3) U, the sum of them goes through at
 most 128 + 1 terms of a thread, 6 steps and 16 waves (a vocabulary past the registers: as many terms more as are read
-again), so log sum is off by (152 + more + mean|x|) U, the mean over the softmax; the rest follows by differentiating."""
+again; a thread that adds its pieces' sums relative to a running maximum has 4 + 3 for each of 16 pieces and 1), so log sum is
+off by (152 + more + mean|x|) U, the mean over the softmax; the rest follows by differentiating."""
 import pytest
 import torch
 
