@@ -602,8 +602,11 @@ hipError_t launch_fp8_matmul(const Fp8Args& a_, hipStream_t s) {
     if (a.m <= 16) return fp8::launch_rows<1>(a, s);
     return a.m <= 32 ? fp8::launch_rows<2>(a, s) : fp8::launch_rows<4>(a, s);
   }
-  if (fp8::tiles_of(a.k, a.m, a.n, 256) >= kCus) return fp8::launch<fp8::Large>(a, s);
-  if (fp8::tiles_of(a.k, a.m, a.n, 128) >= kCus) return fp8::launch<fp8::Middle>(a, s);
+  // Tiles as large as leave most compute units one (us): 4096 x 3328, contraction 1024, 208 tiles of 256: 20.5, in 128s 22.7;
+  // 3000 cubed, 144 of 256: 43, 43 (fp32 71, 65).  2 x 1500 x 700 x 5000, 144 of 128: fp32 39, in 64s 44 (bf16 33, 31);
+  // 4096 x 512 x 4096, 128 of 128: 24 and 32 in fp32, in 64s 22 and 28
+  if (fp8::tiles_of(a.k, a.m, a.n, 256) >= 200) return fp8::launch<fp8::Large>(a, s);
+  if (fp8::tiles_of(a.k, a.m, a.n, 128) >= (a.dtype == DW_F32 ? 144 : 200)) return fp8::launch<fp8::Middle>(a, s);
   const int slices = fp8::slices_of(a.k, a.m, a.n, a.kp / fp8::BK);
   if (slices == 1) return fp8::launch<fp8::Small>(a, s);
   const int words = (int)ceil_div(a.kp / fp8::BK, fp8::GROUP);
