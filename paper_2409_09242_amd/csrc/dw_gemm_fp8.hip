@@ -43,6 +43,13 @@ __device__ __forceinline__ void wait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (0x7 << 4) | (0x0 << 8));
 }
 
+// an index that the compiler takes as it is: it computes what follows from it where that is used and finds the constant parts
+// of addresses, instead of keeping an address per use in registers
+__device__ __forceinline__ int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Each lane's N bytes at base + offset go to LDS at `to` + N * lane; no register receives anything.  Written as assembly
 // because behind the builtin the compiler waits for every load in flight before each read of LDS: it cannot tell that the
 // read is of another stage.  The waits are the kernel's own (wait_vm before the barrier that precedes a stage's reads).
@@ -105,7 +112,11 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   const int logical = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
   const int w = logical / tiles, tile = logical - w * tiles;
   if (w >= a.k) return;
-  const int64_t row0 = (int64_t)(tile % tiles_m) * C::BM, col0 = (int64_t)(tile / tiles_m) * C::BN;
+  // of a worker's tiles eight rows at a time: what a die works on is about as high as wide, and its L2 is read for fewer
+  // rows of a and b (8192 cubed: 433 us with whole columns one after another, 394 so; 4096 x 512 x 4096: 22, 15.3)
+  const int strip = tile / (8 * tiles_n), in_strip = tile - strip * 8 * tiles_n;
+  const int high = tiles_m - strip * 8 < 8 ? tiles_m - strip * 8 : 8;
+  const int64_t row0 = (int64_t)(strip * 8 + in_strip % high) * C::BM, col0 = (int64_t)(in_strip / high) * C::BN;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm0 = (wave % C::WM) * C::WTM * 32, wn0 = (wave / C::WM) * C::WTN * 32;
@@ -127,14 +138,14 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   // uniform base that advances by a block, and a lane's offset from it (a tile's rows span less than 2^32 bytes).
   const bool of_a = wave < C::NW / 2;
   const int first = (of_a ? wave : wave - C::NW / 2) * C::CPW;
-  const int64_t tile0 = of_a ? row0 : col0, all_rows = of_a ? a.m : a.n;
+  const int64_t tile0 = of_a ? row0 : col0, behind = (of_a ? a.m : a.n) - 1 - tile0;
+  const int last = behind < C::BM ? (int)behind : C::BM - 1;
   const uint8_t* base = (of_a ? A : Bm) + tile0 * kp + (int64_t)block0 * BK;
   uint32_t off[C::CPW];
 #pragma unroll
   for (int c = 0; c < C::CPW; ++c) {
     const int row = (first + c) * 8 + (lane >> 3), q = (lane & 7) ^ swizzle(row);
-    const int64_t r = tile0 + row < all_rows ? row : all_rows - 1 - tile0;
-    off[c] = (uint32_t)(r * kp + q * 16);
+    off[c] = (uint32_t)(row < last ? row : last) * (uint32_t)kp + (uint32_t)q * 16;
   }
   // scale words, 64 rows at a time: the same halves
   constexpr int SP = C::BM / 64, SPW = (SP + C::NW / 2 - 1) / (C::NW / 2);
@@ -144,7 +155,7 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
 #pragma unroll
   for (int c = 0; c < SPW; ++c) {
     const int row = (sfirst + c * (C::NW / 2)) * 64 + lane;
-    soff[c] = (uint32_t)((tile0 + row < all_rows ? row : all_rows - 1 - tile0) * a.ks);
+    soff[c] = (uint32_t)(row < last ? row : last) * (uint32_t)a.ks;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char)smem;
   const uint32_t lds_tile = __builtin_amdgcn_readfirstlane(lds0 + (of_a ? 0 : C::A_B) + first * 1024);
@@ -194,11 +205,13 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   };
   int sx[C::WTM], sy[C::WTN], nx[C::WTM], ny[C::WTN];        // scale bytes: of the present block of 128, of the next
   auto read_scales = [&](int blk) {
-    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(smem) + C::OFF_S + ((blk / 4) & 1) * (C::BM + C::BN) * 4 + (blk & 3);
+    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(smem) + C::OFF_S;
+    const int group = ((blk / 4) & 1) * (C::BM + C::BN) * 4 + (blk & 3), lane4 = l32 * 4;
+    const int ox = anew(group + wm0 * 4 + lane4), oy = anew(group + (C::BM + wn0) * 4 + lane4);
 #pragma unroll
-    for (int i = 0; i < C::WTM; ++i) nx[i] = bytes[(wm0 + i * 32 + l32) * 4];
+    for (int i = 0; i < C::WTM; ++i) nx[i] = bytes[ox + i * 128];
 #pragma unroll
-    for (int j = 0; j < C::WTN; ++j) ny[j] = bytes[(C::BM + wn0 + j * 32 + l32) * 4];
+    for (int j = 0; j < C::WTN; ++j) ny[j] = bytes[oy + j * 128];
   };
   auto take_scales = [&]() {
 #pragma unroll
@@ -305,61 +318,57 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
 
   __syncthreads();                                           // the stages are free: each wave stages its rows in its share
   const int64_t rows_left = a.m - row0 - wm0, cols_left = a.n - col0 - wn0;
-  if constexpr (SLICE || EXACT) {
-    constexpr int RS = C::WTN * 128 + 16, LPR = C::WTN * 8, RPP = 64 / LPR;
-    static_assert(C::NW * 32 * RS <= C::OFF_S, "staging fits the stages");
-    char* wl = smem + wave * 32 * RS;
-    float* out = SLICE ? a.part + (((int64_t)blockIdx.y * a.k + w) * a.m + row0 + wm0) * a.n + col0 + wn0
-                       : reinterpret_cast<float*>(a.c) + w * a.c_stride + (row0 + wm0) * a.ldc + col0 + wn0;
-    const int64_t ld = SLICE ? a.n : a.ldc;
+  const int64_t ld = SLICE ? a.n : a.ldc;
+  const int64_t at = SLICE ? (((int64_t)blockIdx.y * a.k + w) * a.m + row0 + wm0) * a.n + col0 + wn0
+                           : w * a.c_stride + (row0 + wm0) * a.ldc + col0 + wn0;
+  // 32 rows of one or two of the tile's 32s at a time: each wave turns them to whole lines in its piece of LDS.  A tile that
+  // lies within C is written without a look at its ends.
+  const bool within = rows_left >= C::WTM * 32 && cols_left >= C::WTN * 32;
+  constexpr int OUT_B = 32 * (128 + 16);                     // of a wave: 32 rows of at most 128 bytes
+  static_assert(C::NW * OUT_B <= C::OFF_S, "staging fits the stages");
+  char* wl = smem + wave * OUT_B;
+  auto write = [&](auto within_) {
+    constexpr bool WITHIN = decltype(within_)::value;
+    constexpr bool F = SLICE || EXACT;
+    constexpr int JS = F || C::WTN < 2 ? 1 : 2, RS = JS * (F ? 128 : 64) + 16, LPR = JS * (F ? 8 : 4), RPP = 64 / LPR, V = F ? 4 : 8;
+    using T = std::conditional_t<F, float, uint16_t>;
+    using E = std::conditional_t<F, F32, Bf16>;
+    const int r0 = lane / LPR, ch = lane % LPR;
+    T* out = reinterpret_cast<T*>(SLICE ? reinterpret_cast<void*>(a.part) : a.c) + at + r0 * ld + ch * V;
 #pragma unroll
-    for (int i = 0; i < C::WTM; ++i) {
+    for (int i = 0; i < C::WTM; ++i)
 #pragma unroll
-      for (int j = 0; j < C::WTN; ++j)
+      for (int j0 = 0; j0 < C::WTN; j0 += JS) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<float4*>(wl + l32 * RS + (j * 32 + g * 8 + half * 4) * 4) =
-              make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+        for (int j = 0; j < JS; ++j) {
+          f32x16& v = acc[i][j0 + j];
 #pragma unroll
-      for (int p = 0; p < 32 / RPP; ++p) {
-        const int row = p * RPP + lane / LPR, ch = lane % LPR;
-        const float4 v = *reinterpret_cast<const float4*>(wl + row * RS + ch * 16);
-        if (i * 32 + row < rows_left) {
-          const float f[4] = {v.x, v.y, v.z, v.w};
-          store16<F32>(out + (i * 32 + row) * ld, ch * 4, cols_left, f);
+          for (int g = 0; g < 4; ++g) {
+            char* to = wl + l32 * RS + (j * 32 + g * 8 + half * 4) * (int)sizeof(T);
+            if constexpr (F) *reinterpret_cast<float4*>(to) = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+            else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(v[4 * g], v[4 * g + 1]), pack_bf16(v[4 * g + 2], v[4 * g + 3]));
+          }
         }
-      }
-    }
-  } else {
-    constexpr int RS = C::WTN * 64 + 16, LPR = C::WTN * 4, RPP = 64 / LPR;
-    char* wl = smem + wave * 32 * RS;
-    uint16_t* out = reinterpret_cast<uint16_t*>(a.c) + w * a.c_stride + (row0 + wm0) * a.ldc + col0 + wn0;
 #pragma unroll
-    for (int i = 0; i < C::WTM; ++i) {
-#pragma unroll
-      for (int j = 0; j < C::WTN; ++j)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<uint2*>(wl + l32 * RS + (j * 32 + g * 8 + half * 4) * 2) =
-              make_uint2(pack_bf16(acc[i][j][4 * g], acc[i][j][4 * g + 1]), pack_bf16(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]));
-#pragma unroll
-      for (int p = 0; p < 32 / RPP; ++p) {
-        const int row = p * RPP + lane / LPR, ch = lane % LPR;
-        const uint4 v = *reinterpret_cast<const uint4*>(wl + row * RS + ch * 16);
-        if (i * 32 + row < rows_left) {
-          uint16_t* o = out + (int64_t)(i * 32 + row) * a.ldc;
-          if (ch * 8 + 8 <= cols_left) {
-            *reinterpret_cast<Raw16a2*>(o + ch * 8) = Raw16a2{{v.x, v.y, v.z, v.w}};
-          } else {
+        for (int p = 0; p < 32 / RPP; ++p) {
+          const uint4 v = *reinterpret_cast<const uint4*>(wl + (p * RPP + r0) * RS + ch * 16);
+          T* o = out + (int64_t)(i * 32 + p * RPP) * ld + j0 * 32;
+          if (WITHIN || (i * 32 + p * RPP + r0 < rows_left && (j0 * 32 + (ch + 1) * V <= cols_left))) {
+            *reinterpret_cast<typename E::Raw*>(o) = typename E::Raw{{v.x, v.y, v.z, v.w}};
+          } else if (i * 32 + p * RPP + r0 < rows_left) {
             const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (ch * 8 + e < cols_left) o[ch * 8 + e] = (uint16_t)(u[e >> 1] >> (16 * (e & 1)));
+            for (int e = 0; e < V; ++e)
+              if (j0 * 32 + ch * V + e < cols_left) {
+                if constexpr (F) o[e] = __uint_as_float(u[e]);
+                else o[e] = (uint16_t)(u[e >> 1] >> (16 * (e & 1)));
+              }
           }
         }
       }
-    }
-  }
+  };
+  if (within) write(std::true_type{});
+  else write(std::false_type{});
 }
 
 // Few rows of a (a served model's tokens): the product is as fast as b can be read.  A block takes 16 rows of b and all of

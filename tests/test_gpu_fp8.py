@@ -154,6 +154,30 @@ def test_products(shape, dtype):
     assert float((got.double() - want).norm() / want.norm()) < (2e-6 if dtype == F32 else 4e-3)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(3, 2400, 2500, 100), (3, 2400, 2500, 200), (3, 2433, 2311, 330), (3, 2400, 2500, 1300), (1, 8192, 4096, 520)])
+def test_products_of_more_tiles_than_run_at_once(shape, dtype):
+    """Ragged ends and whole tiles of the largest size, contractions of one block and of many."""
+    k, m, n, length = shape
+    g = _gen(m + n + length)
+    a = OPS.fp8_quantize(padded((k, m, length), 0, 0, F32, g) * torch.exp(torch.randn(k, m, 1, generator=g, device=DEV)))
+    b = OPS.fp8_quantize(padded((k, n, length), 0, 0, F32, g) * 0.1)
+    bias = torch.randn(k, n, generator=g, device=DEV)
+    va, vb = _values(a), _values(b)
+    product = torch.matmul(va, vb.transpose(1, 2).contiguous())
+    terms = torch.matmul(va.abs(), vb.abs().transpose(1, 2).contiguous())
+    for bias in (None, bias):
+        want = product if bias is None else product + bias.double()[:, None]
+        size = terms if bias is None else terms + bias.double().abs()[:, None]
+        bound = ((length + 2) * U + (8 * 2.0 ** -13 if dtype == BF16 else 0)) * size    # (of eight products the largest is at most their sum)
+        out = torch.full((k, m, n + 3), 7.0, dtype=dtype, device=DEV)
+        got = OPS.fp8_matmul(a, b, bias, out=out[..., 1:n + 1])
+        within(got, want, bound + out_rounding(dtype) * (want.abs() + bound) + 1e-38, "product")
+        assert bool((out[..., 0] == 7).all()) and bool((out[..., n + 1:] == 7).all())
+        for _ in range(3):
+            assert torch.equal(got, OPS.fp8_matmul(a, b, bias, dtype=dtype))
+
+
 def test_scales_apply_to_their_blocks():
     """Integers that fp32 holds exactly: rows and blocks of very different scales, compared for equality."""
     g = _gen(3)
