@@ -8,7 +8,8 @@
 //
 // Rows alone: 16 lanes share a block, 8 elements each, one pass from registers.  With the transposed form or squares a
 // block of 512 threads takes a tile of 128 x 128, 4 rows x 8 columns a thread; the transposed bytes leave through LDS so that
-// both forms are written in whole lines while x is read once.  Bound by memory when there is much of it.
+// both forms are written in whole lines while x is read once.  Bound by memory when there is much of it: 16 x 512 rows of 4096,
+// bf16, 20.5 us = 4.9 TB/s; 4 x 2048 x 4096 in both forms 36 us = 3.7 TB/s, squares of 4 x 4096 x 4096 62 us = 4.3 TB/s.
 #include "dw_fp8.h"
 
 namespace dw {

@@ -20,6 +20,11 @@
 // Operand A of the instruction is the matrix b and operand B is a: a lane then holds one row of C and groups of four
 // consecutive columns, which leave through a piece of LDS of the wave's own as whole row pieces of 16 bytes a lane.
 // The accumulators start from the bias.  Rows past the end of a matrix repeat the last one; what they give is not written.
+//
+// 8192 cubed: 394 us = 2790 TFLOP/s (fp32 757 us = 1450); 4096 cubed: 56 us = 2450 (105 us = 1310).  16 x 512 x 4096 x 4096: 136 us =
+// 2020, where b alone is 268 MB.  What bounds a large product is power: of a block of 128 in a tile of 256 x 256 the matrix
+// instructions take 0.83 us, with zeros for numbers the kernel takes 1.0 and with random ones 1.4 to 1.5, at a lower clock.
+// Tiles that load their successor while they are written, loads further ahead and shorter rows in more stages change nothing.
 #include <type_traits>
 #include <utility>
 
@@ -585,6 +590,15 @@ int slices_of(int k, int64_t m, int64_t n, int64_t blocks) {
   return best;
 }
 
+// Tiles of 256 or of 128 by the turns they take: one of 256 a compute unit, 10 units of time, against two of 128, 5.8, or at most
+// one, 4 (us, 256s and 128s, in bf16; fp32 alike): 3000 cubed, 144 of 256: 43.7, 41.9; 3584 x 3584 x 512, 196: 14.1, 14.6;
+// 4352 x 4096 x 4096, 272: 90, 82; 7168 x 4096 x 2048, 448: 53, 62; 8448 x 4096 x 1024, 528: 48, 44.5; 16384 x 4096 x 1024, 1024: 69, 73
+bool large_tiles(int k, int64_t m, int64_t n) {
+  const int64_t large = tiles_of(k, m, n, 256), middle = tiles_of(k, m, n, 128), rest = middle % (2 * kCus);
+  const double last = rest == 0 ? 0 : rest <= kCus ? 4.0 : 5.8;
+  return 10.0 * (double)ceil_div(large, kCus) <= 5.8 * (double)(middle / (2 * kCus)) + last;
+}
+
 }  // namespace fp8
 
 size_t fp8_scratch_bytes(int k, int64_t m, int64_t n, int64_t kp) {
@@ -611,11 +625,10 @@ hipError_t launch_fp8_matmul(const Fp8Args& a_, hipStream_t s) {
     if (a.m <= 16) return fp8::launch_rows<1>(a, s);
     return a.m <= 32 ? fp8::launch_rows<2>(a, s) : fp8::launch_rows<4>(a, s);
   }
-  // Tiles as large as leave most compute units one (us): 4096 x 3328, contraction 1024, 208 tiles of 256: 20.5, in 128s 22.7;
-  // 3000 cubed, 144 of 256: 43, 43 (fp32 71, 65).  2 x 1500 x 700 x 5000, 144 of 128: fp32 39, in 64s 44 (bf16 33, 31);
-  // 4096 x 512 x 4096, 128 of 128: 24 and 32 in fp32, in 64s 22 and 28
-  if (fp8::tiles_of(a.k, a.m, a.n, 256) >= 200) return fp8::launch<fp8::Large>(a, s);
-  if (fp8::tiles_of(a.k, a.m, a.n, 128) >= (a.dtype == DW_F32 ? 144 : 200)) return fp8::launch<fp8::Middle>(a, s);
+  if (fp8::large_tiles(a.k, a.m, a.n)) return fp8::launch<fp8::Large>(a, s);
+  // Small tiles while they run all at once, two a compute unit (us, 64s and 128s): 4096 x 512 x 4096, 512 of them: 15.0, 23.1 (fp32
+  // 23.8, 28.4); 3 x 700 x 900 x 450, 495: 5.4, 7.1; 2 x 1500 x 700 x 5000, 528: 28.5, 30.4 (fp32 41.3, 36.0); 2048 cubed, 1024: 16.5, 12.6
+  if (fp8::tiles_of(a.k, a.m, a.n, 64) > 2 * kCus) return fp8::launch<fp8::Middle>(a, s);
   const int slices = fp8::slices_of(a.k, a.m, a.n, a.kp / fp8::BK);
   if (slices == 1) return fp8::launch<fp8::Small>(a, s);
   const int words = (int)ceil_div(a.kp / fp8::BK, fp8::GROUP);
