@@ -71,7 +71,7 @@ def _link_torch_module(obj: str) -> None:
     import torch
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     cmd = [shutil.which("g++") or "g++", "-shared", "-o", TORCH_LIB, obj, "-L", HERE, "-l:" + os.path.basename(LIB),
-           "-L", lib, "-lc10", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
+           "-L", lib, "-lc10", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -101,7 +102,8 @@ struct On {
   }
 };
 
-at::Tensor make(at::IntArrayRef shape, at::ScalarType type, at::Device device) { return at::empty(shape, at::TensorOptions().dtype(type).device(device)); }
+// straight from the device's allocator: the way through at::empty takes longer than a small call's launch has to spare
+at::Tensor make(at::IntArrayRef shape, at::ScalarType type, at::Device device) { return at::detail::empty_cuda(shape, type, device, std::nullopt); }
 
 // scratch that torch hands out again only to work behind this call's on the same stream
 struct Scratch {
