@@ -193,12 +193,13 @@ int dw_clip_grads(const void* const* h_grad, const int64_t* h_count, const int32
   if (!(max_norm > 0.f)) return DW_ERR_HYPER;
   if (!d_norm || (!h_grad && z.elements > 0)) return DW_ERR_NULL;
   if (!aligned(d_norm, 4) || (d_out && !grads_ok(d_out, out_stride, k, z.elements))) return DW_ERR_ARG;
-  for (int64_t i = 0; i < (int64_t)k * n_tensors; ++i) {
-    const int j = (int)(i % n_tensors);
-    if (h_count[j] == 0) continue;
-    if (!h_grad[i]) return DW_ERR_NULL;
-    if (!aligned(h_grad[i], type_bytes(h_dtype ? h_dtype[j] : dtype))) return DW_ERR_ARG;
-  }
+  for (int w = 0; w < k; ++w)
+    for (int j = 0; j < n_tensors; ++j) {
+      const void* g = h_grad ? h_grad[(int64_t)w * n_tensors + j] : nullptr;
+      if (h_count[j] == 0) continue;
+      if (!g) return DW_ERR_NULL;
+      if (!aligned(g, type_bytes(h_dtype ? h_dtype[j] : dtype))) return DW_ERR_ARG;
+    }
   if ((!d_scratch || !aligned(d_scratch, 256) || scratch_bytes < dw_clip_grads_scratch_bytes(k, n_tensors, h_count)))
     return DW_ERR_WORKSPACE;
   const hipStream_t s = (hipStream_t)stream;

@@ -293,7 +293,7 @@ PyObject* clip_grads(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   std::vector<int64_t> count(per);
   std::vector<int32_t> type(per);
   int64_t total = 0;
-  for (Py_ssize_t i = 0; i < n; ++i) {
+  for (Py_ssize_t i = 0, j = 0; i < n; ++i, j = j + 1 < per ? j + 1 : 0) {
     const at::Tensor& g = tensor(items[i], "a gradient");
     TORCH_CHECK_VALUE(g.device() == first.device(), "gradients on ", first.device(), " and ", g.device());
     TORCH_CHECK_VALUE(g.is_contiguous(), "a gradient is not contiguous");
@@ -304,7 +304,7 @@ PyObject* clip_grads(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       type[i] = t;
       total += count[i];
     } else {
-      TORCH_CHECK_VALUE(count[i % per] == g.numel() && type[i % per] == t, "worker ", i / per, " has tensors of other sizes or types than worker 0");
+      TORCH_CHECK_VALUE(count[j] == g.numel() && type[j] == t, "worker ", i / per, " has tensors of other sizes or types than worker 0");
     }
   }
   const Param out = param(maybe(a[3], "out"), "out", workers, total, first.device());
