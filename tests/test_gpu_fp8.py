@@ -101,6 +101,17 @@ def test_quantized_numbers(shape, dtype):
                 assert torch.equal(_values(t), _values(m).transpose(1, 2))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(1, 2100, 2050), (1, 2048, 2048), (5, 900, 1000)])
+def test_quantized_numbers_of_many_tiles(shape, dtype):
+    """Both forms of more tiles than compute units, and of as many: by one block, and by one for each."""
+    x = padded(shape, 3, 1, dtype, _gen(sum(shape)))
+    for square in (False, True):
+        m, t = OPS.fp8_quantize(x, square=square, transposed=True)
+        _check_quantized(m, x, square)
+        _check_quantized(t, x.transpose(1, 2), square)
+
+
 def test_rounding_scales_and_extremes():
     x = torch.zeros(1, 8, 128, device=DEV)
     x[0, 0, :4] = torch.tensor([448.0, 447.0, 1.0625, 1.1875])             # ties to even at the fourth bit
