@@ -49,6 +49,12 @@ int type_of(const at::Tensor& t, const char* name) {
   return s == at::kBFloat16 ? DW_BF16 : DW_F32;
 }
 
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw python_error();
+  return v != 0;
+}
+
 struct Matrix { void* p; int64_t ld, stride; };
 
 // a [k][rows][n] tensor with contiguous rows
@@ -169,7 +175,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const at::Tensor y = a[4] == Py_None ? make(x.sizes(), x.scalar_type(), x.device()) : tensor(a[4], "out");
   const Matrix my = matrix_like(y, "out", x.sizes(), x.scalar_type(), x.device());
   at::Tensor mean, rstd;
-  if (a[5] == Py_True) {
+  if (truth(a[5])) {
     mean = make({k, rows}, at::kFloat, x.device());
     rstd = make({k, rows}, at::kFloat, x.device());
   }
@@ -196,12 +202,12 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const void* rstd = values(&tensor(a[4], "rstd"), "rstd", k, rows, at::kFloat, x.device());
   at::Tensor dx, dgamma, dbeta;
   Matrix mdx = {nullptr, n, rows * n};
-  if (a[8] == Py_True) {
+  if (truth(a[8])) {
     dx = a[5] == Py_None ? make(x.sizes(), x.scalar_type(), x.device()) : tensor(a[5], "dx");
     mdx = matrix_like(dx, "dx", x.sizes(), x.scalar_type(), x.device());
   }
   Param dg = {nullptr, n}, db = {nullptr, n};
-  if (a[9] == Py_True) {
+  if (truth(a[9])) {
     dgamma = a[6] == Py_None ? make({k, n}, at::kFloat, x.device()) : tensor(a[6], "dgamma");
     dbeta = a[7] == Py_None ? make({k, n}, at::kFloat, x.device()) : tensor(a[7], "dbeta");
     dg = param(&dgamma, "dgamma", k, n, x.device());
@@ -257,7 +263,7 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const double low = number(a[6]), high = number(a[7]), kl = number(a[8]);
   at::Tensor grad;
   Matrix mg = {nullptr, vocab, rows * vocab};
-  if (a[10] == Py_True) {
+  if (truth(a[10])) {
     grad = a[9] == Py_None ? make(z.sizes(), z.scalar_type(), z.device()) : tensor(a[9], "grad");
     mg = matrix_like(grad, "grad", z.sizes(), z.scalar_type(), z.device());
   }
@@ -338,8 +344,8 @@ PyObject* fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const int64_t k = x.size(0), rows = x.size(1), n = x.size(2);
   const Eight m = make_eight(k, rows, n, x.device());
   Eight t;
-  if (a[2] == Py_True) t = make_eight(k, n, rows, x.device());
-  check(dw_fp8_quantize(mx.p, mx.ld, mx.stride, workers_of(k), rows, n, type, a[1] == Py_True ? 1 : 0, bytes(m.q), bytes(m.scale), bytes(t.q),
+  if (truth(a[2])) t = make_eight(k, n, rows, x.device());
+  check(dw_fp8_quantize(mx.p, mx.ld, mx.stride, workers_of(k), rows, n, type, truth(a[1]) ? 1 : 0, bytes(m.q), bytes(m.scale), bytes(t.q),
                         bytes(t.scale), on.stream),
         "dw_fp8_quantize");
   if (t.q.defined()) return tuple(wrap(m.q), wrap(m.scale), wrap(t.q), wrap(t.scale));
@@ -369,7 +375,7 @@ PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const int64_t k = x.q.size(0), m = x.q.size(1), rows = w.q.size(1);
   TORCH_CHECK_VALUE(w.q.size(0) == k && w.q.device() == device, "operands of ", k, " workers on ", device, " and ", w.q.size(0), " on ", w.q.device());
   const Param b = param(maybe(a[6], "bias"), "bias", k, rows, device);
-  const at::Tensor c = a[7] == Py_None ? make({k, m, rows}, a[8] == Py_True ? at::kBFloat16 : at::kFloat, device) : tensor(a[7], "out");
+  const at::Tensor c = a[7] == Py_None ? make({k, m, rows}, truth(a[8]) ? at::kBFloat16 : at::kFloat, device) : tensor(a[7], "out");
   const int code = type_of(c, "out");
   const Matrix mc = matrix_like(c, "out", {k, m, rows}, c.scalar_type(), device);
   const Scratch scratch(dw_fp8_matmul_scratch_bytes(workers_of(k), m, rows, n), device);

@@ -4,8 +4,9 @@ the library's handle-free entry points (include/dw.h).
 Tensors of activations are [k][rows][n] with contiguous rows (any row and worker stride, so views of wider buffers do),
 float32 or bfloat16; parameters and their gradients are float32.  Outputs and scratch are allocated by torch on the
 current stream of the tensors' device, where the work is enqueued; nothing is synchronised.  As with any torch operator,
-a tensor made on another stream has to be waited for, and recorded, by the caller.  Wrong shapes, types or layouts raise
-ValueError, what the library refuses binding.DwError; there is no CPU path.
+a tensor made on another stream has to be waited for, and recorded, by the caller.  Nothing is recorded for autograd: the
+backward passes are calls of their own.  Wrong shapes, types or layouts raise ValueError, what the library refuses
+binding.DwError; there is no CPU path.
 
 Tensors are taken apart in a compiled module, _dw_torch (csrc/dw_torch.cpp), which calls the same C functions as
 binding.py: these operators run for a few microseconds, and in Python that costs more than the work.

@@ -276,3 +276,11 @@ def test_refusals():
                 lambda: OPS.fp8_matmul(q, q, out=torch.zeros(2, 4, 5, device=DEV)), lambda: OPS.fp8_matmul(q, q, dtype=torch.float16)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_flags_are_taken_by_their_truth():
+    x = torch.ones(1, 4, 200, device=DEV)
+    m, t = OPS.fp8_quantize(x, square=1, transposed=1)
+    want, turned = OPS.fp8_quantize(x, square=True, transposed=True)
+    assert torch.equal(m.scale, want.scale) and torch.equal(t.scale, turned.scale) and t.shape == (1, 200, 4)
+    assert OPS.layer_norm(x, stats=0)[1] is None and OPS.layer_norm(x, stats=1)[1].shape == (1, 4)
