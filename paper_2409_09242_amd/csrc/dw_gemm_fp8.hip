@@ -139,6 +139,12 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   const int block0 = SLICE ? (int)blockIdx.y * a.slice_blocks : 0;
   const int blocks = SLICE ? (all_blocks - block0 < a.slice_blocks ? all_blocks - block0 : a.slice_blocks) : all_blocks;
 
+  // Workers begin at different blocks of the contraction (whole words of scales): the dies, each at a worker of its own, would
+  // otherwise ask for the same columns of long rows at once, which lie in few channels of the memory.  (us, without and with:
+  // 16 x 512 x 4096 x 4096: 146, 139; 16 x 256 x 4096 x 4096: 89, 80.  In tiles of 128 two of three shapes got slower by 3 and 8 %.)
+  const int turn = SLICE || C::BM < 256 || blocks % GROUP ? 0 : w % (blocks / GROUP) * GROUP;
+  auto place = [&](int b) { return b + turn < blocks ? b + turn : b + turn - blocks; };
+
   // The pieces this wave moves: the first half of the waves A's tile, the others B's; piece c holds rows 8c .. 8c+7.  A
   // uniform base that advances by a block, and a lane's offset from it (a tile's rows span less than 2^32 bytes).
   const bool of_a = wave < C::NW / 2;
@@ -167,7 +173,7 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   const uint32_t lds_scale = __builtin_amdgcn_readfirstlane(lds0 + C::OFF_S + (of_a ? 0 : C::BM * 4));
   auto issue = [&](const uint8_t* from, int b, int c) { load_to_lds<16>(from, off[c], lds_tile + (b & (C::STAGES - 1)) * C::STAGE_B + c * 1024); };
   auto issue_scales = [&](int g) {
-    const uint8_t* from = uniform(sbase + g * 4);
+    const uint8_t* from = uniform(sbase + place(g * GROUP));
 #pragma unroll
     for (int c = 0; c < SPW; ++c)
       if (sfirst + c * (C::NW / 2) < SP)
@@ -243,7 +249,7 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
 #pragma unroll
   for (int b = 0; b < C::STAGES; ++b)
     if (b < blocks) {
-      const uint8_t* from = uniform(base + (int64_t)b * BK);
+      const uint8_t* from = uniform(base + (int64_t)place(b) * BK);
 #pragma unroll
       for (int c = 0; c < C::CPW; ++c) issue(from, b, c);
     }
@@ -275,7 +281,7 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
     }
     const bool reads = SUB == 0 || MORE || b + 1 < blocks;
     const int loads = SUB == 1 ? b : b - 1;                  // whose stage is loaded anew
-    const uint8_t* from = uniform(base + (int64_t)(loads + C::STAGES) * BK);
+    const uint8_t* from = uniform(base + (int64_t)place(loads + C::STAGES) * BK);
     constexpr int Q = EXACT ? 4 : 1, PRODUCTS = C::WTM * C::WTN * Q, OPERANDS = C::WTM + C::WTN;
     Wide wide[2];
     if constexpr (EXACT) {
