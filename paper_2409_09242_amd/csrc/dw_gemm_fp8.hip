@@ -22,9 +22,10 @@
 // The accumulators start from the bias.  Rows past the end of a matrix repeat the last one; what they give is not written.
 //
 // 8192 cubed: 394 us = 2790 TFLOP/s (fp32 757 us = 1450); 4096 cubed: 56 us = 2450 (105 us = 1310).  16 x 512 x 4096 x 4096: 136 us =
-// 2020, where b alone is 268 MB.  What bounds a large product is power: of a block of 128 in a tile of 256 x 256 the matrix
-// instructions take 0.83 us, with zeros for numbers the kernel takes 1.0 and with random ones 1.4 to 1.5, at a lower clock.
-// Tiles that load their successor while they are written, loads further ahead and shorter rows in more stages change nothing.
+// 2020, where b alone is 268 MB and comes from memory in pieces of 128 bytes (8 workers, b in the chip's cache: 55 us = 2500).
+// What bounds a large product is power: of a block of 128 in a tile of 256 x 256 the matrix instructions take 0.85 us, with
+// zeros for numbers the kernel takes 1.2 and with random ones 1.5, at a lower clock.  Tiles that load their successor while
+// they are written, loads further ahead and shorter rows in more stages change nothing.
 #include <type_traits>
 #include <utility>
 
