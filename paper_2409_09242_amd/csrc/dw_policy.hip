@@ -11,7 +11,7 @@
 // of each of 1024 threads the rest of the row is read again, from the caches.  Log probabilities alone (no gradient) need no
 // registers for the row, and are the same bits: the same pieces in the same order.  Bound by memory; with the whole row in the
 // registers of one compute unit a block's loads and stores take turns, so rows are shared among as few threads as hold them.
-// 8 x 1024 rows of 131072, bf16, with the gradient: 809 us = 5.3 TB/s; 4 x 100 rows of 5000, fp32: 6.8 us and 2.1 for the sums.
+// 8 x 1024 rows of 131072, bf16, with the gradient: 809 us = 5.3 TB/s; 4 x 100 rows of 5003, fp32: 6.8 us and 2.1 for the sums.
 //
 // Sums over a row are in fp32 (of a thread at most 16 pieces' sums, then a tree); the rows' losses go to scratch and a second kernel
 // adds a worker's up in 64 bits in a fixed order.
