@@ -211,7 +211,7 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   }
   auto read_one = [&](Frags& f, int b, int sub, int r) {     // step `sub` of block b
     const char* stage = smem + (b & (C::STAGES - 1)) * C::STAGE_B;
-    const int h = r & 1, i = r >> 1;
+    const int h = EXACT ? r / (READS / 2) : r & 1, i = EXACT ? r % (READS / 2) : r >> 1;    // (EXACT: what is widened first)
     if (i < C::WTM) f.x[i][h] = *reinterpret_cast<const uint4*>(stage + at_x[sub * 2 + h] + i * 32 * BK);
     else f.y[i - C::WTM][h] = *reinterpret_cast<const uint4*>(stage + at_y[sub * 2 + h] + (i - C::WTM) * 32 * BK);
   };
@@ -241,10 +241,12 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
     return q & 1 ? widen((int)u.z, (int)u.w, power(scale)) : widen((int)u.x, (int)u.y, power(scale));
   };
   struct Wide { bf16x8 x[C::WTM], y[C::WTN]; };
-  auto widen_one = [&](Wide& d, const Frags& f, int q, int i) {
-    if (i < C::WTM) d.x[i] = eight(f.x[i], q, sx[i]);
-    else d.y[i - C::WTM] = eight(f.y[i - C::WTM], q, sy[i - C::WTM]);
+  auto widen_one = [&](Wide& d, const Frags& f, int q, int i, const int (&x)[C::WTM], const int (&y)[C::WTN]) {
+    if (i < C::WTM) d.x[i] = eight(f.x[i], q, x[i]);
+    else d.y[i - C::WTM] = eight(f.y[i - C::WTM], q, y[i - C::WTM]);
   };
+  constexpr int Q = EXACT ? 4 : 1, PRODUCTS = C::WTM * C::WTN * Q, OPERANDS = C::WTM + C::WTN;
+  Wide wide[2];                                              // EXACT: the present quarter of a step, and the next or the next step's first
 
   issue_scales(0);
 #pragma unroll
@@ -262,6 +264,10 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   take_scales();
 #pragma unroll
   for (int r = 0; r < READS; ++r) read_one(f0, 0, 0, r);
+  if constexpr (EXACT) {
+#pragma unroll
+    for (int i = 0; i < OPERANDS; ++i) widen_one(wide[0], f0, 0, i, sx, sy);
+  }
 
   // Step SUB of block b: its operands are in registers.  The second step opens with a barrier: every wave has then read all
   // of block b, whose stage is loaded anew, and block b + 1 has arrived (the counts leave the blocks behind it in flight;
@@ -283,19 +289,13 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
     const bool reads = SUB == 0 || MORE || b + 1 < blocks;
     const int loads = SUB == 1 ? b : b - 1;                  // whose stage is loaded anew
     const uint8_t* from = uniform(base + (int64_t)place(loads + C::STAGES) * BK);
-    constexpr int Q = EXACT ? 4 : 1, PRODUCTS = C::WTM * C::WTN * Q, OPERANDS = C::WTM + C::WTN;
-    Wide wide[2];
-    if constexpr (EXACT) {
-#pragma unroll
-      for (int i = 0; i < OPERANDS; ++i) widen_one(wide[0], now, 0, i);
-    }
     __builtin_amdgcn_sched_barrier(0);
     each<0, PRODUCTS>([&](auto p_) {
       constexpr int PN = C::WTM * C::WTN, p = decltype(p_)::value, q = p / PN, ij = p % PN, i = ij / C::WTN, j = ij % C::WTN;
       if constexpr (EXACT) {
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[q & 1].y[j], wide[q & 1].x[i], acc[i][j], 0, 0, 0);
         if constexpr (q + 1 < Q)
-          each<ij * OPERANDS / PN, (ij + 1) * OPERANDS / PN>([&](auto o) { widen_one(wide[(q + 1) & 1], now, q + 1, o); });
+          each<ij * OPERANDS / PN, (ij + 1) * OPERANDS / PN>([&](auto o) { widen_one(wide[(q + 1) & 1], now, q + 1, o, sx, sy); });
       } else {
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(now.y[j]), whole(now.x[i]), acc[i][j], 0, 0, 0, sy[j], 0, sx[i]);
       }
@@ -307,7 +307,12 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
       }
       if (reads) {
         each<p * READS / PRODUCTS, (p + 1) * READS / PRODUCTS>([&](auto r) { read_one(next, b + SUB, 1 - SUB, r); });
-        if constexpr (SUB == 1 && p == PRODUCTS / 2) read_scales(b + 1);
+        if constexpr (SUB == 1 && p == (EXACT ? 0 : PRODUCTS / 2)) read_scales(b + 1);
+        if constexpr (EXACT && q == Q - 1)
+          each<ij * OPERANDS / PN, (ij + 1) * OPERANDS / PN>([&](auto o) {
+            if constexpr (SUB == 1) widen_one(wide[0], next, 0, o, nx, ny);
+            else widen_one(wide[0], next, 0, o, sx, sy);
+          });
       }
       __builtin_amdgcn_sched_barrier(0);
     });
