@@ -28,7 +28,8 @@ inline int64_t blocks_per_worker(int k, int64_t rows, int groups, int64_t target
 }
 
 // A row of n is its whole pieces of 16 bytes, piece i * TPR + t to thread t, and fewer than V elements more, one each to the
-// first threads: every access is in bounds and no piece needs a mask of its own.
+// first threads: every access is in bounds and no piece needs a mask of its own.  for_row sees to it that there are as many
+// threads as odd elements.
 template <class E, int TPR>
 struct Split {
   int whole, tail;                                         // whole pieces; this thread's element behind them
@@ -402,11 +403,17 @@ __global__ __launch_bounds__(1024) void layer_norm_strips_kernel(NormArgs a) {
   }
 }
 
-// f.template operator()<TPR, ITEMS>() for a row of `pieces` whole pieces: the fewest threads whose registers take the row
-// in up to two pieces each, then up to four of 512 and (WIDE) of 1024; false: too long
-template <bool WIDE, class F>
-bool for_row(int64_t pieces, F f) {
-  if (pieces <= 4) f.template operator()<4, 1>();
+// f.template operator()<TPR, ITEMS>() for a row of n: the fewest threads whose registers take its whole pieces in up to two
+// each, then up to four of 512 and (WIDE) of 1024, and at least as many as it has odd elements; false: too long.  In bf16 the
+// shortest rows have up to seven of those, and four threads only where four will do (us, forward and backward, by four and by
+// eight: 16 x 8192 x 32: 5.4 and 9.4, 6.8 and 11.1; 4 x 512 x 16 alike)
+template <class E, bool WIDE, class F>
+bool for_row(int64_t n, F f) {
+  constexpr int FEWEST = 4;
+  static_assert(E::V >= FEWEST && 16 >= E::V - 1, "every form but the first takes any number of odd elements");
+  const int64_t pieces = n / E::V, odd = n % E::V;
+  if (pieces <= 4 && odd <= FEWEST) f.template operator()<FEWEST, 1>();
+  else if (pieces <= 4) f.template operator()<E::V, 1>();
   else if (pieces <= 16) f.template operator()<16, 1>();
   else if (pieces <= 32) f.template operator()<32, 1>();
   else if (pieces <= 64) f.template operator()<64, 1>();
@@ -440,7 +447,7 @@ struct Forward {
 };
 template <class E>
 hipError_t fwd_any(const NormArgs& a, hipStream_t s) {
-  if (!for_row<true>(a.n / E::V, Forward<E>{a, s}))
+  if (!for_row<E, true>(a.n, Forward<E>{a, s}))
     hipLaunchKernelGGL(layer_norm_long_kernel<E>, dim3((unsigned)blocks_per_worker(a.k, a.rows, 1, 4 * kCus), (unsigned)a.k), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
@@ -466,7 +473,7 @@ struct Strips {
 };
 template <class E>
 hipError_t bwd_any(const NormArgs& a, hipStream_t s) {
-  if (for_row<kWideGrad<E>>(a.n / E::V, Backward<E>{a, s})) return hipGetLastError();
+  if (for_row<E, kWideGrad<E>>(a.n, Backward<E>{a, s})) return hipGetLastError();
   if (a.out.p) {
     hipLaunchKernelGGL(layer_norm_grad_long_kernel<E>, dim3((unsigned)blocks_per_worker(a.k, a.rows, 1, 4 * kCus), (unsigned)a.k), dim3(1024), 0, s, a);
     const hipError_t e = hipGetLastError();
@@ -482,7 +489,7 @@ hipError_t bwd_any(const NormArgs& a, hipStream_t s) {
 int layer_norm_grad_strips(int k, int64_t rows, int64_t n, int dtype) {
   int strips = 0;
   const Strips count{k, rows, &strips};
-  const bool fits = dtype == DW_BF16 ? for_row<kWideGrad<Bf16>>(n / Bf16::V, count) : for_row<kWideGrad<F32>>(n / F32::V, count);
+  const bool fits = dtype == DW_BF16 ? for_row<Bf16, kWideGrad<Bf16>>(n, count) : for_row<F32, kWideGrad<F32>>(n, count);
   return fits ? strips : (int)blocks_per_worker(k, rows, 1, 2 * kCus);
 }
 
