@@ -74,6 +74,13 @@ class PolicyWorkers:
         self._split()
 
 
+def draw_tokens(z, g):
+    """A draw from softmax(z) for every row of logits, int32: the largest of z plus Gumbel noise (an index in range whatever
+    z holds)."""
+    waits = -torch.rand(z.shape, generator=g, device=z.device).clamp_min(1e-20).log()       # exponentially distributed
+    return (z.float() - waits.clamp_min(1e-20).log()).argmax(-1).to(torch.int32)
+
+
 def train(k: int = 4, rows: int = 512, width: int = 72, vocab: int = 75, rounds: int = 20, updates: int = 3, seed: int = 0,
           lr: float = 2.0, device="cuda:0"):
     """Mean reward of the sampled tokens in every round, [rounds][k]."""
@@ -85,9 +92,7 @@ def train(k: int = 4, rows: int = 512, width: int = 72, vocab: int = 75, rounds:
     for _ in range(rounds):
         x = torch.randn(k, rows, width, generator=g, device=device, dtype=torch.bfloat16)
         z, _ = workers.logits(x)
-        # a draw from softmax(z): the largest of z plus Gumbel noise (an index in range whatever z holds)
-        noise = -torch.rand(z.shape, generator=g, device=device).clamp_min(1e-20).log().clamp_min(1e-20).log()
-        token = (z.float() + noise).argmax(-1).to(torch.int32)
+        token = draw_tokens(z, g)
         old = OPS.token_logp(z, token)
         score = x.float() @ teacher.t()
         reward = score.gather(-1, token.long()[..., None])[..., 0]
