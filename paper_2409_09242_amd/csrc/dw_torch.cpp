@@ -134,6 +134,14 @@ void check(int status, const char* where) {
   throw python_error();
 }
 
+// a tensor of the caller's has been written to: a graph of autograd's that saved it sees that its values are gone, as it does
+// behind torch's own in-place operators (tensors made in inference mode have no versions, and no graph saves them)
+void written(PyObject* o) {
+  if (o == Py_None) return;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 int workers_of(int64_t k) {                                  // (what does not fit an int is refused as too many)
   return k > DW_MAX_K ? DW_MAX_K + 1 : (int)k;
 }
@@ -183,6 +191,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                       my.stride, mean.defined() ? static_cast<float*>(mean.data_ptr()) : nullptr,
                       rstd.defined() ? static_cast<float*>(rstd.data_ptr()) : nullptr, on.stream),
         "dw_layer_norm");
+  written(a[4]);
   return tuple(wrap(y), wrap_or_none(mean), wrap_or_none(rstd));
   END_HANDLE_TH_ERRORS
 }
@@ -219,6 +228,8 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                            static_cast<const float*>(rstd), workers_of(k), rows, n, type, mdx.p, mdx.ld, mdx.stride, dg.p, db.p, dg.stride,
                            scratch.p, scratch.bytes, on.stream),
         "dw_layer_norm_grad");
+  if (dx.defined()) written(a[5]);
+  if (dg.p) { written(a[6]); written(a[7]); }
   return tuple(wrap_or_none(dx), wrap_or_none(dgamma), wrap_or_none(dbeta));
   END_HANDLE_TH_ERRORS
 }
@@ -240,6 +251,7 @@ PyObject* token_logp(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   check(dw_token_logp(mz.p, mz.ld, mz.stride, static_cast<const int32_t*>(target), workers_of(k), rows, vocab, type, static_cast<float*>(po),
                       on.stream),
         "dw_token_logp");
+  written(a[2]);
   return wrap(out);
   END_HANDLE_TH_ERRORS
 }
@@ -273,6 +285,7 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                        type, (float)low, (float)high, (float)kl, static_cast<float*>(loss.data_ptr()), static_cast<float*>(logp.data_ptr()),
                        mg.p, mg.ld, mg.stride, scratch.p, scratch.bytes, on.stream),
         "dw_policy_loss");
+  if (grad.defined()) written(a[9]);
   return tuple(wrap(loss), wrap(logp), wrap_or_none(grad));
   END_HANDLE_TH_ERRORS
 }
@@ -320,6 +333,9 @@ PyObject* clip_grads(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   check(dw_clip_grads(address.data(), count.data(), type.data(), k, tensors, DW_F32, (float)max_norm, out.p, out.stride,
                       static_cast<float*>(norm.data_ptr()), scratch.p, scratch.bytes, on.stream),
         "dw_clip_grads");
+  written(a[3]);
+  if (!out.p && std::isfinite((float)max_norm))
+    for (Py_ssize_t i = 0; i < n; ++i) written(items[i]);
   return wrap(norm);
   END_HANDLE_TH_ERRORS
 }
@@ -382,6 +398,7 @@ PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   check(dw_fp8_matmul(bytes(x.q), bytes(x.scale), bytes(w.q), bytes(w.scale), b.p, b.stride, workers_of(k), m, rows, n, code, mc.p, mc.ld,
                       mc.stride, scratch.p, scratch.bytes, on.stream),
         "dw_fp8_matmul");
+  written(a[7]);
   return wrap(c);
   END_HANDLE_TH_ERRORS
 }
@@ -407,6 +424,7 @@ PyObject* fp8_linear(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   check(dw_fp8_linear(mx.p, mx.ld, mx.stride, bytes(w.q), bytes(w.scale), b.p, b.stride, workers_of(k), m, rows, n, type, my.p, my.ld, my.stride,
                       scratch.p, scratch.bytes, on.stream),
         "dw_fp8_linear");
+  written(a[5]);
   return wrap(y);
   END_HANDLE_TH_ERRORS
 }

@@ -5,7 +5,8 @@ Tensors of activations are [k][rows][n] with contiguous rows (any row and worker
 float32 or bfloat16; parameters and their gradients are float32.  Outputs and scratch are allocated by torch on the
 current stream of the tensors' device, where the work is enqueued; nothing is synchronised.  As with any torch operator,
 a tensor made on another stream has to be waited for, and recorded, by the caller.  Nothing is recorded for autograd: the
-backward passes are calls of their own.  Wrong shapes, types or layouts raise ValueError, what the library refuses
+backward passes are calls of their own; tensors that a call writes into count as changed in place, so that a graph which
+saved one refuses its backward pass.  Wrong shapes, types or layouts raise ValueError, what the library refuses
 binding.DwError; there is no CPU path.
 
 Tensors are taken apart in a compiled module, _dw_torch (csrc/dw_torch.cpp), which calls the same C functions as
