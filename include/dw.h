@@ -286,7 +286,8 @@ int dw_draw_batch(dw_handle* h, const void* d_data, const int32_t* d_labels, int
  * need no handle; the conventions above hold (caller's memory and stream, nothing allocated, nothing synchronised).
  * A matrix argument is d_p, ld, stride: element j of row r of worker w is d_p[w*stride + r*ld + j].  Rows are contiguous
  * and may start at any multiple of the element size; ld >= row length; the stride of an input may be 0 (shared by the
- * workers).  Outputs overlap neither each other nor an input, unless a call says so.  dtype is DW_F32 or DW_BF16; sums are
+ * workers), that of an output anything that keeps its rows apart (the workers one behind the other, or interleaved row by
+ * row).  Outputs overlap neither each other nor an input, unless a call says so.  dtype is DW_F32 or DW_BF16; sums are
  * kept in fp32 or more and results do not depend on the order in which blocks run.
  * Scratch is device memory, 256-byte aligned, of the bytes that the call's own function gives (0: none is needed, it may
  * be NULL); its contents need not be kept from one call to the next.
