@@ -216,18 +216,28 @@ PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     mdx = matrix_like(dx, "dx", x.sizes(), x.scalar_type(), x.device());
   }
   Param dg = {nullptr, n}, db = {nullptr, n};
+  at::Tensor through;                                        // [k][n] for the one that is given, where the other has no layout of its own
   if (truth(a[9])) {
     dgamma = a[6] == Py_None ? make({k, n}, at::kFloat, x.device()) : tensor(a[6], "dgamma");
     dbeta = a[7] == Py_None ? make({k, n}, at::kFloat, x.device()) : tensor(a[7], "dbeta");
     dg = param(&dgamma, "dgamma", k, n, x.device());
     db = param(&dbeta, "dbeta", k, n, x.device());
-    TORCH_CHECK_VALUE(dg.stride == db.stride, "dgamma and dbeta have different worker strides");
+    if (dg.stride != db.stride) {
+      TORCH_CHECK_VALUE(a[6] == Py_None || a[7] == Py_None, "dgamma and dbeta have different worker strides");
+      TORCH_CHECK_VALUE(dg.stride >= n && db.stride >= n, "the workers' rows of ", a[6] == Py_None ? "dbeta" : "dgamma", " overlap");
+      through = make({k, n}, at::kFloat, x.device());
+      (a[6] == Py_None ? db : dg) = param(&through, "dgamma", k, n, x.device());
+    }
   }
   const Scratch scratch(dg.p ? dw_layer_norm_grad_scratch_bytes(workers_of(k), rows, n, type) : 0, x.device());
   check(dw_layer_norm_grad(mdy.p, mdy.ld, mdy.stride, mx.p, mx.ld, mx.stride, g.p, g.stride, static_cast<const float*>(mean),
                            static_cast<const float*>(rstd), workers_of(k), rows, n, type, mdx.p, mdx.ld, mdx.stride, dg.p, db.p, dg.stride,
                            scratch.p, scratch.bytes, on.stream),
         "dw_layer_norm_grad");
+  if (through.defined()) {
+    at::AutoDispatchBelowADInplaceOrView below;               // (written() below counts it, and autograd has no part in it)
+    (a[6] == Py_None ? dbeta : dgamma).copy_(through);
+  }
   if (dx.defined()) written(a[5]);
   if (dg.p) { written(a[6]); written(a[7]); }
   return tuple(wrap_or_none(dx), wrap_or_none(dgamma), wrap_or_none(dbeta));

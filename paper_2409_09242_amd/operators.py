@@ -40,7 +40,8 @@ def _ops():
 # ---- layer norm ------------------------------------------------------------------------------------------------------
 
 def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, out=None, stats: bool = True):
-    """y = (x - mean) * rstd * gamma + beta over the last axis of x [k][rows][n]; gamma, beta: float32 [k][n] or None.
+    """y = (x - mean) * rstd * gamma + beta over the last axis of x [k][rows][n]; gamma, beta: float32 [k][n] with the same
+    worker stride, or None.
 
     Returns (y, mean, rstd), the latter float32 [k][rows] for layer_norm_grad, or None both with stats=False (a served
     model).  out: a tensor like x for y."""
@@ -49,8 +50,8 @@ def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, out=None, stats: boo
 
 def layer_norm_grad(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, want_dx: bool = True, want_params: bool = True):
     """(dx, dgamma, dbeta) of layer_norm from dy, its input and the statistics it returned.  dx, dgamma, dbeta: tensors to
-    write into (float32 [k][n] for the latter two, such as views of the flat gradient of Handle.update_only); what is not
-    wanted is returned as None."""
+    write into (float32 [k][n] for the latter two, such as views of the flat gradient of Handle.update_only, with the same
+    worker stride where both are given); what is not wanted is returned as None."""
     return (_MODULE or _ops()).layer_norm_grad(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, want_dx, want_params)
 
 
