@@ -365,7 +365,7 @@ int dw_clip_grads(const void* const* h_grad, const int64_t* h_count, const int32
 
 /*
  * Matrices in 8 bits: rows of e4m3 numbers (4 bits of exponent, 3 of mantissa, largest 448, no infinities) with one scale
- * for each block of 128 along the row, a power of two kept as the byte e + 127.  The matrix instruction applies such
+ * for each block of 128 along the row, a power of two kept as the byte e + 127 (1 to 254).  The matrix instruction applies such
  * scales by itself; e4m3 is a floating format, so against a scale of full precision nothing is lost but up to one of its
  * binades at the small end.  A row of n numbers takes DW_FP8_ROW(n) bytes (zeros behind the n-th) and DW_FP8_SCALES(n) bytes of
  * scales; rows follow each other without gaps, workers too.
@@ -387,10 +387,10 @@ int dw_fp8_quantize(const void* d_x, int64_t x_ld, int64_t x_stride, int k, int6
 
 /*
  * C = A B^T (+ bias) of such matrices, for every worker: A [m] rows and B [n] rows of `contraction` numbers, C [m][n] in
- * `dtype`.  In DW_F32 the sums are those of fp32.  In DW_BF16 the products run at the 8-bit rate, whose instruction adds eight
- * neighbouring products at a time with bits down to 2^-13 of the largest (about 1e-5 of a sum of random terms, a hundredth
- * of the rounding to bf16), and the eights in fp32.  With x, W and dy quantised along the axis that is summed:
- * y = x W^T, dx = dy (W^T)^T, dW = dy^T (x^T)^T.
+ * `dtype`.  In DW_F32 the sums are those of fp32 (of numbers in steps of 2^-132, where a scale is below 2^-123).  In DW_BF16 the
+ * products run at the 8-bit rate, whose instruction adds eight neighbouring products at a time with bits down to 2^-13 of the
+ * largest (about 1e-5 of a sum of random terms, a hundredth of the rounding to bf16), and the eights in fp32.  With x, W and
+ * dy quantised along the axis that is summed:  y = x W^T, dx = dy (W^T)^T, dW = dy^T (x^T)^T.
  *   d_bias      [k] rows of n floats, worker w's at w*bias_stride; NULL: none
  * An empty contraction gives the bias, or zeros (the operands may then be NULL).
  */

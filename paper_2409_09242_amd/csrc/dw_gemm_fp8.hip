@@ -14,8 +14,10 @@
 // (measured; all 8-bit matrix instructions of this chip do).  On normally distributed numbers the sums are then off by
 // 1.4e-5 of their size, on numbers with one in a hundred a hundred times larger by 7e-5: a fraction of a percent of an
 // output's rounding to bf16 (2e-3), but not fp32.  So outputs in fp32 take another way (EXACT): the same bytes are turned
-// into bf16, scale and all, by one instruction for two numbers, which is exact, and multiplied by v_mfma_f32_32x32x16_bf16 at
-// half the rate, whose sums are right to 24 bits.
+// into bf16, scale and all, by one instruction for two numbers and multiplied by v_mfma_f32_32x32x16_bf16 at half the rate, whose
+// sums are right to 24 bits.  The quantiser's largest number is 2^128 (what the lowest value of fp32 or bf16, a usual mask, is
+// rounded to), which bf16 does not hold: both operands are widened at half their size, and the sums are multiplied by four at
+// the end.  That is exact down to scales of 2^-123; below, numbers count in steps of 2^-132, which is twice bf16's smallest.
 //
 // Operand A of the instruction is the matrix b and operand B is a: a lane then holds one row of C and groups of four
 // consecutive columns, which leave through a piece of LDS of the wave's own as whole row pieces of 16 bytes a lane.
@@ -107,7 +109,10 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
   r.v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return __builtin_bit_cast(bf16x8, r);
 }
-__device__ __forceinline__ float power(int byte) { return __uint_as_float((unsigned)byte << 23); }
+// half of 2^(byte - 127), which is what a number is widened with, and what that makes of the product of two (the conversion
+// takes the power from the exponent's bits: 2^-127 for a zero)
+__device__ __forceinline__ float half_power(int byte) { return __uint_as_float(((unsigned)byte - 1u) << 23); }
+constexpr float kWidened = 0.25f;
 
 template <class C, bool EXACT, bool SLICE>
 __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
@@ -238,7 +243,7 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
   };
   auto eight = [](const uint4 (&v)[2], int q, int scale) {
     const uint4 u = v[q >> 1];
-    return q & 1 ? widen((int)u.z, (int)u.w, power(scale)) : widen((int)u.x, (int)u.y, power(scale));
+    return q & 1 ? widen((int)u.z, (int)u.w, half_power(scale)) : widen((int)u.x, (int)u.y, half_power(scale));
   };
   struct Wide { bf16x8 x[C::WTM], y[C::WTN]; };
   auto widen_one = [&](Wide& d, const Frags& f, int q, int i, const int (&x)[C::WTM], const int (&y)[C::WTN]) {
@@ -265,6 +270,14 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
 #pragma unroll
   for (int r = 0; r < READS; ++r) read_one(f0, 0, 0, r);
   if constexpr (EXACT) {
+    if (!SLICE && a.bias) {                                  // (not where it is read: that would wait for it before the first loads)
+#pragma unroll
+      for (int i = 0; i < C::WTM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::WTN; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] *= kWidened;
+    }
 #pragma unroll
     for (int i = 0; i < OPERANDS; ++i) widen_one(wide[0], f0, 0, i, sx, sy);
   }
@@ -362,7 +375,10 @@ __global__ __launch_bounds__(C::NT, C::PER_CU) void gemm_fp8_kernel(Fp8Args a) {
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             char* to = wl + l32 * RS + (j * 32 + g * 8 + half * 4) * (int)sizeof(T);
-            if constexpr (F) *reinterpret_cast<float4*>(to) = make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+            if constexpr (F) {
+              constexpr float S = EXACT ? 1.f / kWidened : 1.f;
+              *reinterpret_cast<float4*>(to) = make_float4(v[4 * g] * S, v[4 * g + 1] * S, v[4 * g + 2] * S, v[4 * g + 3] * S);
+            }
             else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(v[4 * g], v[4 * g + 1]), pack_bf16(v[4 * g + 2], v[4 * g + 3]));
           }
         }
@@ -436,12 +452,12 @@ __global__ __launch_bounds__(kRowWaves * 64) void gemm_fp8_rows_kernel(Fp8Args a
   for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto multiply = [&](const Piece& y, const Piece (&x)[MT]) {
     if constexpr (EXACT) {
-      const float sy = power(y.scale);
+      const float sy = half_power(y.scale);
       const bf16x8 y0 = widen((int)y.lo.x, (int)y.lo.y, sy), y1 = widen((int)y.lo.z, (int)y.lo.w, sy);
       const bf16x8 y2 = widen((int)y.hi.x, (int)y.hi.y, sy), y3 = widen((int)y.hi.z, (int)y.hi.w, sy);
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        const float sx = power(x[i].scale);
+        const float sx = half_power(x[i].scale);
         acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y0, widen((int)x[i].lo.x, (int)x[i].lo.y, sx), acc[i], 0, 0, 0);
         acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y1, widen((int)x[i].lo.z, (int)x[i].lo.w, sx), acc[i], 0, 0, 0);
         acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y2, widen((int)x[i].hi.x, (int)x[i].hi.y, sx), acc[i], 0, 0, 0);
@@ -492,7 +508,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void gemm_fp8_rows_kernel(Fp8Args a
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) sums[wave][i][r16][part * 4 + r] = acc[i][r];
+    for (int r = 0; r < 4; ++r) sums[wave][i][r16][part * 4 + r] = acc[i][r] * (EXACT ? 1.f / kWidened : 1.f);
   __syncthreads();
   for (int e = threadIdx.x; e < MT * 256; e += WAVES * 64) {
     const int m = e >> 4, c = e & 15;
