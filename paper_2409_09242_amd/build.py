@@ -156,12 +156,14 @@ def build(verbose: bool = True) -> str:
         torch_obj = ex.submit(_compile_torch_module)
         objs = list(ex.map(_compile, srcs))
         check.result()
-        torch_obj = torch_obj.result()
     cmd = [_hipcc(), "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))
-    _link_torch_module(torch_obj)
+    # the library stands by itself where the module cannot be built, and no module of other sources beside it
+    if os.path.exists(TORCH_LIB):
+        os.remove(TORCH_LIB)
+    _link_torch_module(torch_obj.result())
     with open(STAMP, "w") as f:
         f.write(digest + "\n")
     if verbose:
