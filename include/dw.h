@@ -348,7 +348,7 @@ int dw_policy_loss(const void* d_logits, int64_t ld, int64_t stride, const int32
  *   norm = sqrt(sum g^2),  c = min(1, max_norm / (norm + 1e-6)),  g' = c g
  * The workers are replicas of one model: tensor j has h_count[j] elements for each of them.
  *   h_grad    host array of k*n_tensors device addresses, worker w's tensor j at w*n_tensors + j; contiguous tensors at any
- *             multiple of their element size; not read (and may be NULL) where the count is 0
+ *             multiple of their element size, none overlapping another; not read (and may be NULL) where the count is 0
  *   h_dtype   [n_tensors] types, or NULL: all are `dtype`
  *   d_out     NULL: clipped in place (a worker whose norm is within max_norm is only read).  Otherwise the gradients stay
  *             and g' goes to [k] vectors of floats, worker w's at w*out_stride, its tensors one behind the other in their

@@ -10,7 +10,7 @@
 // arguments, where the chunks and elements of its tensors begin (once) and their addresses (for each worker).
 //
 // Bound by memory: 8 workers of 50.4e6 elements in bf16 into a flat fp32 gradient: 138 us for the norms (5.9 TB/s), 511 for the
-// packing (4.7 TB/s, twice as many bytes written as read).  The second read is the price of a norm over all of it; the last
+// packing (4.7 TB/s, twice as many bytes written as read); in place 454 for both, all clipped.  The second read is the price of a norm over all of it; the last
 // 256 MB of the first pass are read first by the second, from the chip's cache.
 #include "dw_ops.h"
 

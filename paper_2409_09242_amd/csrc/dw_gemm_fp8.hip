@@ -23,8 +23,8 @@
 // consecutive columns, which leave through a piece of LDS of the wave's own as whole row pieces of 16 bytes a lane.
 // The accumulators start from the bias.  Rows past the end of a matrix repeat the last one; what they give is not written.
 //
-// 8192 cubed: 394 us = 2790 TFLOP/s (fp32 757 us = 1450); 4096 cubed: 56 us = 2450 (105 us = 1310).  16 x 512 x 4096 x 4096: 136 us =
-// 2020, where b alone is 268 MB and comes from memory in pieces of 128 bytes (8 workers, b in the chip's cache: 55 us = 2500).
+// 8192 cubed: 384 us = 2860 TFLOP/s (fp32 730 us = 1510); 4096 cubed: 56 us = 2480 (106 us = 1290).  16 x 512 x 4096 x 4096: 134 us =
+// 2050, where b alone is 268 MB and comes from memory in pieces of 128 bytes (8 workers, b in the chip's cache: 55 us = 2520).
 // What bounds a large product is power: of a block of 128 in a tile of 256 x 256 the matrix instructions take 0.85 us, with
 // zeros for numbers the kernel takes 1.2 and with random ones 1.5, at a lower clock.  Tiles that load their successor while
 // they are written, loads further ahead and shorter rows in more stages change nothing.
@@ -603,8 +603,8 @@ bool rows_kernel(int k, int64_t m, int64_t n, int64_t kp) {
 }
 
 // Slices of the contraction (whole words of scales, 512 numbers) for products with fewer 64 x 64 tiles than compute units,
-// by what they would take: 0.3 us a block of 128 (bf16 0.25, fp32 0.45), and for slices 3.5 us and their sums, written and
-// read, at 2 TB/s.  1024 x 8192, m = 64: 18 us whole, 8.5 in slices; 4096 x 4096, m = 128: 11 whole, 13.4 in two, 15.3 in four.
+// by what they would take: 0.3 us a block of 128 (measured: bf16 0.25, fp32 0.45; one number, so that both results take the same
+// scratch), and for slices 3.5 us and their sums, written and read, at 2 TB/s.  1024 x 8192, m = 64: 18 us whole, 8.5 in slices; 4096 x 4096, m = 128: 11 whole, 13.4 in two, 15.3 in four.
 int slices_of(int k, int64_t m, int64_t n, int64_t blocks) {
   const int64_t tiles = tiles_of(k, m, n, 64), words = ceil_div(blocks, GROUP);
   int best = 1;
@@ -655,7 +655,8 @@ hipError_t launch_fp8_matmul(const Fp8Args& a_, hipStream_t s) {
   }
   if (fp8::large_tiles(a.k, a.m, a.n)) return fp8::launch<fp8::Large>(a, s);
   // Small tiles while they run all at once, two a compute unit (us, 64s and 128s): 4096 x 512 x 4096, 512 of them: 15.0, 23.1 (fp32
-  // 23.8, 28.4); 3 x 700 x 900 x 450, 495: 5.4, 7.1; 2 x 1500 x 700 x 5000, 528: 28.5, 30.4 (fp32 41.3, 36.0); 2048 cubed, 1024: 16.5, 12.6
+  // 23.8, 28.4); 3 x 700 x 900 x 450, 495: 5.4, 7.1; 2 x 1500 x 700 x 5000, 528: 28.5, 30.4 (fp32 41.3, 36.0: the limit is where fp32
+  // turns, which bf16 does a little later); 2048 cubed, 1024: 16.5, 12.6
   if (fp8::tiles_of(a.k, a.m, a.n, 64) > 2 * kCus) return fp8::launch<fp8::Middle>(a, s);
   const int slices = fp8::slices_of(a.k, a.m, a.n, a.kp / fp8::BK);
   if (slices == 1) return fp8::launch<fp8::Small>(a, s);

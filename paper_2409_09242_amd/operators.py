@@ -1,8 +1,9 @@
 """Operators of a language model's training step on the GPU, for k worker replicas in one call: the tensor-level form of
 the library's handle-free entry points (include/dw.h).
 
-Tensors of activations are [k][rows][n] with contiguous rows (any row and worker stride, so views of wider buffers do),
-float32 or bfloat16; parameters and their gradients are float32.  Outputs and scratch are allocated by torch on the
+Tensors of activations are [k][rows][n] with contiguous rows (views of wider buffers do: rows of a worker n or more elements
+apart, workers any number, 0 for an input that they share; rows that are written share no element), float32 or bfloat16;
+parameters and their gradients are float32.  Outputs and scratch are allocated by torch on the
 current stream of the tensors' device, where the work is enqueued; nothing is synchronised.  As with any torch operator,
 a tensor made on another stream has to be waited for, and recorded, by the caller.  Nothing is recorded for autograd: the
 backward passes are calls of their own; tensors that a call writes into count as changed in place, so that a graph which
@@ -78,7 +79,8 @@ def policy_loss(logits, target, old_logp, advantage, weight=None, ref_logp=None,
 def clip_grads(grads, max_norm: float, workers: int = 1, out=None):
     """Clip every worker's gradients to a global 2-norm of at most max_norm; returns the norms before, float32 [workers].
 
-    grads: the tensors of worker 0, then those of worker 1 in the same order and so on (contiguous, float32 or bfloat16).
+    grads: the tensors of worker 0, then those of worker 1 in the same order and so on (contiguous, float32 or bfloat16, each
+    once: none overlaps another).
     They are scaled in place, or left alone with out, float32 [workers][total]: the clipped gradients one behind the other,
     as Handle.update_only takes them."""
     return (_MODULE or _ops()).clip_grads(grads, max_norm, workers, out)
