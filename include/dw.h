@@ -409,6 +409,99 @@ int dw_fp8_linear(const void* d_x, int64_t x_ld, int64_t x_stride, const uint8_t
                   int64_t y_stride, void* d_scratch, size_t scratch_bytes, void* stream);
 
 /*
+ * Rows of a table for tokens, and the gradient of the table:
+ *   y[w][r] = scale T[w][d_token[w][r]],      dT[w][v] = scale sum over r with d_token[w][r] = v of dy[w][r]
+ * A token outside [0, vocab) (padding) gives a row of zeros and adds nothing.
+ *   d_token     [k][rows], contiguous
+ *   d_table     rows of n in `table_dtype`, worker w's row v at w*table_stride + v*table_ld; y in `dtype`
+ *   d_grad      [k][vocab] rows of n floats.  accumulate 0: every row is written, zeros where no token was; 1: the sums are added
+ *               to the rows of the tokens that are there, and the others are not touched
+ * The rows of a token are added in fp32 in the order of r, 32 at a time and those sums in their order: no atomics.
+ */
+int dw_embedding(const int32_t* d_token, const void* d_table, int64_t table_ld, int64_t table_stride, int table_dtype, int k,
+                 int64_t rows, int64_t vocab, int64_t n, int dtype, float scale, void* d_y, int64_t y_ld, int64_t y_stride,
+                 void* stream);
+size_t dw_embedding_grad_scratch_bytes(int k, int64_t rows, int64_t vocab, int64_t n);
+int dw_embedding_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const int32_t* d_token, int k, int64_t rows,
+                      int64_t vocab, int64_t n, int dtype, float scale, int accumulate, float* d_grad, int64_t grad_ld,
+                      int64_t grad_stride, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Dropout: y = residual + m x / q.  m is 1 where a 16-bit number of the counter-based stream is below round((1 - p) 65536), else 0,
+ * and q = round((1 - p) 65536) / 65536, so that y's mean is x's (p comes in steps of 2^-16).  Element j of row r of worker w takes bits
+ * 16 (j mod 4) to 16 (j mod 4) + 15 of mix(key(seed, w, step) + GAMMA*(r*ceil(n/4) + floor(j/4) + 1)), mix, GAMMA and key as for the
+ * Rademacher stream: the mask is stored nowhere, and the backward pass is the same call on dy without a residual.  Give every
+ * dropout of a model a seed of its own, other than the configuration's.
+ *   p           0 <= p <= 1; a dropped element's x is not looked at (an infinity or NaN there leaves no trace)
+ *   d_step      NULL, or a device address of one 64-bit number that is added to `step` when the work runs: a captured graph
+ *               whose caller counts it up draws another mask at every replay
+ *   d_residual  NULL: none.  d_y may be d_x or d_residual itself (same ld and stride)
+ */
+int dw_dropout(const void* d_x, int64_t x_ld, int64_t x_stride, const void* d_residual, int64_t residual_ld,
+               int64_t residual_stride, int k, int64_t rows, int64_t n, int dtype, float p, uint64_t seed, uint64_t step,
+               const uint64_t* d_step, void* d_y, int64_t y_ld, int64_t y_stride, void* stream);
+
+/*
+ * Root-mean-square norm behind the residual's addition:
+ *   h = residual + dropout(x)  (dw_dropout's, in `dtype`),    y = h r gamma,    r = 1/sqrt(mean(h^2) + eps) over a row of n
+ * where h is what is stored, rounded to `dtype`: what the norm's backward pass reads is what it was the norm of.
+ *   d_residual, p ... d_step   as for dw_dropout; NULL and 0: h is x, and d_h may be NULL too
+ *   d_gamma     [k] rows of n floats, worker w's at w*param_stride; NULL: 1
+ *   d_h         NULL: not wanted.  May be d_x or d_residual itself (same ld and stride)
+ *   d_y         the norm in `dtype`; NULL: not wanted
+ *   d_q, d_scale, d_qt, d_scale_t   the norm in 8 bits, as dw_fp8_quantize would write it from the fp32 values of y, and its transposed
+ *               form; NULL: not wanted.  The transposed form is made by a second pass, from h (d_x where h is x) and d_rstd, which it
+ *               then needs
+ *   d_rstd      [k][rows] floats receiving r; NULL: not wanted
+ */
+int dw_rms_norm(const void* d_x, int64_t x_ld, int64_t x_stride, const void* d_residual, int64_t residual_ld,
+                int64_t residual_stride, const float* d_gamma, int64_t param_stride, int k, int64_t rows, int64_t n, int dtype,
+                float eps, float p, uint64_t seed, uint64_t step, const uint64_t* d_step, void* d_h, int64_t h_ld,
+                int64_t h_stride, void* d_y, int64_t y_ld, int64_t y_stride, uint8_t* d_q, uint8_t* d_scale, uint8_t* d_qt,
+                uint8_t* d_scale_t, float* d_rstd, void* stream);
+
+/*
+ * Its backward pass.  With t = h r and a = dy gamma:
+ *   dres = r (a - t mean(a t)) + dh,    dx = dropout(dres) with the forward pass's mask,    dgamma = sum over the worker's rows of dy t
+ *   d_h, d_rstd    as dw_rms_norm left them
+ *   d_dh           the gradient that reaches h from further on; NULL: none
+ *   d_dres         gradient of the residual (and of x without dropout); may be NULL, and may be d_dh or d_dy itself (same ld and stride)
+ *   d_dx           gradient of x where that is another; may be NULL, and may be d_dy itself
+ *   d_dgamma       [k] rows of n floats at w*grad_stride, overwritten; may be NULL
+ */
+size_t dw_rms_norm_grad_scratch_bytes(int k, int64_t rows, int64_t n, int dtype);
+int dw_rms_norm_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const void* d_h, int64_t h_ld, int64_t h_stride,
+                     const float* d_gamma, int64_t param_stride, const float* d_rstd, const void* d_dh, int64_t dh_ld,
+                     int64_t dh_stride, int k, int64_t rows, int64_t n, int dtype, float p, uint64_t seed, uint64_t step,
+                     const uint64_t* d_step, void* d_dres, int64_t dres_ld, int64_t dres_stride, void* d_dx, int64_t dx_ld,
+                     int64_t dx_stride, float* d_dgamma, int64_t grad_stride, void* d_scratch, size_t scratch_bytes,
+                     void* stream);
+
+/*
+ * Logits as a token is drawn from them, for requests in the middle of their answers.  In this order, for token j of a row:
+ *   seen in the request so far                       z := z / repetition where z > 0, else z repetition
+ *   c times in its answer so far, c > 0              z := z - (frequency c + presence)
+ *   with a bias                                      z := z + bias_j
+ *   where the mask's bit is 0                        z := -inf, whatever it was
+ *   d_history     [k][rows] rows of `length` tokens (prompt and answer, in their order), worker w's row r at
+ *                 w*history_stride + r*history_ld (0: shared); tokens outside [0, vocab) count for nothing.  NULL with length 0: none
+ *   d_filled      [k][rows] how many of them there are (less than 0: 0, more than `length`: `length`); NULL: `length`
+ *   d_answer      [k][rows] how many of those are the prompt; NULL: none
+ *   d_repetition, d_presence, d_frequency   [k][rows] floats; NULL: 1, 0, 0
+ *   d_bias        rows of vocab floats; NULL: none.  bias_ld and bias_stride may be 0 (shared by the rows, by the workers)
+ *   d_mask        rows of ceil(vocab/32) words, bit j mod 32 of word j/32 is token j's, 1: allowed; NULL: all are.  mask_ld and
+ *                 mask_stride (in words) may be 0
+ *   d_out         may be d_logits itself (same ld and stride)
+ * An element that nothing of this applies to is handed on as it is.  A row whose mask allows nothing is -inf throughout.
+ */
+#define DW_MAX_HISTORY (1 << 24)
+int dw_adjust_logits(const void* d_logits, int64_t ld, int64_t stride, const int32_t* d_history, int64_t history_ld,
+                     int64_t history_stride, int64_t length, const int32_t* d_filled, const int32_t* d_answer,
+                     const float* d_repetition, const float* d_presence, const float* d_frequency, const float* d_bias,
+                     int64_t bias_ld, int64_t bias_stride, const uint32_t* d_mask, int64_t mask_ld, int64_t mask_stride, int k,
+                     int64_t rows, int64_t vocab, int dtype, void* d_out, int64_t out_ld, int64_t out_stride, void* stream);
+
+/*
  * Per-kernel timing for benchmarks (not part of the method).  While enabled, every kernel the handle launches
  * is bracketed by two HIP events on the caller's stream.  dw_profile_read synchronises the stream and returns,
  * per kernel class, the number of launches and their summed duration in milliseconds since the last read

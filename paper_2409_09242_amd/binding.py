@@ -31,7 +31,8 @@ EXPORTS = ("dw_strerror", "dw_last_hip_error", "dw_param_count", "dw_workspace_b
            "dw_overlap_partition_static", "dw_layer_norm", "dw_layer_norm_grad_scratch_bytes", "dw_layer_norm_grad",
            "dw_token_logp", "dw_policy_loss_scratch_bytes", "dw_policy_loss", "dw_clip_grads_scratch_bytes", "dw_clip_grads",
            "dw_fp8_quantize", "dw_fp8_matmul_scratch_bytes", "dw_fp8_matmul",
-           "dw_fp8_linear_scratch_bytes", "dw_fp8_linear")
+           "dw_fp8_linear_scratch_bytes", "dw_fp8_linear", "dw_embedding", "dw_embedding_grad_scratch_bytes", "dw_embedding_grad",
+           "dw_dropout", "dw_rms_norm", "dw_rms_norm_grad_scratch_bytes", "dw_rms_norm_grad", "dw_adjust_logits")
 KERNEL_CLASSES = ("rademacher", "gemm_fwd", "head", "gemm_wgrad", "gemm_dgrad", "update", "weights", "pull", "gather", "step")
 
 
@@ -68,7 +69,7 @@ def lib() -> C.CDLL:
         raise RuntimeError("libdw.so is missing: build it with `python -m paper_2409_09242_amd.build` "
                            "(there is no fallback path)")
     L = C.CDLL(LIB_PATH)
-    vp, i32, i64 = C.c_void_p, C.c_int, C.c_int64
+    vp, i32, i64, u64 = C.c_void_p, C.c_int, C.c_int64, C.c_uint64
     L.dw_strerror.restype = C.c_char_p; L.dw_strerror.argtypes = [i32]
     L.dw_last_hip_error.restype = i32; L.dw_last_hip_error.argtypes = []
     L.dw_param_count.restype = i32; L.dw_param_count.argtypes = [C.POINTER(dw_config), C.POINTER(i64)]
@@ -119,6 +120,25 @@ def lib() -> C.CDLL:
     L.dw_fp8_linear_scratch_bytes.argtypes = [i32, i64, i64, i64]
     L.dw_fp8_linear.restype = i32
     L.dw_fp8_linear.argtypes = [vp, i64, i64, vp, vp, vp, i64, i32, i64, i64, i64, i32, vp, i64, i64, vp, sz, vp]
+    L.dw_embedding.restype = i32
+    L.dw_embedding.argtypes = [vp, vp, i64, i64, i32, i32, i64, i64, i64, i32, f32, vp, i64, i64, vp]
+    L.dw_embedding_grad_scratch_bytes.restype = sz
+    L.dw_embedding_grad_scratch_bytes.argtypes = [i32, i64, i64, i64]
+    L.dw_embedding_grad.restype = i32
+    L.dw_embedding_grad.argtypes = [vp, i64, i64, vp, i32, i64, i64, i64, i32, f32, i32, vp, i64, i64, vp, sz, vp]
+    L.dw_dropout.restype = i32
+    L.dw_dropout.argtypes = [vp, i64, i64, vp, i64, i64, i32, i64, i64, i32, f32, u64, u64, vp, vp, i64, i64, vp]
+    L.dw_rms_norm.restype = i32
+    L.dw_rms_norm.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i32, i64, i64, i32, f32, f32, u64, u64, vp, vp, i64, i64, vp,
+                              i64, i64, vp, vp, vp, vp, vp, vp]
+    L.dw_rms_norm_grad_scratch_bytes.restype = sz
+    L.dw_rms_norm_grad_scratch_bytes.argtypes = [i32, i64, i64, i32]
+    L.dw_rms_norm_grad.restype = i32
+    L.dw_rms_norm_grad.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, vp, vp, i64, i64, i32, i64, i64, i32, f32, u64, u64, vp,
+                                   vp, i64, i64, vp, i64, i64, vp, i64, vp, sz, vp]
+    L.dw_adjust_logits.restype = i32
+    L.dw_adjust_logits.argtypes = [vp, i64, i64, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, i64, vp, i64, i64, i32, i64, i64,
+                                   i32, vp, i64, i64, vp]
     _LIB = L
     return L
 

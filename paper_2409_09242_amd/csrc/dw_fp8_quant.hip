@@ -41,7 +41,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
 
 constexpr int kTileThreads = 512, kRows = 4;                // rows of a thread
 
-template <class E, bool SQUARE>
+// NORM: the numbers are x rstd gamma, a root-mean-square norm whose rows' factors are known (multiplied anew where they are used
+// next, like the unpacking)
+template <class E, bool SQUARE, bool NORM>
 __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a) {
   constexpr int WAVES = kTileThreads / 64;
   __shared__ uint32_t tops[WAVES][128];
@@ -62,6 +64,25 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
     if (r < a.rows) raw[i].load(x + r * a.x.ld, c0 + tc * 8, a.n);
     else raw[i].zero();
   }
+  float by_row[kRows], by_col[8];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) by_row[i] = NORM && r0 + tr * kRows + i < a.rows ? a.rstd[w * a.rows + r0 + tr * kRows + i] : 1.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) by_col[j] = 1.f;
+  if constexpr (NORM)
+    if (a.gamma) load_floats<8>(a.gamma + w * a.gamma_stride, c0 + tc * 8, a.n, 0.f, by_col);
+  auto values = [&](int i, float (&f)[8]) {
+    raw[i].floats(f);
+    if constexpr (NORM) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = f[j] * by_row[i] * by_col[j];
+    }
+  };
+  // (what fills the last block is +0 whatever gamma's sign)
+  auto one = [&](int i, int j) {
+    if constexpr (NORM) return r0 + tr * kRows + i < a.rows ? raw[i].one(j) * by_row[i] * by_col[j] : 0.f;
+    else return raw[i].one(j);
+  };
   uint32_t row_top[kRows], col_top[8];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) row_top[i] = 0;
@@ -70,7 +91,7 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
     float f[8];
-    raw[i].floats(f);
+    values(i, f);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t m = magnitude(f[j]);
@@ -100,7 +121,7 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
       if (r < a.rows) {
         const int64_t row = w * a.rows + r;
         float f[8];
-        raw[i].floats(f);
+        values(i, f);
         *reinterpret_cast<uint2*>(a.q + row * np + c0 + tc * 8) = to_e4m3(f, s.inverse);
         uint8_t* sc = a.scale + row * ns;
         if (tc == 0) sc[blockIdx.x] = (uint8_t)s.byte;
@@ -137,8 +158,8 @@ __global__ __launch_bounds__(kTileThreads) void quantize_tile_kernel(QuantArgs a
   for (int j = 0; j < 8; ++j) {
     const float inv = SQUARE ? all.inverse : inverse[tc * 8 + j];
     int v = 0;
-    v = __builtin_amdgcn_cvt_pk_fp8_f32(raw[0].one(j) * inv, raw[1].one(j) * inv, v, false);
-    v = __builtin_amdgcn_cvt_pk_fp8_f32(raw[2].one(j) * inv, raw[3].one(j) * inv, v, true);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(one(0, j) * inv, one(1, j) * inv, v, false);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(one(2, j) * inv, one(3, j) * inv, v, true);
     tile[tc * 8 + j][tr ^ ((tc & 7) << 2)] = (uint32_t)v;
   }
   __syncthreads();
@@ -170,8 +191,9 @@ hipError_t quantize(const QuantArgs& a, hipStream_t s) {
   const int64_t tiles = DW_FP8_ROW(a.n) / 128 * (DW_FP8_ROW(a.rows) / 128) * a.k;
   const int forms = a.q && a.qt && tiles <= kCus ? 2 : 1;
   const dim3 grid((unsigned)(DW_FP8_ROW(a.n) / 128), (unsigned)(DW_FP8_ROW(a.rows) / 128), (unsigned)(a.k * forms));
-  if (a.square) hipLaunchKernelGGL((quantize_tile_kernel<E, true>), grid, dim3(kTileThreads), 0, s, a);
-  else hipLaunchKernelGGL((quantize_tile_kernel<E, false>), grid, dim3(kTileThreads), 0, s, a);
+  if (a.rstd) hipLaunchKernelGGL((quantize_tile_kernel<E, false, true>), grid, dim3(kTileThreads), 0, s, a);
+  else if (a.square) hipLaunchKernelGGL((quantize_tile_kernel<E, true, false>), grid, dim3(kTileThreads), 0, s, a);
+  else hipLaunchKernelGGL((quantize_tile_kernel<E, false, false>), grid, dim3(kTileThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -177,7 +177,7 @@ __device__ __forceinline__ void row_sum2(float x, float y, float* lds, int& turn
   sy = y;
 }
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---- layer norm (dw_norm.hip) ----------------------------------------------------------------------------------------
 struct Rows { const void* p; int64_t ld, stride; };        // element (w, r, j) at p + w*stride + r*ld + j, in elements
@@ -262,6 +262,8 @@ struct QuantArgs {
   int64_t rows, n;
   uint8_t* q; uint8_t* scale;                              // [k][rows][DW_FP8_ROW(n)], [k][rows][DW_FP8_SCALES(n)], or nullptr
   uint8_t* qt; uint8_t* scale_t;                           // [k][n][DW_FP8_ROW(rows)], [k][n][DW_FP8_SCALES(rows)], or nullptr
+  const float* rstd;                                       // [k][rows]: the numbers are x rstd gamma (x alone where nullptr)
+  const float* gamma; int64_t gamma_stride;                // [k] rows of n, or nullptr: 1
 };
 hipError_t launch_fp8_quantize(const QuantArgs& a, int dtype, hipStream_t s);
 
@@ -279,5 +281,86 @@ size_t fp8_scratch_bytes(int k, int64_t m, int64_t n, int64_t kp);
 hipError_t launch_fp8_matmul(const Fp8Args& a, hipStream_t s);
 bool fp8_linear_fused(int k, int64_t m, int64_t n, int64_t kp);
 hipError_t launch_fp8_linear_fused(const Fp8Args& a, hipStream_t s);
+
+// ---- dropout (dw_dropout.hip, dw_dropout.h) --------------------------------------------------------------------------
+struct Drop {
+  uint64_t seed, step;
+  const uint64_t* d_step;                                  // nullptr, or what is added to step
+  uint32_t limit;                                          // kept: a 16-bit number below it (65536: everything, no dropout)
+  float factor;                                            // of what is kept
+};
+struct DropoutArgs {
+  Rows x, res;                                             // res.p = nullptr: none
+  RowsOut y;
+  Drop drop;
+  int k;
+  int64_t rows, n;
+};
+hipError_t launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s);
+
+// ---- root-mean-square norm (dw_rms.hip) --------------------------------------------------------------------------------
+struct RmsArgs {
+  Rows x, res;                                             // res.p = nullptr: none
+  Drop drop;
+  const float* gamma; int64_t param_stride;
+  RowsOut h, y;                                            // p = nullptr: not wanted
+  uint8_t* q; uint8_t* scale;                              // y in 8 bits, or nullptr
+  float* rstd;                                             // [k][rows], or nullptr
+  int k;
+  int64_t rows, n;
+  float eps;
+};
+hipError_t launch_rms_norm(const RmsArgs& a, int dtype, hipStream_t s);
+
+struct RmsGradArgs {
+  Rows dy, h, dh;                                          // dh.p = nullptr: none
+  Drop drop;
+  const float* gamma; int64_t param_stride;
+  const float* rstd;                                       // [k][rows]
+  RowsOut dres, dx;                                        // p = nullptr: not wanted
+  float* dgamma; int64_t grad_stride;                      // nullptr: not wanted
+  float* part;                                             // [k][strips][n]
+  int k, strips;
+  int64_t rows, n;
+};
+int rms_norm_grad_strips(int k, int64_t rows, int64_t n, int dtype);
+hipError_t launch_rms_norm_grad(const RmsGradArgs& a, int dtype, hipStream_t s);
+
+// ---- embedding (dw_embed.hip) ------------------------------------------------------------------------------------------
+struct EmbedArgs {
+  const int32_t* token;                                    // [k][rows]
+  Rows table;
+  RowsOut y;
+  int k;
+  int64_t rows, vocab, n;
+  float scale;
+};
+hipError_t launch_embedding(const EmbedArgs& a, int table_dtype, int dtype, hipStream_t s);
+
+struct EmbedGradArgs {
+  const int32_t* token;                                    // [k][rows]
+  Rows dy;
+  float* grad; int64_t grad_ld, grad_stride;
+  int k, accumulate;
+  int64_t rows, vocab, n;
+  float scale;
+  char* scratch;
+};
+size_t embedding_grad_scratch(int k, int64_t rows, int64_t vocab, int64_t n);
+hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, hipStream_t s);
+
+// ---- logits before a token is drawn (dw_adjust.hip) --------------------------------------------------------------------
+struct AdjustArgs {
+  Rows logits;
+  RowsOut out;
+  const int32_t* history; int64_t history_ld, history_stride, length;
+  const int32_t* filled; const int32_t* answer;            // [k][rows] each, or nullptr
+  const float* repetition; const float* presence; const float* frequency;
+  const float* bias; int64_t bias_ld, bias_stride;
+  const uint32_t* mask; int64_t mask_ld, mask_stride;
+  int k;
+  int64_t rows, vocab;
+};
+hipError_t launch_adjust_logits(const AdjustArgs& a, int dtype, hipStream_t s);
 
 }  // namespace dw

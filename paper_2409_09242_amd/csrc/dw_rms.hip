@@ -1,0 +1,439 @@
+// Root-mean-square norm of the rows of k workers behind the residual's addition and a dropout, its output in 8 bits, and its
+// backward pass (gfx950, wave64).
+//
+//   h = residual + dropout(x),   y = h r gamma,   r = 1 / sqrt(mean(h^2) + eps)            over a row of n
+//   with t = h r and a = dy gamma:
+//   dres = r (a - t mean(a t)) + dh,   dx = dropout(dres),   dgamma = sum over rows of dy t
+//
+// TPR threads share a row and keep it in registers as ITEMS pieces of 16 bytes each, so x and the residual are read once; h is
+// rounded as it is stored before it is squared, so that the backward pass reads what the norm was taken of.  Sums over a row go
+// through the lanes and, above a wave, through LDS, in fp32.
+//
+// In 8 bits a block of 128 columns lies in 16 (bf16) or 32 (fp32) neighbouring lanes: its largest magnitude is found by lane
+// moves and the bytes leave from registers, without a trip of y through memory.  The transposed form needs 128 rows at once and is
+// the quantiser's own kernel, which multiplies h by r and gamma as it loads it.
+//
+// Backward: a group of threads takes every strips-th row of one worker and keeps its column sums in registers; one row of partial
+// sums per block goes to scratch, and a second kernel adds those up in their order.
+#include "dw_dropout.h"
+#include "dw_fp8.h"
+
+namespace dw {
+
+namespace {
+
+inline int64_t blocks_per_worker(int k, int64_t rows, int groups, int64_t target) {
+  const int64_t most = ceil_div(rows, groups), share = target > k ? target / k : 1;
+  return most < share ? most : share;
+}
+
+// one piece of h: x, dropped, the residual added, rounded as it is stored
+template <class E>
+__device__ __forceinline__ void piece_of_h(const typename E::T* x, const typename E::T* res, const DropKey& key, bool drop, int64_t r,
+                                           int64_t groups, int64_t e0, int64_t n, float (&f)[E::V]) {
+  load_floats16<E>(x, e0, n, f);
+  if (drop) key.piece<E::V>(r, groups, e0, f);
+  if (res) {
+    float b[E::V];
+    load_floats16<E>(res, e0, n, b);
+#pragma unroll
+    for (int j = 0; j < E::V; ++j) f[j] += b[j];
+  }
+  if (drop || res) as_stored<E>(f);
+}
+
+// the largest magnitude of the lanes that share a block of 128 columns, to all of them
+template <class E>
+__device__ __forceinline__ uint32_t block_top(const float (&f)[E::V]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < E::V; ++j) top = larger(top, magnitude(f[j]));
+  top = largest_of_16(top);
+  if constexpr (E::V == 4) top = larger(top, (uint32_t)__shfl_xor((int)top, 16));
+  return top;
+}
+
+// y of one piece in 8 bits: numbers, and the block's scale by its first lane (and what fills the last word of scales)
+template <class E>
+__device__ __forceinline__ void put_eight(uint8_t* q, uint8_t* scale, int64_t e0, int64_t n, const float (&y)[E::V]) {
+  const int64_t np = DW_FP8_ROW(n), ns = DW_FP8_SCALES(n);
+  const Scale s = scale_of(block_top<E>(y));
+  if (e0 >= np) return;
+  int lo = 0;
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * s.inverse, y[1] * s.inverse, lo, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * s.inverse, y[3] * s.inverse, lo, true);
+  if constexpr (E::V == 8) {
+    int hi = 0;
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4] * s.inverse, y[5] * s.inverse, hi, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6] * s.inverse, y[7] * s.inverse, hi, true);
+    *reinterpret_cast<uint2*>(q + e0) = make_uint2((uint32_t)lo, (uint32_t)hi);
+  } else {
+    *reinterpret_cast<uint32_t*>(q + e0) = (uint32_t)lo;
+  }
+  const int64_t b = e0 >> 7;
+  if ((e0 & 127) == 0) {
+    scale[b] = (uint8_t)s.byte;
+    if (b == np / 128 - 1)
+      for (int64_t i = b + 1; i < ns; ++i) scale[i] = 127;
+  }
+}
+
+template <class E, int TPR, int ITEMS, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void rms_norm_kernel(RmsArgs a) {
+  constexpr int V = E::V, GROUPS = BLOCK / TPR;
+  __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)];
+  int turn = 0;
+  const int w = blockIdx.y, t = GROUPS == 1 ? threadIdx.x : threadIdx.x % TPR, g = GROUPS == 1 ? 0 : threadIdx.x / TPR;
+  const int64_t n = a.n, groups = ceil_div(n, 4), np = DW_FP8_ROW(n), ns = DW_FP8_SCALES(n);
+  const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
+  const typename E::T* res = reinterpret_cast<const typename E::T*>(a.res.p) + w * a.res.stride;
+  typename E::T* h = reinterpret_cast<typename E::T*>(a.h.p) + w * a.h.stride;
+  typename E::T* y = reinterpret_cast<typename E::T*>(a.y.p) + w * a.y.stride;
+  const float* gamma = a.gamma ? a.gamma + w * a.param_stride : nullptr;
+  const bool drop = a.drop.limit < 65536u;
+  const DropKey key(a.drop, w);
+  const float inv_n = 1.f / (float)n;
+  for (int64_t r = (int64_t)blockIdx.x * GROUPS + g; r < a.rows; r += (int64_t)gridDim.x * GROUPS) {
+    float v[ITEMS][V];
+    float sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int64_t e0 = (int64_t)(i * TPR + t) * V;
+      piece_of_h<E>(x + r * a.x.ld, a.res.p ? res + r * a.res.ld : nullptr, key, drop, r, groups, e0, n, v[i]);
+#pragma unroll
+      for (int j = 0; j < V; ++j) sq += v[i][j] * v[i][j];
+      if (a.h.p) store16<E>(h + r * a.h.ld, e0, n, v[i]);
+    }
+    const float rstd = 1.f / sqrtf(row_sum<TPR>(sq, red, turn) * inv_n + a.eps);
+    if (t == 0 && a.rstd) a.rstd[w * a.rows + r] = rstd;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int64_t e0 = (int64_t)(i * TPR + t) * V;
+      float ga[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) ga[j] = 1.f;
+      if (gamma) load_floats<V>(gamma, e0, n, 0.f, ga);
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * rstd * ga[j];
+      if (a.y.p) store16<E>(y + r * a.y.ld, e0, n, v[i]);
+      if (a.q) put_eight<E>(a.q + (w * a.rows + r) * np, a.scale + (w * a.rows + r) * ns, e0, n, v[i]);
+    }
+  }
+}
+
+// rows too long for registers: a block goes over the row twice, the second time over h where that was stored (each thread what it
+// wrote itself: h may be the residual or x)
+template <class E>
+__global__ __launch_bounds__(1024) void rms_norm_long_kernel(RmsArgs a) {
+  constexpr int V = E::V, TPR = 1024;
+  __shared__ float red[2 * TPR / 64];
+  int turn = 0;
+  const int w = blockIdx.y, t = threadIdx.x;
+  const int64_t n = a.n, groups = ceil_div(n, 4), np = DW_FP8_ROW(n), ns = DW_FP8_SCALES(n);
+  const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
+  const typename E::T* res = reinterpret_cast<const typename E::T*>(a.res.p) + w * a.res.stride;
+  typename E::T* h = reinterpret_cast<typename E::T*>(a.h.p) + w * a.h.stride;
+  typename E::T* y = reinterpret_cast<typename E::T*>(a.y.p) + w * a.y.stride;
+  const float* gamma = a.gamma ? a.gamma + w * a.param_stride : nullptr;
+  const bool drop = a.drop.limit < 65536u;
+  const DropKey key(a.drop, w);
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    float v[V], sq = 0.f;
+    auto fresh = [&](int64_t e0) { piece_of_h<E>(x + r * a.x.ld, a.res.p ? res + r * a.res.ld : nullptr, key, drop, r, groups, e0, n, v); };
+    for (int64_t e0 = (int64_t)t * V; e0 < n; e0 += TPR * V) {
+      fresh(e0);
+#pragma unroll
+      for (int j = 0; j < V; ++j) sq += v[j] * v[j];
+      if (a.h.p) store16<E>(h + r * a.h.ld, e0, n, v);
+    }
+    const float rstd = 1.f / sqrtf(row_sum<TPR>(sq, red, turn) * (1.f / (float)n) + a.eps);
+    if (t == 0 && a.rstd) a.rstd[w * a.rows + r] = rstd;
+    // (whole blocks of 128: the lanes that share one stay together, and a row in 8 bits is written to its end)
+    for (int64_t e0 = (int64_t)t * V; e0 < np; e0 += TPR * V) {
+      if (a.h.p) load_floats16<E>(h + r * a.h.ld, e0, n, v);
+      else fresh(e0);
+      float ga[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) ga[j] = 1.f;
+      if (gamma) load_floats<V>(gamma, e0, n, 0.f, ga);
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = v[j] * rstd * ga[j];
+      if (a.y.p) store16<E>(y + r * a.y.ld, e0, n, v);
+      if (a.q) put_eight<E>(a.q + (w * a.rows + r) * np, a.scale + (w * a.rows + r) * ns, e0, n, v);
+    }
+  }
+}
+
+template <class E, int TPR, int ITEMS, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void rms_norm_grad_kernel(RmsGradArgs a) {
+  constexpr int V = E::V, GROUPS = BLOCK / TPR, COLS = TPR * ITEMS * V;
+  __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)];
+  __shared__ float cols[GROUPS > 1 ? GROUPS * COLS : 1];
+  int turn = 0;
+  const int w = blockIdx.y, t = GROUPS == 1 ? threadIdx.x : threadIdx.x % TPR, g = GROUPS == 1 ? 0 : threadIdx.x / TPR;
+  const int64_t n = a.n, groups = ceil_div(n, 4);
+  const typename E::T* dy = reinterpret_cast<const typename E::T*>(a.dy.p) + w * a.dy.stride;
+  const typename E::T* h = reinterpret_cast<const typename E::T*>(a.h.p) + w * a.h.stride;
+  const typename E::T* dh = reinterpret_cast<const typename E::T*>(a.dh.p) + w * a.dh.stride;
+  typename E::T* dres = reinterpret_cast<typename E::T*>(a.dres.p) + w * a.dres.stride;
+  typename E::T* dx = reinterpret_cast<typename E::T*>(a.dx.p) + w * a.dx.stride;
+  const float* gamma = a.gamma ? a.gamma + w * a.param_stride : nullptr;
+  const DropKey key(a.drop, w);
+  const float inv_n = 1.f / (float)n;
+  float dg[ITEMS][V];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+    for (int j = 0; j < V; ++j) dg[i][j] = 0.f;
+  for (int64_t r = (int64_t)blockIdx.x * GROUPS + g; r < a.rows; r += (int64_t)gridDim.x * GROUPS) {
+    const float rstd = a.rstd[w * a.rows + r];
+    float v[ITEMS][V], u[ITEMS][V], sum = 0.f;             // a, and t
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int64_t e0 = (int64_t)(i * TPR + t) * V;
+      float ga[V];
+      load_floats16<E>(dy + r * a.dy.ld, e0, n, v[i]);
+      load_floats16<E>(h + r * a.h.ld, e0, n, u[i]);
+#pragma unroll
+      for (int j = 0; j < V; ++j) ga[j] = 1.f;
+      if (gamma) load_floats<V>(gamma, e0, n, 0.f, ga);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        u[i][j] *= rstd;
+        dg[i][j] += v[i][j] * u[i][j];
+        v[i][j] *= ga[j];
+        sum += v[i][j] * u[i][j];
+      }
+    }
+    if (!a.dres.p && !a.dx.p) continue;
+    const float c = row_sum<TPR>(sum, red, turn) * inv_n;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int64_t e0 = (int64_t)(i * TPR + t) * V;
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[i][j] = rstd * (v[i][j] - u[i][j] * c);
+      if (a.dh.p) {
+        float b[V];
+        load_floats16<E>(dh + r * a.dh.ld, e0, n, b);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[i][j] += b[j];
+      }
+      if (a.dres.p) store16<E>(dres + r * a.dres.ld, e0, n, v[i]);
+      if (a.dx.p) {
+        key.piece<V>(r, groups, e0, v[i]);
+        store16<E>(dx + r * a.dx.ld, e0, n, v[i]);
+      }
+    }
+  }
+  if (!a.part) return;
+  float* out = a.part + ((int64_t)w * gridDim.x + blockIdx.x) * n;
+  if constexpr (GROUPS == 1) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if ((int64_t)(i * TPR + t) * V + j < n) out[(int64_t)(i * TPR + t) * V + j] = dg[i][j];
+  } else {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j) cols[g * COLS + (i * TPR + t) * V + j] = dg[i][j];
+    __syncthreads();
+    for (int e = threadIdx.x; e < n; e += BLOCK) {
+      float s = cols[e];
+#pragma unroll
+      for (int q = 1; q < GROUPS; ++q) s += cols[q * COLS + e];
+      out[e] = s;
+    }
+  }
+}
+
+// column sums for rows too long for registers: a thread owns V columns, a block every strips-th row.  It runs first: the row
+// kernel may write over dy
+template <class E>
+__global__ __launch_bounds__(256) void rms_norm_cols_kernel(RmsGradArgs a) {
+  constexpr int V = E::V;
+  const int w = blockIdx.z;
+  const int64_t n = a.n, e0 = ((int64_t)blockIdx.y * 256 + threadIdx.x) * V;
+  if (e0 >= n) return;
+  const typename E::T* dy = reinterpret_cast<const typename E::T*>(a.dy.p) + w * a.dy.stride;
+  const typename E::T* h = reinterpret_cast<const typename E::T*>(a.h.p) + w * a.h.stride;
+  float dg[V], u[V], v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) dg[j] = 0.f;
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const float rstd = a.rstd[w * a.rows + r];
+    load_floats16<E>(dy + r * a.dy.ld, e0, n, v);
+    load_floats16<E>(h + r * a.h.ld, e0, n, u);
+#pragma unroll
+    for (int j = 0; j < V; ++j) dg[j] += v[j] * (u[j] * rstd);
+  }
+  float* out = a.part + ((int64_t)w * gridDim.x + blockIdx.x) * n;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (e0 + j < n) out[e0 + j] = dg[j];
+}
+
+template <class E>
+__global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(RmsGradArgs a) {
+  constexpr int V = E::V, TPR = 1024;
+  __shared__ float red[2 * TPR / 64];
+  int turn = 0;
+  const int w = blockIdx.y, t = threadIdx.x;
+  const int64_t n = a.n, groups = ceil_div(n, 4);
+  const typename E::T* dy = reinterpret_cast<const typename E::T*>(a.dy.p) + w * a.dy.stride;
+  const typename E::T* h = reinterpret_cast<const typename E::T*>(a.h.p) + w * a.h.stride;
+  const typename E::T* dh = reinterpret_cast<const typename E::T*>(a.dh.p) + w * a.dh.stride;
+  typename E::T* dres = reinterpret_cast<typename E::T*>(a.dres.p) + w * a.dres.stride;
+  typename E::T* dx = reinterpret_cast<typename E::T*>(a.dx.p) + w * a.dx.stride;
+  const float* gamma = a.gamma ? a.gamma + w * a.param_stride : nullptr;
+  const DropKey key(a.drop, w);
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const float rstd = a.rstd[w * a.rows + r];
+    float v[V], u[V], ga[V], sum = 0.f;
+    auto read = [&](int64_t e0) {
+      load_floats16<E>(dy + r * a.dy.ld, e0, n, v);
+      load_floats16<E>(h + r * a.h.ld, e0, n, u);
+#pragma unroll
+      for (int j = 0; j < V; ++j) ga[j] = 1.f;
+      if (gamma) load_floats<V>(gamma, e0, n, 0.f, ga);
+#pragma unroll
+      for (int j = 0; j < V; ++j) { u[j] *= rstd; v[j] *= ga[j]; }
+    };
+    for (int64_t e0 = (int64_t)t * V; e0 < n; e0 += TPR * V) {
+      read(e0);
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum += v[j] * u[j];
+    }
+    const float c = row_sum<TPR>(sum, red, turn) * (1.f / (float)n);
+    for (int64_t e0 = (int64_t)t * V; e0 < n; e0 += TPR * V) {
+      read(e0);
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = rstd * (v[j] - u[j] * c);
+      if (a.dh.p) {
+        load_floats16<E>(dh + r * a.dh.ld, e0, n, u);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] += u[j];
+      }
+      if (a.dres.p) store16<E>(dres + r * a.dres.ld, e0, n, v);
+      if (a.dx.p) {
+        key.piece<V>(r, groups, e0, v);
+        store16<E>(dx + r * a.dx.ld, e0, n, v);
+      }
+    }
+  }
+}
+
+// dgamma from the blocks' partial sums: 64 columns a block, its 16 waves take every 16th strip each
+__global__ __launch_bounds__(1024) void rms_norm_strips_kernel(RmsGradArgs a) {
+  __shared__ float lds[16][64];
+  const int w = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t n = a.n, e = (int64_t)blockIdx.x * 64 + lane;
+  float s = 0.f;
+  if (e < n)
+    for (int p = wave; p < a.strips; p += 16) s += a.part[((int64_t)w * a.strips + p) * n + e];
+  lds[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && e < n) {
+#pragma unroll
+    for (int q = 1; q < 16; ++q) s += lds[q][lane];
+    a.dgamma[w * a.grad_stride + e] = s;
+  }
+}
+
+// f.template operator()<TPR, ITEMS>() for rows of so many pieces; false: too long.  The lanes that share a block of 128 columns are
+// in one group from 128 / V threads on, which is the fewest with an output in 8 bits (EIGHT)
+template <class E, bool EIGHT, bool WIDE, class F>
+bool for_row(int64_t pieces, F f) {
+  if (!EIGHT && pieces <= 4) f.template operator()<4, 1>();
+  else if ((!EIGHT || E::V == 8) && pieces <= 16) f.template operator()<16, 1>();
+  else if (pieces <= 32) f.template operator()<32, 1>();
+  else if (pieces <= 64) f.template operator()<64, 1>();
+  else if (pieces <= 128) f.template operator()<64, 2>();
+  else if (pieces <= 256) f.template operator()<256, 1>();
+  else if (pieces <= 512) f.template operator()<256, 2>();
+  else if (pieces <= 1024) f.template operator()<512, 2>();
+  else if (pieces <= 2048) f.template operator()<512, 4>();
+  else if constexpr (WIDE) {
+    if (pieces > 4096) return false;
+    f.template operator()<1024, 4>();
+  } else return false;
+  return true;
+}
+constexpr int block_of(int tpr) { return tpr < 256 ? 256 : tpr; }
+
+template <class E>
+struct Forward {
+  const RmsArgs& a;
+  hipStream_t s;
+  template <int TPR, int ITEMS>
+  void operator()() const {
+    constexpr int BLOCK = block_of(TPR);
+    const dim3 grid((unsigned)blocks_per_worker(a.k, a.rows, BLOCK / TPR, 2048 * (int64_t)kCus / BLOCK), (unsigned)a.k);
+    hipLaunchKernelGGL((rms_norm_kernel<E, TPR, ITEMS, BLOCK>), grid, dim3(BLOCK), 0, s, a);
+  }
+};
+template <class E>
+hipError_t forward(const RmsArgs& a, hipStream_t s) {
+  const Forward<E> f{a, s};
+  const bool fits = a.q ? for_row<E, true, true>(DW_FP8_ROW(a.n) / E::V, f) : for_row<E, false, true>(ceil_div(a.n, E::V), f);
+  if (!fits)
+    hipLaunchKernelGGL(rms_norm_long_kernel<E>, dim3((unsigned)blocks_per_worker(a.k, a.rows, 1, 4 * kCus), (unsigned)a.k), dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+
+template <class E> constexpr bool kWideGrad = E::V == 4;
+int64_t grad_blocks(int tpr) { return (tpr >= 1024 ? 1 : tpr >= 256 ? 2 : 4) * (int64_t)kCus; }
+
+template <class E>
+struct Backward {
+  const RmsGradArgs& a;
+  hipStream_t s;
+  template <int TPR, int ITEMS>
+  void operator()() const {
+    constexpr int BLOCK = block_of(TPR);
+    hipLaunchKernelGGL((rms_norm_grad_kernel<E, TPR, ITEMS, BLOCK>), dim3((unsigned)a.strips, (unsigned)a.k), dim3(BLOCK), 0, s, a);
+  }
+};
+struct Strips {
+  int k; int64_t rows; int* strips;
+  template <int TPR, int ITEMS>
+  void operator()() const { *strips = (int)blocks_per_worker(k, rows, block_of(TPR) / TPR, grad_blocks(TPR)); }
+};
+template <class E>
+hipError_t backward(const RmsGradArgs& a, hipStream_t s) {
+  if (for_row<E, false, kWideGrad<E>>(ceil_div(a.n, E::V), Backward<E>{a, s})) return hipGetLastError();
+  if (a.part) {
+    hipLaunchKernelGGL(rms_norm_cols_kernel<E>, dim3((unsigned)a.strips, (unsigned)ceil_div(a.n, 256 * E::V), (unsigned)a.k), dim3(256), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || (!a.dres.p && !a.dx.p)) return e;
+  }
+  hipLaunchKernelGGL(rms_norm_grad_long_kernel<E>, dim3((unsigned)blocks_per_worker(a.k, a.rows, 1, 4 * kCus), (unsigned)a.k), dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(const RmsArgs& a, int dtype, hipStream_t s) {
+  return dtype == DW_BF16 ? forward<Bf16>(a, s) : forward<F32>(a, s);
+}
+
+int rms_norm_grad_strips(int k, int64_t rows, int64_t n, int dtype) {
+  int strips = 0;
+  const Strips count{k, rows, &strips};
+  const bool fits = dtype == DW_BF16 ? for_row<Bf16, false, kWideGrad<Bf16>>(ceil_div(n, Bf16::V), count)
+                                     : for_row<F32, false, kWideGrad<F32>>(ceil_div(n, F32::V), count);
+  return fits ? strips : (int)blocks_per_worker(k, rows, 1, 2 * kCus);
+}
+
+hipError_t launch_rms_norm_grad(const RmsGradArgs& a, int dtype, hipStream_t s) {
+  if (a.rows > 0) {
+    const hipError_t e = dtype == DW_BF16 ? backward<Bf16>(a, s) : backward<F32>(a, s);
+    if (e != hipSuccess) return e;
+  }
+  if (!a.dgamma) return hipSuccess;                        // (no rows: no strips, and the sums are zero)
+  hipLaunchKernelGGL(rms_norm_strips_kernel, dim3((unsigned)ceil_div(a.n, 64), (unsigned)a.k), dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace dw

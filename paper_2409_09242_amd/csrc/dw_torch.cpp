@@ -439,6 +439,259 @@ PyObject* fp8_linear(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- embedding -------------------------------------------------------------------------------------------------------
+
+// token, table, scale, out, bf16 -> y
+PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  expect(n_args, 5);
+  const at::Tensor& table = tensor(a[1], "table");
+  const int table_type = type_of(table, "table");
+  const Matrix mt = matrix(table, "table");
+  On on(table);
+  const at::Device device = table.device();
+  const at::Tensor& token = tensor(a[0], "token");
+  TORCH_CHECK_VALUE(token.dim() == 2, "token has shape ", token.sizes(), ": [k][rows] is wanted");
+  const int64_t k = table.size(0), vocab = table.size(1), n = table.size(2), rows = token.size(1);
+  const void* pt = values(&token, "token", k, rows, at::kInt, device);
+  const double scale = number(a[2]);
+  const at::Tensor y = a[3] == Py_None ? make({k, rows, n}, truth(a[4]) ? at::kBFloat16 : at::kFloat, device) : tensor(a[3], "out");
+  const int type = type_of(y, "out");
+  const Matrix my = matrix_like(y, "out", {k, rows, n}, y.scalar_type(), device);
+  check(dw_embedding(static_cast<const int32_t*>(pt), mt.p, mt.ld, mt.stride, table_type, workers_of(k), rows, vocab, n, type, (float)scale, my.p,
+                     my.ld, my.stride, on.stream),
+        "dw_embedding");
+  written(a[3]);
+  return wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// dy, token, vocab, scale, out, accumulate -> grad
+PyObject* embedding_grad(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  expect(n_args, 6);
+  const at::Tensor& dy = tensor(a[0], "dy");
+  const int type = type_of(dy, "dy");
+  const Matrix mdy = matrix(dy, "dy");
+  On on(dy);
+  const at::Device device = dy.device();
+  const int64_t k = dy.size(0), rows = dy.size(1), n = dy.size(2);
+  const void* token = values(&tensor(a[1], "token"), "token", k, rows, at::kInt, device);
+  const bool given = a[4] != Py_None, accumulate = truth(a[5]);
+  TORCH_CHECK_VALUE(given || a[2] != Py_None, "vocab or out is wanted");
+  TORCH_CHECK_VALUE(given || !accumulate, "out is wanted to add to");
+  if (given) TORCH_CHECK_VALUE(tensor(a[4], "out").dim() == 3, "out has shape ", tensor(a[4], "out").sizes(), ": [k][vocab][n] is wanted");
+  const int64_t vocab = a[2] != Py_None ? whole(a[2]) : tensor(a[4], "out").size(1);
+  TORCH_CHECK_VALUE(vocab >= 1, "a vocabulary of ", vocab);
+  const double scale = number(a[3]);
+  const at::Tensor grad = given ? tensor(a[4], "out") : make({k, vocab, n}, at::kFloat, device);
+  const Matrix mg = matrix_like(grad, "out", {k, vocab, n}, at::kFloat, device);
+  const Scratch scratch(dw_embedding_grad_scratch_bytes(workers_of(k), rows, vocab, n), device);
+  check(dw_embedding_grad(mdy.p, mdy.ld, mdy.stride, static_cast<const int32_t*>(token), workers_of(k), rows, vocab, n, type, (float)scale,
+                          accumulate ? 1 : 0, static_cast<float*>(mg.p), mg.ld, mg.stride, scratch.p, scratch.bytes, on.stream),
+        "dw_embedding_grad");
+  written(a[4]);
+  return wrap(grad);
+  END_HANDLE_TH_ERRORS
+}
+
+// ---- dropout and the norm of the residual stream ----------------------------------------------------------------------
+
+// a dropout's share, seed and step; the step may be a 64-bit number on the device
+struct DropArgs {
+  float p;
+  uint64_t seed, step = 0;
+  const uint64_t* d_step = nullptr;
+  DropArgs(PyObject* share, PyObject* seed_, PyObject* step_, at::Device device) {
+    p = (float)number(share);
+    seed = bits(seed_);
+    if (!THPVariable_Check(step_)) { step = bits(step_); return; }
+    const at::Tensor& t = THPVariable_Unpack(step_);
+    TORCH_CHECK_VALUE(t.scalar_type() == at::kLong && t.numel() == 1 && t.device() == device, "step is ", t.scalar_type(), " ", t.sizes(), " on ",
+                      t.device(), ": a number, or one int64 on ", device, " is wanted");
+    d_step = static_cast<const uint64_t*>(t.data_ptr());
+  }
+  static uint64_t bits(PyObject* o) {
+    const unsigned long long v = PyLong_AsUnsignedLongLongMask(o);
+    if (v == (unsigned long long)-1 && PyErr_Occurred()) throw python_error();
+    return (uint64_t)v;
+  }
+};
+
+// a tensor like x that is only read, or nothing
+Matrix maybe_like(PyObject* o, const char* name, const at::Tensor& x) {
+  const at::Tensor* t = maybe(o, name);
+  return t ? matrix_like(*t, name, x.sizes(), x.scalar_type(), x.device()) : Matrix{nullptr, x.size(2), x.size(1) * x.size(2)};
+}
+
+// x, p, seed, step, residual, out -> y
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  expect(n_args, 6);
+  const at::Tensor& x = tensor(a[0], "x");
+  const int type = type_of(x, "x");
+  const Matrix mx = matrix(x, "x");
+  On on(x);
+  const DropArgs d(a[1], a[2], a[3], x.device());
+  const Matrix mr = maybe_like(a[4], "residual", x);
+  const at::Tensor y = a[5] == Py_None ? make(x.sizes(), x.scalar_type(), x.device()) : tensor(a[5], "out");
+  const Matrix my = matrix_like(y, "out", x.sizes(), x.scalar_type(), x.device());
+  check(dw_dropout(mx.p, mx.ld, mx.stride, mr.p, mr.ld, mr.stride, workers_of(x.size(0)), x.size(1), x.size(2), type, d.p, d.seed, d.step,
+                   d.d_step, my.p, my.ld, my.stride, on.stream),
+        "dw_dropout");
+  written(a[5]);
+  return wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// what both forms of the norm take: x, gamma, eps, residual, p, seed, step, h
+struct RmsCall {
+  const at::Tensor& x;
+  int type;
+  Matrix mx, mr, mh;
+  On on;
+  DropArgs d;
+  Param g;
+  double eps;
+  at::Tensor h;
+  explicit RmsCall(PyObject* const* a)
+      : x(tensor(a[0], "x")), type(type_of(x, "x")), mx(matrix(x, "x")), on(x), d(a[4], a[5], a[6], x.device()),
+        g(param(maybe(a[1], "gamma"), "gamma", x.size(0), x.size(2), x.device())), eps(number(a[2])) {
+    mr = maybe_like(a[3], "residual", x);
+    if (a[7] != Py_None) h = tensor(a[7], "sum_out");
+    else if (mr.p || d.p > 0.f) h = make(x.sizes(), x.scalar_type(), x.device());
+    mh = h.defined() ? matrix_like(h, "sum_out", x.sizes(), x.scalar_type(), x.device()) : Matrix{nullptr, x.size(2), x.size(1) * x.size(2)};
+  }
+  int operator()(const Matrix& my, const at::Tensor& q, const at::Tensor& scale, const at::Tensor& qt, const at::Tensor& scale_t,
+                 const at::Tensor& rstd) {
+    auto at_bytes = [](const at::Tensor& t) { return t.defined() ? static_cast<uint8_t*>(t.data_ptr()) : nullptr; };
+    return dw_rms_norm(mx.p, mx.ld, mx.stride, mr.p, mr.ld, mr.stride, g.p, g.stride, workers_of(x.size(0)), x.size(1), x.size(2), type,
+                       (float)eps, d.p, d.seed, d.step, d.d_step, mh.p, mh.ld, mh.stride, my.p, my.ld, my.stride, at_bytes(q),
+                       at_bytes(scale), at_bytes(qt), at_bytes(scale_t), rstd.defined() ? static_cast<float*>(rstd.data_ptr()) : nullptr,
+                       on.stream);
+  }
+  PyObject* sum() { return h.defined() ? wrap(h) : wrap(x); }
+};
+
+// x, gamma, eps, residual, p, seed, step, sum_out, out, stats -> (y, h, rstd)
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  expect(n_args, 10);
+  RmsCall c(a);
+  const at::Tensor y = a[8] == Py_None ? make(c.x.sizes(), c.x.scalar_type(), c.x.device()) : tensor(a[8], "out");
+  const Matrix my = matrix_like(y, "out", c.x.sizes(), c.x.scalar_type(), c.x.device());
+  at::Tensor rstd;
+  if (truth(a[9])) rstd = make({c.x.size(0), c.x.size(1)}, at::kFloat, c.x.device());
+  check(c(my, {}, {}, {}, {}, rstd), "dw_rms_norm");
+  written(a[7]);
+  written(a[8]);
+  return tuple(wrap(y), c.sum(), wrap_or_none(rstd));
+  END_HANDLE_TH_ERRORS
+}
+
+// x, gamma, eps, residual, p, seed, step, sum_out, stats, transposed -> (q, scale, qt, scale_t, h, rstd)
+PyObject* rms_norm_fp8(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  expect(n_args, 10);
+  RmsCall c(a);
+  const int64_t k = c.x.size(0), rows = c.x.size(1), n = c.x.size(2);
+  const Eight m = make_eight(k, rows, n, c.x.device());
+  const bool transposed = truth(a[9]), stats = truth(a[8]);
+  Eight t;
+  if (transposed) t = make_eight(k, n, rows, c.x.device());
+  at::Tensor rstd;
+  if (stats || transposed) rstd = make({k, rows}, at::kFloat, c.x.device());
+  check(c({nullptr, n, rows * n}, m.q, m.scale, t.q, t.scale, rstd), "dw_rms_norm");
+  written(a[7]);
+  return tuple(wrap(m.q), wrap(m.scale), wrap_or_none(t.q), wrap_or_none(t.scale), c.sum(), stats ? wrap(rstd) : none());
+  END_HANDLE_TH_ERRORS
+}
+
+// dy, h, gamma, rstd, dh, p, seed, step, dres, dx, dgamma, want_dx, want_params -> (dres, dx, dgamma)
+PyObject* rms_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  expect(n_args, 13);
+  const at::Tensor& h = tensor(a[1], "h");
+  const int type = type_of(h, "h");
+  const Matrix mh = matrix(h, "h");
+  On on(h);
+  const at::Device device = h.device();
+  const int64_t k = h.size(0), rows = h.size(1), n = h.size(2);
+  const Matrix mdy = matrix_like(tensor(a[0], "dy"), "dy", h.sizes(), h.scalar_type(), device);
+  const Param g = param(maybe(a[2], "gamma"), "gamma", k, n, device);
+  const void* rstd = values(&tensor(a[3], "rstd"), "rstd", k, rows, at::kFloat, device);
+  const Matrix mdh = maybe_like(a[4], "dh", h);
+  const DropArgs d(a[5], a[6], a[7], device);
+  at::Tensor dres, dx, dgamma;
+  Matrix mres = {nullptr, n, rows * n}, mdx = mres;
+  const bool want = truth(a[11]);
+  if (want) {
+    dres = a[8] == Py_None ? make(h.sizes(), h.scalar_type(), device) : tensor(a[8], "dres");
+    mres = matrix_like(dres, "dres", h.sizes(), h.scalar_type(), device);
+    if (a[9] != Py_None) dx = tensor(a[9], "dx");
+    else if (d.p > 0.f) dx = make(h.sizes(), h.scalar_type(), device);
+    if (dx.defined()) mdx = matrix_like(dx, "dx", h.sizes(), h.scalar_type(), device);
+  }
+  Param dg = {nullptr, n};
+  if (truth(a[12])) {
+    dgamma = a[10] == Py_None ? make({k, n}, at::kFloat, device) : tensor(a[10], "dgamma");
+    dg = param(&dgamma, "dgamma", k, n, device);
+  }
+  const Scratch scratch(dg.p ? dw_rms_norm_grad_scratch_bytes(workers_of(k), rows, n, type) : 0, device);
+  check(dw_rms_norm_grad(mdy.p, mdy.ld, mdy.stride, mh.p, mh.ld, mh.stride, g.p, g.stride, static_cast<const float*>(rstd), mdh.p, mdh.ld,
+                         mdh.stride, workers_of(k), rows, n, type, d.p, d.seed, d.step, d.d_step, mres.p, mres.ld, mres.stride, mdx.p, mdx.ld,
+                         mdx.stride, dg.p, dg.stride, scratch.p, scratch.bytes, on.stream),
+        "dw_rms_norm_grad");
+  if (want) { written(a[8]); written(a[9]); }
+  if (dg.p) written(a[10]);
+  return tuple(wrap_or_none(dres), dx.defined() ? wrap(dx) : wrap_or_none(dres), wrap_or_none(dgamma));
+  END_HANDLE_TH_ERRORS
+}
+
+// ---- logits before a token is drawn ------------------------------------------------------------------------------------
+
+// a [k][rows][n] tensor that is only read, whose rows or workers may be one (strides of zero)
+Matrix shared(const at::Tensor* t, const char* name, int64_t k, int64_t rows, int64_t n, at::ScalarType type, at::Device device) {
+  if (!t) return {nullptr, n, rows * n};
+  TORCH_CHECK_VALUE(t->dim() == 3 && t->size(0) == k && t->size(1) == rows && t->size(2) == n && t->scalar_type() == type && t->device() == device,
+                    name, " is ", t->scalar_type(), " ", t->sizes(), " on ", t->device(), ": ", type, " [", k, "][", rows, "][", n, "] on ", device,
+                    " is wanted");
+  return matrix(*t, name);
+}
+
+// logits, history, filled, answer, repetition, presence, frequency, bias, mask, out -> z
+PyObject* adjust_logits(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  expect(n_args, 10);
+  const at::Tensor& z = tensor(a[0], "logits");
+  const int type = type_of(z, "logits");
+  const Matrix mz = matrix(z, "logits");
+  On on(z);
+  const at::Device device = z.device();
+  const int64_t k = z.size(0), rows = z.size(1), vocab = z.size(2);
+  const at::Tensor* history = maybe(a[1], "history");
+  const int64_t length = history && history->dim() == 3 ? history->size(2) : 0;
+  const Matrix mhist = shared(history, "history", k, rows, length, at::kInt, device);
+  const int32_t* row_i[2];
+  const char* int_names[] = {"filled", "answer"};
+  for (int i = 0; i < 2; ++i)
+    row_i[i] = static_cast<const int32_t*>(values(maybe(a[2 + i], int_names[i]), int_names[i], k, rows, at::kInt, device));
+  const float* row_f[3];
+  const char* names[] = {"repetition", "presence", "frequency"};
+  for (int i = 0; i < 3; ++i) row_f[i] = static_cast<const float*>(values(maybe(a[4 + i], names[i]), names[i], k, rows, at::kFloat, device));
+  const Matrix mb = shared(maybe(a[7], "bias"), "bias", k, rows, vocab, at::kFloat, device);
+  const Matrix mm = shared(maybe(a[8], "mask"), "mask", k, rows, (vocab + 31) / 32, at::kInt, device);
+  const at::Tensor out = a[9] == Py_None ? make(z.sizes(), z.scalar_type(), device) : tensor(a[9], "out");
+  const Matrix mo = matrix_like(out, "out", z.sizes(), z.scalar_type(), device);
+  check(dw_adjust_logits(mz.p, mz.ld, mz.stride, static_cast<const int32_t*>(mhist.p), mhist.ld, mhist.stride, length, row_i[0], row_i[1], row_f[0],
+                         row_f[1], row_f[2], static_cast<const float*>(mb.p), mb.ld, mb.stride, static_cast<const uint32_t*>(mm.p), mm.ld, mm.stride,
+                         workers_of(k), rows, vocab, type, mo.p, mo.ld, mo.stride, on.stream),
+        "dw_adjust_logits");
+  written(a[9]);
+  return wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
 // the class of errors for a negative status
 PyObject* set_error(PyObject*, PyObject* cls) {
   Py_INCREF(cls);
@@ -449,7 +702,9 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 #define DW_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DW_FAST(layer_norm), DW_FAST(layer_norm_grad), DW_FAST(token_logp), DW_FAST(policy_loss), DW_FAST(clip_grads),
-                         DW_FAST(fp8_quantize), DW_FAST(fp8_matmul), DW_FAST(fp8_linear), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         DW_FAST(fp8_quantize), DW_FAST(fp8_matmul), DW_FAST(fp8_linear),
+                         DW_FAST(embedding), DW_FAST(embedding_grad), DW_FAST(dropout), DW_FAST(rms_norm), DW_FAST(rms_norm_fp8), DW_FAST(rms_norm_grad),
+                         DW_FAST(adjust_logits), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dw_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,4 +1,4 @@
-"""Operators of a language model's training step on the GPU, for k worker replicas in one call: the tensor-level form of
+"""Operators of a language model's training step and rollout on the GPU, for k worker replicas in one call: the tensor-level form of
 the library's handle-free entry points (include/dw.h).
 
 Tensors of activations are [k][rows][n] with contiguous rows (views of wider buffers do: rows of a worker n or more elements
@@ -126,3 +126,75 @@ def fp8_matmul(a: Fp8Matrix, b: Fp8Matrix, bias=None, dtype=torch.bfloat16, out=
 def fp8_linear(x, weight: Fp8Matrix, bias=None, out=None):
     """x W^T (+ bias) with x [k][rows][n] quantised on the way and W kept in 8 bits; [k][rows][W's rows] in x's type."""
     return (_MODULE or _ops()).fp8_linear(x, weight.q, weight.scale, weight.n, bias, out)
+
+
+# ---- embedding -------------------------------------------------------------------------------------------------------
+
+def embedding(token, table, scale: float = 1.0, dtype=None, out=None):
+    """scale * table[token], [k][rows][n]: token int32 [k][rows], table [k][vocab][n] (one that the workers share: expanded); zeros
+    for tokens outside the vocabulary.  dtype: of the result, the table's if it is None."""
+    if dtype is None:
+        dtype = getattr(table, "dtype", None)
+    elif dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise ValueError("dtype is %s: float32 or bfloat16 is wanted" % dtype)
+    return (_MODULE or _ops()).embedding(token, table, scale, out, dtype is torch.bfloat16)
+
+
+def embedding_grad(dy, token, vocab=None, scale: float = 1.0, out=None, accumulate: bool = False):
+    """The gradient of embedding's table, float32 [k][vocab][n], from dy [k][rows][n].
+
+    out: where it goes, such as a view of the flat gradient of Handle.update_only; accumulate=True adds to the rows of the tokens
+    that are there and leaves the others alone (a table that the output layer shares)."""
+    return (_MODULE or _ops()).embedding_grad(dy, token, vocab, scale, out, accumulate)
+
+
+# ---- dropout and the norm of the residual stream ----------------------------------------------------------------------
+
+def dropout(x, p: float, seed: int, step=0, residual=None, out=None):
+    """residual + x with a share p of its elements dropped and the others scaled; see dw_dropout.  The mask follows from seed, step and
+    an element's place, so dropout(dy, p, seed, step) is the backward pass.
+
+    step: a number, or one int64 on the device, which is read when the work runs (a captured graph whose caller counts it up
+    draws anew at every replay).  out: a tensor like x, x or the residual themselves among them."""
+    return (_MODULE or _ops()).dropout(x, p, seed, step, residual, out)
+
+
+def rms_norm(x, gamma=None, eps: float = 1e-6, residual=None, p: float = 0.0, seed: int = 0, step=0, sum_out=None, out=None,
+             stats: bool = True):
+    """(y, h, rstd): h = residual + dropout(x), y = h rstd gamma over the last axis, rstd = 1/sqrt(mean(h^2) + eps).
+
+    h is x itself without a residual and a dropout.  gamma: float32 [k][n] or None.  sum_out, out: tensors like x for h and y;
+    sum_out may be x or the residual.  stats=False: rstd is None."""
+    return (_MODULE or _ops()).rms_norm(x, gamma, eps, residual, p, seed, step, sum_out, out, stats)
+
+
+def rms_norm_fp8(x, gamma=None, eps: float = 1e-6, residual=None, p: float = 0.0, seed: int = 0, step=0, sum_out=None,
+                 stats: bool = True, transposed: bool = False):
+    """rms_norm with y in 8 bits, (Fp8Matrix, h, rstd), quantised from the fp32 values; transposed=True: (that, the same of y^T) in its
+    place, as fp8_quantize gives them."""
+    q, scale, qt, scale_t, h, rstd = (_MODULE or _ops()).rms_norm_fp8(x, gamma, eps, residual, p, seed, step, sum_out, stats, transposed)
+    y = Fp8Matrix(q, scale, x.shape[2])
+    return ((y, Fp8Matrix(qt, scale_t, x.shape[1])) if transposed else y), h, rstd
+
+
+def rms_norm_grad(dy, h, gamma, rstd, dh=None, p: float = 0.0, seed: int = 0, step=0, dres=None, dx=None, dgamma=None,
+                  want_dx: bool = True, want_params: bool = True):
+    """(gradient of the residual, of x, of gamma) of rms_norm from dy, the h and rstd it returned, and the gradient dh that reaches h
+    from further on; p, seed and step as they were given to it.
+
+    Without a dropout the first two are one tensor.  dres, dx, dgamma: tensors to write into (dres may be dh or dy, dx dy); what is not
+    wanted is returned as None."""
+    return (_MODULE or _ops()).rms_norm_grad(dy, h, gamma, rstd, dh, p, seed, step, dres, dx, dgamma, want_dx, want_params)
+
+
+# ---- logits before a token is drawn ------------------------------------------------------------------------------------
+
+def adjust_logits(logits, history=None, filled=None, answer=None, repetition=None, presence=None, frequency=None, bias=None, mask=None,
+                  out=None):
+    """Logits [k][rows][vocab] with penalties for tokens of the requests so far, a bias and a grammar's mask; see dw_adjust_logits.
+
+    history: int32 [k][rows][length], of which the first filled (int32 [k][rows]) count, and the first answer (int32 [k][rows])
+    of those are the prompt; repetition, presence, frequency: float32 [k][rows]; bias: float32 [k][rows][vocab]; mask: int32
+    [k][rows][ceil(vocab/32)], a bit a token.  history, bias and mask may be expanded over rows or workers.  out: a tensor like
+    logits, the logits themselves among them."""
+    return (_MODULE or _ops()).adjust_logits(logits, history, filled, answer, repetition, presence, frequency, bias, mask, out)

@@ -1,0 +1,134 @@
+"""Rows of a table and the table's gradient against the formulas in 64 bits.
+
+Bounds (U = 2^-24): a looked-up number is rounded once in fp32 and once to its type; a sum of m rows is off by at most m + 1 roundings of
+the sum of magnitudes (each term goes through at most that many additions in any order, and the scale is one more), and
+one more where it is added to what was there."""
+import pytest
+import torch
+
+from paper_2409_09242_amd import operators as OPS
+from operators_ref import U, out_rounding, padded, within
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+DEV = "cuda:0"
+
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _tokens(k, rows, vocab, g, how="mixed"):
+    """Common and rare tokens, some that are none (before and behind the vocabulary)."""
+    u = torch.rand(k, rows, generator=g, device=DEV, dtype=torch.float64)
+    t = (torch.exp(u * torch.log(torch.tensor(vocab + 1.0, device=DEV, dtype=torch.float64))).long() - 1).clamp(0, vocab - 1)
+    if how == "mixed" and rows > 3:
+        t[:, ::7] = -1
+        t[:, 3::11] = vocab
+        t[:, 5::13] = torch.tensor(-(1 << 31), device=DEV)
+        t[:, 4::17] = (1 << 31) - 1
+    if how == "one":
+        t[:] = vocab // 2
+    if how == "none":
+        t[:] = -1
+    return t.to(torch.int32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("table_dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [1, 3, 4, 7, 8, 9, 31, 64, 100, 257, 1001, 2048, 4096, 5003])
+def test_lookup(n, table_dtype, dtype):
+    g = _gen(n)
+    for k, rows, vocab, pad, lead in ((1, 1, 1, 0, 0), (3, 50, 97, 3, 1), (2, 9, 1000, 0, 3)):
+        table = padded((k, vocab, n), pad, lead, table_dtype, g)
+        token = _tokens(k, rows, vocab, g)
+        out = torch.full((k, rows, n + 2), 7.0, dtype=dtype, device=DEV)
+        y = OPS.embedding(token, table, 1.7, out=out[..., 1:n + 1])
+        ok = (token >= 0) & (token < vocab)
+        want = torch.stack([table[w].double()[token[w].long().clamp(0, vocab - 1)] for w in range(k)]) * float(torch.tensor(1.7)) * ok[..., None]
+        within(y, want, U * want.abs() + out_rounding(dtype) * want.abs() * 1.01, "y")
+        assert bool((out[..., 0] == 7).all()) and bool((out[..., -1] == 7).all())
+        assert torch.equal(OPS.embedding(token, table, 1.7, dtype=dtype), y)
+        if dtype == table_dtype:
+            assert torch.equal(OPS.embedding(token, table, 1.7), y)
+            assert torch.equal(OPS.embedding(token, table)[ok], torch.cat([table[w][token[w][ok[w]].long()] for w in range(k)]))
+        one = table[:1].expand(k, vocab, n)                  # a table that the workers share
+        assert torch.equal(OPS.embedding(token, one, 1.7, dtype=dtype), OPS.embedding(token, one.contiguous(), 1.7, dtype=dtype))
+
+
+def _check_grad(got, dy, token, vocab, scale, old=None):
+    k = dy.shape[0]
+    for w in range(k):
+        ok = (token[w] >= 0) & (token[w] < vocab)
+        at, d = token[w][ok].long(), dy[w][ok].double() * scale
+        want = torch.zeros(vocab, dy.shape[2], dtype=torch.float64, device=DEV).index_add_(0, at, d)
+        size = torch.zeros_like(want).index_add_(0, at, d.abs())
+        m = torch.bincount(at, minlength=vocab)[:, None]
+        bound = (m + 2) * U * size
+        if old is not None:
+            bound = bound + U * (want.abs() + size + old[w].double().abs())
+            want = want + old[w].double()
+            assert torch.equal(got[w][m[:, 0] == 0], old[w][m[:, 0] == 0])
+        within(got[w], want, bound + 1e-38, "worker %d" % w)
+
+
+# rows on both sides of a chunk of places, of a block of counting, of the change of sorts and of its tiles
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k,rows,vocab,n", [(1, 1, 1, 1), (2, 2, 3, 5), (3, 31, 7, 8), (2, 32, 40, 9), (2, 33, 40, 64), (1, 64, 2, 100), (3, 65, 1000, 17),
+                                            (2, 333, 97, 1001), (1, 1000, 5003, 33), (64, 40, 11, 12), (1, 8192, 300, 20), (1, 8193, 300, 20),
+                                            (2, 12289, 255, 7), (2, 9000, 256, 8), (1, 20000, 70000, 6), (1, 70, 30, 5003), (1, 8200, 1 << 24, 1)])
+def test_gradient(k, rows, vocab, n, dtype):
+    g = _gen(rows)
+    for how in ("mixed", "one", "none") if vocab < 1 << 20 else ("mixed",):
+        token = _tokens(k, rows, vocab, g, how)
+        dy = padded((k, rows, n), 3, 1, dtype, g) if how == "mixed" else torch.randn(k, rows, n, generator=g, device=DEV).to(dtype)
+        got = OPS.embedding_grad(dy, token, vocab, 0.5)
+        _check_grad(got, dy, token, vocab, 0.5)
+        assert torch.equal(got, OPS.embedding_grad(dy, token, vocab, 0.5))
+        if vocab * n > 1 << 20:
+            continue
+        flat = torch.full((k, vocab, n + 2), 7.0, device=DEV)
+        view = flat[..., 1:n + 1]
+        OPS.embedding_grad(dy, token, scale=0.5, out=view)   # rows with gaps, as they are
+        assert torch.equal(view, got) and bool((flat[..., 0] == 7).all()) and bool((flat[..., -1] == 7).all())
+        old = torch.randn(k, vocab, n, generator=g, device=DEV)
+        view.copy_(old)
+        OPS.embedding_grad(dy, token, vocab, 0.5, out=view, accumulate=True)
+        _check_grad(view, dy, token, vocab, 0.5, old)
+        assert bool((flat[..., 0] == 7).all()) and bool((flat[..., -1] == 7).all())
+
+
+def test_gradient_of_no_rows():
+    dy, token = torch.empty(2, 0, 30, device=DEV), torch.empty(2, 0, dtype=torch.int32, device=DEV)
+    assert torch.equal(OPS.embedding_grad(dy, token, 9), torch.zeros(2, 9, 30, device=DEV))
+    old = torch.randn(2, 9, 30, device=DEV)
+    kept = old.clone()
+    OPS.embedding_grad(dy, token, out=old, accumulate=True)
+    assert torch.equal(old, kept)
+    assert OPS.embedding(token, old).shape == (2, 0, 30)
+
+
+def test_a_token_alone_in_a_large_batch():
+    """Whole numbers, whose sums are exact whatever their order: one token's rows among many chunks, at both ends and in between."""
+    g = _gen(3)
+    for rows in (500, 40000):
+        dy = torch.randint(-8, 9, (1, rows, 40), generator=g, device=DEV).float()
+        for v, others in ((0, 5), (9, 3), (4, 20)):
+            token = torch.full((1, rows), v, dtype=torch.int32, device=DEV)
+            token[0, ::others] = torch.arange(len(token[0, ::others]), device=DEV, dtype=torch.int32) % 10
+            got = OPS.embedding_grad(dy, token, 10)
+            want = torch.zeros(10, 40, dtype=torch.float64, device=DEV).index_add_(0, token[0].long(), dy[0].double())
+            assert torch.equal(got[0].double(), want)
+
+
+def test_gradient_against_differences():
+    """The lookup is linear in the table: <embedding(T), dy> = <T, embedding_grad(dy)>."""
+    g = _gen(6)
+    token = _tokens(2, 300, 50, g)
+    table, dy = torch.randn(2, 50, 24, generator=g, device=DEV), torch.randn(2, 300, 24, generator=g, device=DEV)
+    left = (OPS.embedding(token, table, 3.0).double() * dy.double()).sum()
+    grad = OPS.embedding_grad(dy, token, 50, 3.0)
+    right = (grad.double() * table.double()).sum()
+    assert abs(float(left - right)) <= 303 * U * float((OPS.embedding(token, table, 3.0).double() * dy.double()).abs().sum())
