@@ -166,7 +166,7 @@ def test_then_a_row_without_a_choice_has_no_probability():
 def test_long_histories(m, dtype):
     """Also alone and in place, where nothing but the history's tokens changes."""
     g = _gen(m)
-    for vocab in (50, 40003):
+    for vocab in (50, 40003, 300000):
         z = torch.randn(1, 3, vocab, generator=g, device=DEV).mul_(3).to(dtype)
         args = _request(1, 3, m, vocab, g)
         got = OPS.adjust_logits(z, *args)
