@@ -416,7 +416,7 @@ int dw_fp8_linear(const void* d_x, int64_t x_ld, int64_t x_stride, const uint8_t
  *   d_table     rows of n in `table_dtype`, worker w's row v at w*table_stride + v*table_ld; y in `dtype`
  *   d_grad      [k][vocab] rows of n floats.  accumulate 0: every row is written, zeros where no token was; 1: the sums are added
  *               to the rows of the tokens that are there, and the others are not touched
- * The rows of a token are added in fp32 in the order of r, 32 at a time and those sums in their order: no atomics.
+ * The rows of a token are added in fp32, in an order that follows from the tokens alone: no atomics.
  */
 int dw_embedding(const int32_t* d_token, const void* d_table, int64_t table_ld, int64_t table_stride, int table_dtype, int k,
                  int64_t rows, int64_t vocab, int64_t n, int dtype, float scale, void* d_y, int64_t y_ld, int64_t y_stride,

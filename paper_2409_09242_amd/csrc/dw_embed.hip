@@ -12,7 +12,13 @@
 //
 // The sort: up to kRankRows places by counting (a place's rank is the number of smaller tokens, and of equal ones before it), which is
 // n^2 comparisons but a single launch; longer lists digit by digit, eight bits at a time from the lowest, in blocks of kTile
-// places whose counts of every digit are added up between the two passes over them.
+// places whose counts of every digit are added up between the two passes over them.  One worker's 8192 places by counting 15 us, by
+// digits (two of them) 34; 65536 places 47.
+//
+// Where the whole gradient is wanted, rows that no token has are filled with zeros beside the last kernel's sums, each row written
+// once.  4 x 4096 rows of 4096, bf16, over 32000 tokens: counting 10 us, sums 62 to 85 (134 MB read, 150 written), the 2 GB of
+// zeros 340 = 5.9 TB/s (a fill alone reaches 6.4); 3 x 333 rows of 1001, fp32, over 5003: 3.0, 6.1, 12.2.  Lookups: 8 x 1024 rows of
+// 4096, fp32 to bf16, 31 us = 6.4 TB/s of what passes (common rows come from the caches); one row 2.0, less than a launch's 2.4.
 #include "dw_ops.h"
 
 namespace dw {
@@ -111,30 +117,50 @@ hipError_t lookup(const EmbedArgs& a, hipStream_t s) {
 
 constexpr int kRankRows = 8192;                            // up to here by counting
 constexpr int kTile = 4096;                                // places of a block when sorting by digits, 1024 a wave
-constexpr int kChunk = 32;                                 // places whose rows a group of threads adds up
+constexpr int kChunk = 16;                                 // places whose rows a group of threads adds up
 
 // what is no token sorts behind all tokens
 __device__ __forceinline__ int32_t key_of(int32_t token, int32_t vocab) { return (uint32_t)token < (uint32_t)vocab ? token : vocab; }
 
-// 64 places a block, their keys against all of the worker's by 16 waves
-__global__ __launch_bounds__(1024) void rank_kernel(const int32_t* token, int32_t* sorted, int32_t* place, int rows, int32_t vocab) {
-  __shared__ int32_t part[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// 64 places a block, their keys against all of the worker's by 16 waves, 64 others at a time: a wave has those in its lanes, all
+// groups on their way at once, and hands them round one after another.  Of places before the block's an equal key counts, of
+// those behind not, and of its own those of lower lanes.
+__global__ __launch_bounds__(1024) void rank_kernel(const int32_t* __restrict__ token, int32_t* __restrict__ sorted, int32_t* __restrict__ place,
+                                                    int rows, int32_t vocab) {
+  constexpr int GROUPS = kRankRows / 1024;
+  __shared__ int part[16][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t* tok = token + (int64_t)blockIdx.y * rows;
-  const int r = blockIdx.x * 64 + lane;
-  const int32_t mine = r < rows ? key_of(tok[r], vocab) : 0;
-  const int per = (rows + 15) / 16, from = wave * per, to = from + per < rows ? from + per : rows;
+  const int own = blockIdx.x, r = own * 64 + lane;
+  const uint32_t last = (uint32_t)vocab;                   // (what is no token is behind it, also as an unsigned number below zero)
+  auto key = [&](int s) { const uint32_t v = (uint32_t)tok[s]; return v < last ? v : last; };
+  uint32_t others[GROUPS];
+#pragma unroll
+  for (int q = 0; q < GROUPS; ++q) {
+    const int s = (wave + q * 16) * 64 + lane;
+    others[q] = s < rows ? key(s) : ~0u;                   // (none: above every key)
+  }
+  const uint32_t mine = r < rows ? key(r) : 0u;
   int rank = 0;
-  for (int s = from; s < to; ++s) {
-    const int32_t other = key_of(tok[s], vocab);
-    rank += other < mine || (other == mine && s < r) ? 1 : 0;
+#pragma unroll
+  for (int q = 0; q < GROUPS; ++q) {
+    const int g = wave + q * 16;
+    if (g * 64 >= rows) break;
+    if (g != own) {
+      const uint32_t limit = g < own ? mine + 1u : mine;
+#pragma unroll
+      for (int i = 0; i < 64; ++i) rank += (uint32_t)__builtin_amdgcn_readlane((int)others[q], i) < limit ? 1 : 0;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 64; ++i) rank += (uint32_t)__builtin_amdgcn_readlane((int)others[q], i) < mine + (i < lane ? 1u : 0u) ? 1 : 0;
+    }
   }
   part[wave][lane] = rank;
   __syncthreads();
   if (wave != 0 || r >= rows) return;
 #pragma unroll
   for (int q = 1; q < 16; ++q) rank += part[q][lane];
-  sorted[(int64_t)blockIdx.y * rows + rank] = mine;
+  sorted[(int64_t)blockIdx.y * rows + rank] = (int32_t)mine;
   place[(int64_t)blockIdx.y * rows + rank] = r;
 }
 
@@ -156,8 +182,9 @@ __global__ __launch_bounds__(256) void digit_count_kernel(Digits d) {
   const int w = blockIdx.y;
   count[threadIdx.x] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < kTile; i += 256) {
-    const int64_t r = (int64_t)blockIdx.x * kTile + i;
+#pragma unroll
+  for (int i = 0; i < kTile / 256; ++i) {
+    const int64_t r = (int64_t)blockIdx.x * kTile + i * 256 + threadIdx.x;
     if (r < d.rows) atomicAdd(&count[(uint32_t)d.key(w, r) >> d.shift & 255u], 1u);
   }
   __syncthreads();
@@ -200,22 +227,28 @@ __global__ __launch_bounds__(256) void digit_place_kernel(Digits d) {
   __shared__ uint32_t next[4][256];
   const int w = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t r0 = (int64_t)blockIdx.x * kTile + wave * 1024;
+  int32_t keys[16], places[16];                            // all on their way at once
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int64_t r = r0 + i * 64 + lane;
+    keys[i] = r < d.rows ? d.key(w, r) : 0;
+    places[i] = d.token ? (int32_t)r : r < d.rows ? d.place_in[w * d.rows + r] : 0;
+  }
 #pragma unroll
   for (int q = 0; q < 4; ++q) next[q][threadIdx.x] = 0;
   __syncthreads();
-  for (int i = 0; i < 16; ++i) {
-    const int64_t r = r0 + i * 64 + lane;
-    if (r < d.rows) atomicAdd(&next[wave][(uint32_t)d.key(w, r) >> d.shift & 255u], 1u);
-  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (r0 + i * 64 + lane < d.rows) atomicAdd(&next[wave][(uint32_t)keys[i] >> d.shift & 255u], 1u);
   __syncthreads();
   uint32_t at = d.count[((int64_t)w * 256 + threadIdx.x) * d.tiles + blockIdx.x];
 #pragma unroll
   for (int q = 0; q < 4; ++q) { const uint32_t c = next[q][threadIdx.x]; next[q][threadIdx.x] = at; at += c; }
   __syncthreads();
+#pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int64_t r = r0 + i * 64 + lane;
-    const bool there = r < d.rows;
-    const int32_t key = there ? d.key(w, r) : 0;
+    const bool there = r0 + i * 64 + lane < d.rows;
+    const int32_t key = keys[i];
     const uint32_t digit = (uint32_t)key >> d.shift & 255u;
     uint64_t same = __ballot(there);
 #pragma unroll
@@ -232,7 +265,7 @@ __global__ __launch_bounds__(256) void digit_place_kernel(Digits d) {
     __builtin_amdgcn_wave_barrier();
     if (there) {
       d.key_out[w * d.rows + to] = key;
-      d.place_out[w * d.rows + to] = d.token ? (int32_t)r : d.place_in[w * d.rows + r];
+      d.place_out[w * d.rows + to] = places[i];
     }
   }
 }
@@ -244,112 +277,188 @@ struct SumArgs {
   const int32_t* key; const int32_t* place;                // [k][rows], sorted
   float* part;                                             // [k][chunks][2][n]: of a token that came from the chunk before, and that goes on
   int64_t chunks;
+  int log_tpr;                                             // threads of a chunk
+  int slices;                                              // parts of a row by so many pieces; one more for what is behind the whole pieces
+  int log_join;                                            // threads of a row in the last kernel
+  int64_t join_blocks;                                     // of a worker, in the last kernel; those behind them fill rows that no token has
+  int fill_rows;                                           // of a block
 };
 
-__global__ __launch_bounds__(256) void embed_zero_kernel(EmbedGradArgs a) {
-  const int w = blockIdx.y;
-  float* grad = a.grad + w * a.grad_stride;
-  if (a.grad_ld == a.n) {                                  // rows without gaps are one
-    const int64_t all = a.vocab * a.n;
-    for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e < all; e += (int64_t)gridDim.x * 1024) {
-      const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-      store16<F32>(grad, e, all, zero);
-    }
-    return;
-  }
-  for (int64_t v = blockIdx.x; v < a.vocab; v += gridDim.x)
-    for (int64_t e = threadIdx.x * 4; e < a.n; e += 1024) {
-      const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-      store16<F32>(grad + v * a.grad_ld, e, a.n, zero);
-    }
-}
-
-// the elements e0 .. e0+V-1 of a row of the gradient
-template <int V>
-__device__ __forceinline__ void put_sum(const EmbedGradArgs& a, int w, int32_t v, int64_t e0, float (&s)[V]) {
-  float* row = a.grad + w * a.grad_stride + v * a.grad_ld;
+// the sum of a token's rows in columns e0 .. e0+W-1, in the gradient or (part of it) in scratch
+template <int W>
+__device__ __forceinline__ void put_sum(const EmbedGradArgs& a, float* to, bool whole, const float (&s)[W]) {
+  if constexpr (W == 1) {
+    *to = whole ? (a.accumulate ? *to + s[0] * a.scale : s[0] * a.scale) : s[0];
+  } else {
 #pragma unroll
-  for (int q = 0; q < V / 4; ++q) {
-    float f[4];
+    for (int q = 0; q < W / 4; ++q) {
+      float f[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = s[4 * q + j] * a.scale;
-    if (a.accumulate) {
-      float old[4];
-      load_floats<4>(row, e0 + 4 * q, a.n, 0.f, old);
+      for (int j = 0; j < 4; ++j) f[j] = whole ? s[4 * q + j] * a.scale : s[4 * q + j];
+      if (whole && a.accumulate) {
+        uint32_t old[4];
+        load_piece<F32>(to + 4 * q, old);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f[j] += old[j];
-    }
-    store16<F32>(row, e0 + 4 * q, a.n, f);
-  }
-}
-
-template <class E>
-__global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s, int log_tpr) {
-  constexpr int V = E::V;
-  const EmbedGradArgs& a = s.a;
-  const int w = blockIdx.z, t = threadIdx.x & ((1 << log_tpr) - 1);
-  const int64_t c = (int64_t)blockIdx.x * (256 >> log_tpr) + (threadIdx.x >> log_tpr);
-  const int64_t e0 = (((int64_t)blockIdx.y << log_tpr) + t) * V;
-  if (c >= s.chunks || e0 >= a.n) return;
-  const typename E::T* dy = reinterpret_cast<const typename E::T*>(a.dy.p) + w * a.dy.stride;
-  const int32_t* key = s.key + w * a.rows;
-  const int32_t* place = s.place + w * a.rows;
-  const int64_t i0 = c * kChunk, i1 = i0 + kChunk < a.rows ? i0 + kChunk : a.rows;
-  float* part = s.part + (w * s.chunks + c) * 2 * a.n;
-  float sum[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) sum[j] = 0.f;
-  int32_t now = key[i0];
-  bool from_before = i0 > 0 && key[i0 - 1] == now;
-  for (int64_t i = i0; i < i1; ++i) {
-    if (now >= a.vocab) return;                            // nothing but what is no token from here on
-    float f[V];
-    uint32_t raw[4];
-    load16<E>(dy + place[i] * a.dy.ld, e0, a.n, raw);
-    E::unpack(raw, f);
-#pragma unroll
-    for (int j = 0; j < V; ++j) sum[j] += f[j];
-    const int32_t next = i + 1 < a.rows ? key[i + 1] : -1;
-    if (i + 1 == i1 || next != now) {
-      const bool goes_on = i + 1 == i1 && next == now;
-      if (from_before || goes_on) {
-        float* to = part + (from_before ? 0 : a.n);
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (e0 + j < a.n) to[e0 + j] = sum[j];
-      } else {
-        put_sum<V>(a, w, now, e0, sum);
+        for (int j = 0; j < 4; ++j) f[j] += __uint_as_float(old[j]);
       }
+      store_piece<F32>(to + 4 * q, f);
+    }
+  }
+}
+
+// A chunk's rows in columns e0 .. e0+W-1 (W: a piece, or one behind the whole pieces), `key` and `place` of it in LDS: key[-1] is the one
+// before it, key[count] the one behind.  All rows are on their way before the first is added: memory operations of a wave are
+// waited for in their order, so a load behind the write of a sum would wait for that too.
+template <class E, int W>
+__device__ __forceinline__ void sum_chunk(const SumArgs& s, int w, int64_t c, int count, const int32_t* key, const int32_t* place, int64_t e0) {
+  const EmbedGradArgs& a = s.a;
+  const typename E::T* dy = reinterpret_cast<const typename E::T*>(a.dy.p) + w * a.dy.stride + e0;
+  float* grad = a.grad + w * a.grad_stride + e0;
+  float* part = s.part + (w * s.chunks + c) * 2 * a.n + e0;
+  uint32_t raw[kChunk][W == 1 ? 1 : 4];
 #pragma unroll
-      for (int j = 0; j < V; ++j) sum[j] = 0.f;
-      now = next;
+  for (int i = 0; i < kChunk; ++i) {
+    const typename E::T* row = dy + place[i] * a.dy.ld;    // (behind the chunk's last the first row of all: in bounds, and not added)
+    if constexpr (W == 1) raw[i][0] = __float_as_uint(E::one(row));
+    else load_piece<E>(row, raw[i]);
+  }
+  float sum[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) sum[j] = 0.f;
+  bool from_before = key[-1] == key[0];
+#pragma unroll
+  for (int i = 0; i < kChunk; ++i) {
+    const int32_t now = key[i], next = key[i + 1];
+    if (i >= count || now >= a.vocab) break;               // nothing but what is no token from here on
+    if constexpr (W == 1) {
+      sum[0] += __uint_as_float(raw[i][0]);
+    } else {
+      float f[W];
+      E::unpack(raw[i], f);
+#pragma unroll
+      for (int j = 0; j < W; ++j) sum[j] += f[j];
+    }
+    if (i + 1 == count || next != now) {
+      const bool whole = !from_before && next != now;
+      put_sum<W>(a, whole ? grad + now * a.grad_ld : from_before ? part : part + a.n, whole, sum);
+#pragma unroll
+      for (int j = 0; j < W; ++j) sum[j] = 0.f;
       from_before = false;
     }
   }
 }
 
-// tokens that go on from the chunk they begin in: its partial sum and those of the chunks behind it
-__global__ __launch_bounds__(256) void embed_join_kernel(SumArgs s) {
+// rows of the gradient that no token has: a thread looks for each among the sorted keys, then a wave writes it
+__device__ __forceinline__ void fill_rows(const SumArgs& s, int w, int64_t v0, int32_t* present) {
   const EmbedGradArgs& a = s.a;
-  const int w = blockIdx.z;
   const int32_t* key = s.key + w * a.rows;
-  const int64_t c = blockIdx.x, i0 = c * kChunk, last = i0 + kChunk - 1;
-  if (last + 1 >= a.rows) return;
-  const int32_t v = key[last];
-  if (v >= a.vocab || key[last + 1] != v) return;
-  if (key[i0] == v && i0 > 0 && key[i0 - 1] == v) return;  // began before
-  const int64_t e0 = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
-  if (e0 >= a.n) return;
-  const float* part = s.part + (w * s.chunks + c) * 2 * a.n;
-  float sum[4];
-  load_floats<4>(part + a.n, e0, a.n, 0.f, sum);
-  for (int64_t q = 1; (c + q) * kChunk < a.rows && key[(c + q) * kChunk] == v; ++q) {
-    float f[4];
-    load_floats<4>(part + q * 2 * a.n, e0, a.n, 0.f, f);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum[j] += f[j];
+  const int64_t v1 = v0 + s.fill_rows < a.vocab ? v0 + s.fill_rows : a.vocab;
+  if (v0 + threadIdx.x < v1) {
+    const int32_t v = (int32_t)(v0 + threadIdx.x);
+    int64_t lo = 0, hi = a.rows;                           // the first key that is not below v lies in lo .. hi
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) >> 1;
+      if (key[mid] < v) lo = mid + 1;
+      else hi = mid;
+    }
+    present[threadIdx.x] = lo < a.rows && key[lo] == v;
   }
-  put_sum<4>(a, w, v, e0, sum);
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t v = v0 + (threadIdx.x >> 6); v < v1; v += 4) {
+    if (present[v - v0]) continue;
+    float* row = a.grad + w * a.grad_stride + v * a.grad_ld;
+    const int whole = (int)a.n & ~3;
+    for (int e = lane * 4; e < whole; e += 256) store_piece<F32>(row + e, zero);
+    if (whole + lane < a.n) row[whole + lane] = 0.f;
+  }
+}
+
+constexpr int kFewestThreads = 8;                          // of a chunk, so that a block's places fit its LDS
+
+template <class E>
+__global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
+  constexpr int CHUNKS = 256 / kFewestThreads, KEYS = kChunk + 8;               // a key before and one behind, and whole pieces of LDS
+  __shared__ __align__(16) int32_t key[CHUNKS * KEYS], place[CHUNKS * kChunk];
+  const EmbedGradArgs& a = s.a;
+  const int w = blockIdx.y;
+  const int slices = s.slices + (a.n % E::V ? 1 : 0), slice = blockIdx.x % slices;
+  const int t = threadIdx.x & ((1 << s.log_tpr) - 1), g = threadIdx.x >> s.log_tpr;
+  const int64_t c = (int64_t)(blockIdx.x / slices) * (256 >> s.log_tpr) + g, i0 = c * kChunk;
+  const int count = i0 + kChunk < a.rows ? kChunk : (int)(a.rows - i0);         // (not positive: no chunk)
+  int32_t* my_key = key + g * KEYS + 4;
+  int32_t* my_place = place + g * kChunk;
+  for (int i = t; i < kChunk + 2; i += 1 << s.log_tpr) {
+    const int64_t at = i0 + i - 1;
+    my_key[i - 1] = at >= 0 && at < a.rows ? s.key[w * a.rows + at] : -1;
+    if (i < kChunk) my_place[i] = i < count ? s.place[w * a.rows + i0 + i] : 0;
+  }
+  __syncthreads();
+  if (count <= 0) return;
+  const int64_t whole = a.n / E::V;
+  if (slice == s.slices) {
+    if (whole * E::V + t < a.n) sum_chunk<E, 1>(s, w, c, count, my_key, my_place, whole * E::V + t);
+    return;
+  }
+  const int64_t q = ((int64_t)slice << s.log_tpr) + t;
+  if (q < whole) sum_chunk<E, E::V>(s, w, c, count, my_key, my_place, q * E::V);
+}
+
+// tokens that go on from the chunk c they begin in, in 1024 columns: its partial sum and those of the chunks behind it.  Four columns a
+// thread; where a row has fewer, several threads share them, each adds every so-manieth sum, and those are added in their order.
+__device__ __forceinline__ void join(const SumArgs& s, int w, int64_t c, int64_t slice, float4* lds) {
+  const EmbedGradArgs& a = s.a;
+  const int32_t* key = s.key + w * a.rows;
+  const int64_t i0 = c * kChunk, last = i0 + kChunk - 1;
+  const int32_t v = key[last], behind = key[last + 1], first = key[i0], before = i0 > 0 ? key[i0 - 1] : -1;       // (a chunk follows)
+  if (v >= a.vocab || behind != v || (first == v && before == v)) return;       // (or it began before)
+  const int mine = threadIdx.x & ((1 << s.log_join) - 1), share = threadIdx.x >> s.log_join, shares = 256 >> s.log_join;
+  const int64_t e0 = ((slice << s.log_join) + mine) * 4;
+  const float* part = s.part + (w * s.chunks + c) * 2 * a.n;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f}, f[4];
+  const int lane = threadIdx.x & 63;
+  if (e0 < a.n && share == 0) load_floats<4>(part + a.n, e0, a.n, 0.f, sum);
+  int64_t at = 1 + share;                                  // the next chunk (from c on) of this thread's
+  for (int64_t q = 1; c + q < s.chunks; q += 64) {         // the next 64 chunks: in how many of them does it go on?
+    const bool there = c + q + lane < s.chunks;
+    const uint64_t not_mine = ~__ballot(there && key[(c + q + (there ? lane : 0)) * kChunk] == v);
+    const int run = not_mine ? __builtin_ctzll(not_mine) : 64;
+    if (e0 < a.n) {
+#pragma unroll 4
+      for (; at < q + run; at += shares) {
+        load_floats<4>(part + at * 2 * a.n, e0, a.n, 0.f, f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] += f[j];
+      }
+    }
+    if (run < 64) break;
+  }
+  if (shares > 1) {                                        // (every thread of the block is here)
+    lds[threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    __syncthreads();
+    if (share > 0) return;
+    for (int q = 1; q < shares; ++q) {
+      const float4 more = lds[(q << s.log_join) + mine];
+      sum[0] += more.x; sum[1] += more.y; sum[2] += more.z; sum[3] += more.w;
+    }
+  }
+  if (e0 >= a.n) return;
+  float* row = a.grad + w * a.grad_stride + v * a.grad_ld;
+  if (e0 + 4 <= a.n) put_sum<4>(a, row + e0, true, sum);
+  else
+    for (int j = 0; j < 4; ++j) {
+      const float one[1] = {sum[j]};
+      if (e0 + j < a.n) put_sum<1>(a, row + e0 + j, true, one);
+    }
+}
+
+__global__ __launch_bounds__(256) void embed_join_kernel(SumArgs s) {
+  __shared__ float4 lds[256];
+  const int w = blockIdx.y;
+  const int64_t slices = ceil_div(s.a.n, 1024);
+  if (blockIdx.x < s.join_blocks) join(s, w, blockIdx.x / slices, blockIdx.x % slices, lds);
+  else fill_rows(s, w, (blockIdx.x - s.join_blocks) * s.fill_rows, reinterpret_cast<int32_t*>(lds));
 }
 
 // scratch: sorted keys and places, then (digits) the others of the two, and counts, then the partial sums
@@ -372,11 +481,14 @@ struct GradLayout {
 };
 
 template <class E>
-hipError_t sums(const SumArgs& s, hipStream_t stream) {
-  const int64_t pieces = ceil_div(s.a.n, E::V);
-  const int l = log_threads(pieces);
-  const dim3 grid((unsigned)ceil_div(s.chunks, 256 >> l), (unsigned)ceil_div(pieces, 1 << l), (unsigned)s.a.k);
-  hipLaunchKernelGGL(embed_sum_kernel<E>, grid, dim3(256), 0, stream, s, l);
+hipError_t sums(SumArgs& s, hipStream_t stream) {
+  const EmbedGradArgs& a = s.a;
+  const int64_t whole = a.n / E::V;
+  s.log_tpr = log_threads(whole);
+  if ((1 << s.log_tpr) < kFewestThreads) s.log_tpr = log_threads(kFewestThreads);
+  s.slices = (int)ceil_div(whole, 1 << s.log_tpr);
+  const int64_t blocks = ceil_div(s.chunks, 256 >> s.log_tpr) * (s.slices + (a.n % E::V ? 1 : 0));
+  hipLaunchKernelGGL(embed_sum_kernel<E>, dim3((unsigned)blocks, (unsigned)a.k), dim3(256), 0, stream, s);
   return hipGetLastError();
 }
 
@@ -391,16 +503,11 @@ size_t embedding_grad_scratch(int k, int64_t rows, int64_t vocab, int64_t n) { r
 
 hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, hipStream_t s) {
   hipError_t e = hipSuccess;
-  if (!a.accumulate) {
-    const int64_t want = ceil_div(a.vocab * a.n, 1024 * 4);
-    hipLaunchKernelGGL(embed_zero_kernel, dim3((unsigned)(want < 8 * kCus ? want : 8 * kCus), (unsigned)a.k), dim3(256), 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (a.rows == 0) return e;
   const GradLayout lay(a.k, a.rows, a.n);
   int32_t* key = reinterpret_cast<int32_t*>(a.scratch + lay.key);
   int32_t* place = reinterpret_cast<int32_t*>(a.scratch + lay.place);
-  if (a.rows <= kRankRows) {
+  if (a.rows == 0) {                                       // nothing to sort: every row is one to fill
+  } else if (a.rows <= kRankRows) {
     hipLaunchKernelGGL(rank_kernel, dim3((unsigned)ceil_div(a.rows, 64), (unsigned)a.k), dim3(1024), 0, s, a.token, key, place, (int)a.rows,
                        (int32_t)a.vocab);
     if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -432,9 +539,19 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, hipStream_t 
     key = const_cast<int32_t*>(d.key_in);
     place = const_cast<int32_t*>(d.place_in);
   }
-  SumArgs sum = {a, key, place, reinterpret_cast<float*>(a.scratch + lay.part), lay.chunks};
-  if ((e = dtype == DW_BF16 ? sums<Bf16>(sum, s) : sums<F32>(sum, s)) != hipSuccess || lay.chunks == 1) return e;
-  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(lay.chunks - 1), (unsigned)ceil_div(a.n, 1024), (unsigned)a.k), dim3(256), 0, s, sum);
+  SumArgs sum = {};
+  sum.a = a;
+  sum.key = key;
+  sum.place = place;
+  sum.part = reinterpret_cast<float*>(a.scratch + lay.part);
+  sum.chunks = lay.chunks;
+  if (a.rows > 0 && (e = dtype == DW_BF16 ? sums<Bf16>(sum, s) : sums<F32>(sum, s)) != hipSuccess) return e;
+  sum.log_join = log_threads(ceil_div(a.n, 4));
+  sum.join_blocks = lay.chunks > 1 ? (lay.chunks - 1) * ceil_div(a.n, 1024) : 0;
+  sum.fill_rows = (int)(a.n >= 4096 ? 16 : a.n <= 256 ? 256 : 65536 / a.n);     // 256 KB a block, and a row a thread
+  const int64_t blocks = sum.join_blocks + (a.accumulate ? 0 : ceil_div(a.vocab, sum.fill_rows));
+  if (blocks == 0) return e;
+  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)blocks, (unsigned)a.k), dim3(256), 0, s, sum);
   return hipGetLastError();
 }
 
