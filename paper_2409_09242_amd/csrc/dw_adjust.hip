@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
       const int q = i * kThreads + t;
       bits[i] = ~0u;
       if (q < pieces) {
-        load_piece<E>(at_piece<E>(z + j0, q), raw[i]);
+        load_piece_once<E>(at_piece<E>(z + j0, q), raw[i]);
         if (mask) bits[i] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(mask + (j0 >> 5)) + (uint32_t)(q * V >> 5 << 2));
       }
     }

@@ -37,6 +37,11 @@ struct DropKey {
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = (uint32_t)(u >> (16 * j) & 0xFFFFu) < limit ? x[j] * factor : 0.f;
   }
+  // the element in column e of row r
+  __device__ __forceinline__ float one(int64_t r, int64_t groups, int64_t e, float x) const {
+    const uint64_t u = stream_mix(counter(r, groups, e >> 2));
+    return (uint32_t)(u >> (16 * (e & 3)) & 0xFFFFu) < limit ? x * factor : 0.f;
+  }
   // the V elements from column e0 (a multiple of four) of row r
   template <int V>
   __device__ __forceinline__ void piece(int64_t r, int64_t groups, int64_t e0, float (&x)[V]) const {

@@ -9,40 +9,54 @@ namespace dw {
 
 namespace {
 
-template <class E>
+// a thread takes every tpr-th piece of its group's row; the elements behind the row's whole pieces one each
+template <class E, bool RES>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int log_tpr) {
   constexpr int V = E::V;
-  const int w = blockIdx.y, t = threadIdx.x & ((1 << log_tpr) - 1), g = threadIdx.x >> log_tpr;
+  const int w = blockIdx.y, tpr = 1 << log_tpr, t = threadIdx.x & (tpr - 1), g = threadIdx.x >> log_tpr;
+  const int n = (int)a.n, whole = n / V;
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
-  const typename E::T* res = a.res.p ? reinterpret_cast<const typename E::T*>(a.res.p) + w * a.res.stride : nullptr;
+  const typename E::T* res = reinterpret_cast<const typename E::T*>(a.res.p) + w * a.res.stride;
   typename E::T* y = reinterpret_cast<typename E::T*>(a.y.p) + w * a.y.stride;
   const DropKey key(a.drop, w);
-  const int64_t n = a.n, groups = ceil_div(n, 4), step = (int64_t)gridDim.x * (256 >> log_tpr);
+  const int64_t groups = ceil_div(n, 4), step = (int64_t)gridDim.x * (256 >> log_tpr);
   for (int64_t r = (int64_t)blockIdx.x * (256 >> log_tpr) + g; r < a.rows; r += step) {
-    for (int64_t e0 = (int64_t)t * V; e0 < n; e0 += (int64_t)V << log_tpr) {
+    const typename E::T* xr = x + r * a.x.ld;
+    const typename E::T* rr = res + r * a.res.ld;
+    typename E::T* yr = y + r * a.y.ld;
+    for (int q = t; q < whole; q += tpr) {
+      uint32_t raw[4], add[4];
+      load_piece_once<E>(at_piece<E>(xr, q), raw);
+      if constexpr (RES) load_piece_once<E>(at_piece<E>(rr, q), add);
       float f[V];
-      load_floats16<E>(x + r * a.x.ld, e0, n, f);
-      key.piece<V>(r, groups, e0, f);
-      if (res) {
+      E::unpack(raw, f);
+      key.piece<V>(r, groups, (int64_t)q * V, f);
+      if constexpr (RES) {
         float b[V];
-        load_floats16<E>(res + r * a.res.ld, e0, n, b);
+        E::unpack(add, b);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] += b[j];
       }
-      store16<E>(y + r * a.y.ld, e0, n, f);
+      store_piece<E>(at_piece<E>(yr, q), f);
+    }
+    for (int e = whole * V + t; e < n; e += tpr) {
+      const float f = key.one(r, groups, e, E::one(xr + e));
+      E::put(yr + e, RES ? f + E::one(rr + e) : f);
     }
   }
 }
 
 template <class E>
 hipError_t dropout(const DropoutArgs& a, hipStream_t s) {
-  const int64_t pieces = ceil_div(a.n, E::V);
+  const int64_t pieces = a.n / E::V;
   int log_tpr = 0;
   while (log_tpr < 8 && (1 << log_tpr) < pieces) ++log_tpr;
   int64_t blocks = ceil_div(a.rows, 256 >> log_tpr);
-  const int64_t most = 16 * kCus / a.k > 1 ? 16 * kCus / a.k : 1;
+  const int64_t most = 64 * kCus / a.k;
   if (blocks > most) blocks = most;
-  hipLaunchKernelGGL(dropout_kernel<E>, dim3((unsigned)blocks, (unsigned)a.k), dim3(256), 0, s, a, log_tpr);
+  const dim3 grid((unsigned)blocks, (unsigned)a.k);
+  if (a.res.p) hipLaunchKernelGGL((dropout_kernel<E, true>), grid, dim3(256), 0, s, a, log_tpr);
+  else hipLaunchKernelGGL((dropout_kernel<E, false>), grid, dim3(256), 0, s, a, log_tpr);
   return hipGetLastError();
 }
 

@@ -320,7 +320,7 @@ __device__ __forceinline__ void sum_chunk(const SumArgs& s, int w, int64_t c, in
   for (int i = 0; i < kChunk; ++i) {
     const typename E::T* row = dy + place[i] * a.dy.ld;    // (behind the chunk's last the first row of all: in bounds, and not added)
     if constexpr (W == 1) raw[i][0] = __float_as_uint(E::one(row));
-    else load_piece<E>(row, raw[i]);
+    else load_piece_once<E>(row, raw[i]);
   }
   float sum[W];
 #pragma unroll

@@ -38,6 +38,8 @@ struct F32 {
     for (int j = 0; j < 4; ++j) r[j] = __float_as_uint(f[j]);
   }
   __device__ static __forceinline__ float one(const T* p) { return *p; }
+  __device__ static __forceinline__ uint32_t bits(const T* p) { return *reinterpret_cast<const uint32_t*>(p); }      // as it is in memory
+  __device__ static __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits); }
   __device__ static __forceinline__ void put(T* p, float f) { *p = f; }
   typedef Raw16a4 Raw;
 };
@@ -57,6 +59,8 @@ struct Bf16 {
     for (int j = 0; j < 4; ++j) r[j] = pack_bf16(f[2 * j], f[2 * j + 1]);
   }
   __device__ static __forceinline__ float one(const T* p) { return __uint_as_float((uint32_t)*p << 16); }
+  __device__ static __forceinline__ uint32_t bits(const T* p) { return *p; }
+  __device__ static __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits << 16); }
   __device__ static __forceinline__ void put(T* p, float f) { *p = (uint16_t)pack_bf16(f, 0.f); }
   typedef Raw16a2 Raw;
 };

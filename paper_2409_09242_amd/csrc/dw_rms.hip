@@ -15,6 +15,11 @@
 //
 // Backward: a group of threads takes every strips-th row of one worker and keeps its column sums in registers; one row of partial
 // sums per block goes to scratch, and a second kernel adds those up in their order.
+//
+// Bound by memory at the rate of its mix of reads and writes (a copy 4.75 TB/s, two reads a write 5.9): forward 16 x 512 rows of 4096,
+// bf16, with a residual 54 us = 5.0 TB/s, its 8-bit form with dropout, 8 x 1024 x 4096, 43 us = 5.4 and 26 for the transposed form;
+// backward 3 x 2731 rows of 5003, fp32, with a gradient from further on and a dropout's own output 161 us = 5.1 TB/s, and 5 for the
+// columns' sums.  One row 3.7 us.  Rows that registers do not hold (above 32768 columns, backward in bf16 above 16384) 2.3 TB/s.
 #include "dw_dropout.h"
 #include "dw_fp8.h"
 
@@ -78,13 +83,82 @@ __device__ __forceinline__ void put_eight(uint8_t* q, uint8_t* scale, int64_t e0
   }
 }
 
-template <class E, int TPR, int ITEMS, int BLOCK>
+// A row of n is its whole pieces of 16 bytes, piece i * TPR + t to thread t, and fewer than V elements more, one each to the first
+// threads: every access is in bounds and no piece needs a mask of its own.  for_row sees to it that there are as many threads as odd
+// elements.
+template <class E, int TPR>
+struct Split {
+  int whole, odd, t, column;                               // whole pieces; elements behind them; this thread, and its element of those
+  bool has_odd;
+  __device__ __forceinline__ Split(int64_t n, int t_) : whole((int)(n / E::V)), odd((int)(n % E::V)), t(t_), column(whole * E::V + t_), has_odd(t_ < odd) {}
+};
+
+// ITEMS pieces of a row and its odd element as they are in memory, so that nothing waits for them before they are used; what a thread
+// has not reads as zero.  They stream through once: without displacing what is read again, they are read faster too (16384 x 4096, bf16,
+// forward: 85 us and 105, backward 95 and 108).
+template <class E, int TPR, int ITEMS>
+struct RowRegs {
+  uint32_t piece[ITEMS][4], odd;
+  __device__ __forceinline__ void load(const typename E::T* row, const Split<E, TPR>& s) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      if (i * TPR + s.t < s.whole) {
+        load_piece_once<E>(at_piece<E>(row, i * TPR + s.t), piece[i]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) piece[i][j] = 0u;
+      }
+    }
+    odd = 0u;
+    if (s.has_odd) odd = E::bits(row + s.column);
+  }
+};
+template <class E, int TPR, int ITEMS>
+__device__ __forceinline__ void store_row(typename E::T* row, const Split<E, TPR>& s, const float (&f)[ITEMS][E::V], float odd) {
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i)
+    if (i * TPR + s.t < s.whole) store_piece<E>(at_piece<E>(row, i * TPR + s.t), f[i]);
+  if (s.has_odd) E::put(row + s.column, odd);
+}
+template <class E>
+__device__ __forceinline__ float as_stored_one(float f) {
+  return E::V == 8 ? __uint_as_float(pack_bf16(f, 0.f) << 16) : f;
+}
+
+// the elements behind the whole pieces, from the first threads of the group to the one whose next piece they begin, for the block of 128
+// that they share with the pieces before them
+template <class E, int TPR, int ITEMS>
+__device__ __forceinline__ void gather_odd(float (&v)[ITEMS][E::V], float odd, const Split<E, TPR>& s, float* lds) {
+  float f[E::V];
+  if constexpr (TPR > 64) {
+    __syncthreads();                                       // (what an earlier row left there has been read)
+    if (s.has_odd) lds[s.t] = odd;
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < E::V; ++j) {
+    if constexpr (TPR > 64) f[j] = lds[j];
+    else f[j] = __shfl(odd, j, TPR);
+    f[j] = j < s.odd ? f[j] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i)
+    if (i * TPR + s.t == s.whole)
+#pragma unroll
+      for (int j = 0; j < E::V; ++j) v[i][j] = f[j];
+}
+
+// FEW: gamma of the thread's columns stays in registers over its rows.  The next row travels while this one is worked on, except for
+// the longest rows, for which 1024 threads have no registers left.
+template <class E, int TPR, int ITEMS, int BLOCK, bool FEW>
 __global__ __launch_bounds__(BLOCK) void rms_norm_kernel(RmsArgs a) {
   constexpr int V = E::V, GROUPS = BLOCK / TPR;
-  __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)];
+  constexpr bool AHEAD = TPR < 1024 || ITEMS <= 2;
+  __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)], odd_lds[8];
   int turn = 0;
   const int w = blockIdx.y, t = GROUPS == 1 ? threadIdx.x : threadIdx.x % TPR, g = GROUPS == 1 ? 0 : threadIdx.x / TPR;
   const int64_t n = a.n, groups = ceil_div(n, 4), np = DW_FP8_ROW(n), ns = DW_FP8_SCALES(n);
+  const Split<E, TPR> split(n, t);
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride;
   const typename E::T* res = reinterpret_cast<const typename E::T*>(a.res.p) + w * a.res.stride;
   typename E::T* h = reinterpret_cast<typename E::T*>(a.h.p) + w * a.h.stride;
@@ -93,30 +167,66 @@ __global__ __launch_bounds__(BLOCK) void rms_norm_kernel(RmsArgs a) {
   const bool drop = a.drop.limit < 65536u;
   const DropKey key(a.drop, w);
   const float inv_n = 1.f / (float)n;
-  for (int64_t r = (int64_t)blockIdx.x * GROUPS + g; r < a.rows; r += (int64_t)gridDim.x * GROUPS) {
-    float v[ITEMS][V];
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  RowRegs<E, TPR, ITEMS> next, next_res;
+  auto fetch = [&](int64_t r) {
+    next.load(x + r * a.x.ld, split);
+    if (a.res.p) next_res.load(res + r * a.res.ld, split);
+  };
+  int64_t r = (int64_t)blockIdx.x * GROUPS + g;
+  if (AHEAD && r < a.rows) fetch(r);
+  float ga[ITEMS][V], ga_odd = 1.f;
+  auto param = [&](int i) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) ga[i][j] = 1.f;
+    if (gamma && i * TPR + t < split.whole) load_floats<V>(gamma, (int64_t)(i * TPR + t) * V, n, 0.f, ga[i]);
+  };
+  if constexpr (FEW) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) param(i);
+  }
+  if (gamma && split.has_odd) ga_odd = gamma[split.column];
+  for (; r < a.rows; r += step) {
+    if constexpr (!AHEAD) fetch(r);
+    float v[ITEMS][V], odd = E::value(next.odd);
     float sq = 0.f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int64_t e0 = (int64_t)(i * TPR + t) * V;
-      piece_of_h<E>(x + r * a.x.ld, a.res.p ? res + r * a.res.ld : nullptr, key, drop, r, groups, e0, n, v[i]);
+      E::unpack(next.piece[i], v[i]);
+      if (drop) key.piece<V>(r, groups, (int64_t)(i * TPR + t) * V, v[i]);
+      if (a.res.p) {
+        float b[V];
+        E::unpack(next_res.piece[i], b);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[i][j] += b[j];
+      }
+      if (drop || a.res.p) as_stored<E>(v[i]);
 #pragma unroll
       for (int j = 0; j < V; ++j) sq += v[i][j] * v[i][j];
-      if (a.h.p) store16<E>(h + r * a.h.ld, e0, n, v[i]);
     }
+    if (split.odd) {
+      if (drop) odd = key.one(r, groups, split.column, odd);
+      if (a.res.p) odd += E::value(next_res.odd);
+      odd = as_stored_one<E>(odd);
+      sq += odd * odd;                                     // (zero where there is none)
+    }
+    if (AHEAD && r + step < a.rows) fetch(r + step);
+    if (a.h.p) store_row<E, TPR, ITEMS>(h + r * a.h.ld, split, v, odd);
     const float rstd = 1.f / sqrtf(row_sum<TPR>(sq, red, turn) * inv_n + a.eps);
     if (t == 0 && a.rstd) a.rstd[w * a.rows + r] = rstd;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int64_t e0 = (int64_t)(i * TPR + t) * V;
-      float ga[V];
+      if constexpr (!FEW) param(i);
 #pragma unroll
-      for (int j = 0; j < V; ++j) ga[j] = 1.f;
-      if (gamma) load_floats<V>(gamma, e0, n, 0.f, ga);
+      for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * rstd * ga[i][j];
+    }
+    odd = odd * rstd * ga_odd;
+    if (a.y.p) store_row<E, TPR, ITEMS>(y + r * a.y.ld, split, v, odd);
+    if (a.q) {
+      if (split.odd) gather_odd<E, TPR, ITEMS>(v, odd, split, odd_lds);
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * rstd * ga[j];
-      if (a.y.p) store16<E>(y + r * a.y.ld, e0, n, v[i]);
-      if (a.q) put_eight<E>(a.q + (w * a.rows + r) * np, a.scale + (w * a.rows + r) * ns, e0, n, v[i]);
+      for (int i = 0; i < ITEMS; ++i)
+        put_eight<E>(a.q + (w * a.rows + r) * np, a.scale + (w * a.rows + r) * ns, (int64_t)(i * TPR + t) * V, n, v[i]);
     }
   }
 }
@@ -164,14 +274,18 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(RmsArgs a) {
   }
 }
 
+// Registers hold the rows and the column sums of a thread's pieces, gamma, and the next rows on their way; 1024 threads have half as many
+// each, so there, with more than eight columns a thread, gamma comes from the caches and the next rows are not fetched ahead.
 template <class E, int TPR, int ITEMS, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void rms_norm_grad_kernel(RmsGradArgs a) {
   constexpr int V = E::V, GROUPS = BLOCK / TPR, COLS = TPR * ITEMS * V;
+  constexpr bool AHEAD = TPR < 1024 || ITEMS * V <= 8;
   __shared__ float red[2 * (TPR > 64 ? TPR / 64 : 1)];
-  __shared__ float cols[GROUPS > 1 ? GROUPS * COLS : 1];
+  __shared__ float cols[GROUPS > 1 ? GROUPS * (COLS + V) : 1];
   int turn = 0;
   const int w = blockIdx.y, t = GROUPS == 1 ? threadIdx.x : threadIdx.x % TPR, g = GROUPS == 1 ? 0 : threadIdx.x / TPR;
   const int64_t n = a.n, groups = ceil_div(n, 4);
+  const Split<E, TPR> split(n, t);
   const typename E::T* dy = reinterpret_cast<const typename E::T*>(a.dy.p) + w * a.dy.stride;
   const typename E::T* h = reinterpret_cast<const typename E::T*>(a.h.p) + w * a.h.stride;
   const typename E::T* dh = reinterpret_cast<const typename E::T*>(a.dh.p) + w * a.dh.stride;
@@ -179,50 +293,74 @@ __global__ __launch_bounds__(BLOCK) void rms_norm_grad_kernel(RmsGradArgs a) {
   typename E::T* dx = reinterpret_cast<typename E::T*>(a.dx.p) + w * a.dx.stride;
   const float* gamma = a.gamma ? a.gamma + w * a.param_stride : nullptr;
   const DropKey key(a.drop, w);
+  const bool wanted = a.dres.p || a.dx.p;
   const float inv_n = 1.f / (float)n;
-  float dg[ITEMS][V];
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  RowRegs<E, TPR, ITEMS> next_dy, next_h, next_dh;
+  float next_rstd = 0.f;
+  auto fetch = [&](int64_t r) {
+    next_dy.load(dy + r * a.dy.ld, split);
+    next_h.load(h + r * a.h.ld, split);
+    if (AHEAD && a.dh.p && wanted) next_dh.load(dh + r * a.dh.ld, split);
+    next_rstd = a.rstd[w * a.rows + r];
+  };
+  int64_t r = (int64_t)blockIdx.x * GROUPS + g;
+  if (AHEAD && r < a.rows) fetch(r);
+  float dg[ITEMS][V], ga[ITEMS][V], dg_odd = 0.f, ga_odd = 1.f;
 #pragma unroll
-  for (int i = 0; i < ITEMS; ++i)
+  for (int i = 0; i < ITEMS; ++i) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) dg[i][j] = 0.f;
-  for (int64_t r = (int64_t)blockIdx.x * GROUPS + g; r < a.rows; r += (int64_t)gridDim.x * GROUPS) {
-    const float rstd = a.rstd[w * a.rows + r];
+    for (int j = 0; j < V; ++j) { dg[i][j] = 0.f; ga[i][j] = 1.f; }
+    if (AHEAD && gamma && i * TPR + t < split.whole) load_floats<V>(gamma, (int64_t)(i * TPR + t) * V, n, 0.f, ga[i]);
+  }
+  if (gamma && split.has_odd) ga_odd = gamma[split.column];
+  for (; r < a.rows; r += step) {
+    if constexpr (!AHEAD) fetch(r);
+    const float rstd = next_rstd;
     float v[ITEMS][V], u[ITEMS][V], sum = 0.f;             // a, and t
+    uint32_t more[ITEMS][4], more_odd = 0u;                // dh as it is in memory
+    float v_odd = E::value(next_dy.odd), u_odd = E::value(next_h.odd) * rstd;
+    if (AHEAD && a.dh.p) more_odd = next_dh.odd;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int64_t e0 = (int64_t)(i * TPR + t) * V;
-      float ga[V];
-      load_floats16<E>(dy + r * a.dy.ld, e0, n, v[i]);
-      load_floats16<E>(h + r * a.h.ld, e0, n, u[i]);
+      E::unpack(next_dy.piece[i], v[i]);
+      E::unpack(next_h.piece[i], u[i]);
+      if constexpr (AHEAD)
 #pragma unroll
-      for (int j = 0; j < V; ++j) ga[j] = 1.f;
-      if (gamma) load_floats<V>(gamma, e0, n, 0.f, ga);
+        for (int j = 0; j < 4; ++j) more[i][j] = a.dh.p ? next_dh.piece[i][j] : 0u;
+      if (!AHEAD && gamma && i * TPR + t < split.whole) load_floats<V>(gamma, (int64_t)(i * TPR + t) * V, n, 0.f, ga[i]);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         u[i][j] *= rstd;
         dg[i][j] += v[i][j] * u[i][j];
-        v[i][j] *= ga[j];
+        v[i][j] *= ga[i][j];
         sum += v[i][j] * u[i][j];
       }
     }
-    if (!a.dres.p && !a.dx.p) continue;
+    dg_odd += v_odd * u_odd;                               // (zeros where there is none)
+    v_odd *= ga_odd;
+    sum += v_odd * u_odd;
+    if (AHEAD && r + step < a.rows) fetch(r + step);
+    if (!wanted) continue;
     const float c = row_sum<TPR>(sum, red, turn) * inv_n;
+    if (!AHEAD && a.dh.p) { next_dh.load(dh + r * a.dh.ld, split); more_odd = next_dh.odd; }
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int64_t e0 = (int64_t)(i * TPR + t) * V;
+      float b[V];
+      if constexpr (!AHEAD)
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[i][j] = rstd * (v[i][j] - u[i][j] * c);
-      if (a.dh.p) {
-        float b[V];
-        load_floats16<E>(dh + r * a.dh.ld, e0, n, b);
+        for (int j = 0; j < 4; ++j) more[i][j] = a.dh.p ? next_dh.piece[i][j] : 0u;
+      E::unpack(more[i], b);
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[i][j] += b[j];
-      }
-      if (a.dres.p) store16<E>(dres + r * a.dres.ld, e0, n, v[i]);
-      if (a.dx.p) {
-        key.piece<V>(r, groups, e0, v[i]);
-        store16<E>(dx + r * a.dx.ld, e0, n, v[i]);
-      }
+      for (int j = 0; j < V; ++j) v[i][j] = rstd * (v[i][j] - u[i][j] * c) + b[j];
+    }
+    v_odd = rstd * (v_odd - u_odd * c) + E::value(more_odd);
+    if (a.dres.p) store_row<E, TPR, ITEMS>(dres + r * a.dres.ld, split, v, v_odd);
+    if (a.dx.p) {
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) key.piece<V>(r, groups, (int64_t)(i * TPR + t) * V, v[i]);
+      if (split.odd) v_odd = key.one(r, groups, split.column, v_odd);
+      store_row<E, TPR, ITEMS>(dx + r * a.dx.ld, split, v, v_odd);
     }
   }
   if (!a.part) return;
@@ -230,19 +368,26 @@ __global__ __launch_bounds__(BLOCK) void rms_norm_grad_kernel(RmsGradArgs a) {
   if constexpr (GROUPS == 1) {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
+      if (i * TPR + t < split.whole) {
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if ((int64_t)(i * TPR + t) * V + j < n) out[(int64_t)(i * TPR + t) * V + j] = dg[i][j];
+        for (int q = 0; q < V / 4; ++q) {
+          const float f[4] = {dg[i][4 * q], dg[i][4 * q + 1], dg[i][4 * q + 2], dg[i][4 * q + 3]};
+          store_piece<F32>(out + (int64_t)(i * TPR + t) * V + 4 * q, f);
+        }
+      }
+    if (split.has_odd) out[split.column] = dg_odd;
   } else {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-      for (int j = 0; j < V; ++j) cols[g * COLS + (i * TPR + t) * V + j] = dg[i][j];
+      for (int j = 0; j < V; ++j) cols[g * (COLS + V) + (i * TPR + t) * V + j] = dg[i][j];
+    __syncthreads();                                       // (the odd elements' places may be those of a piece that is not there)
+    if (split.has_odd) cols[g * (COLS + V) + split.column] = dg_odd;
     __syncthreads();
     for (int e = threadIdx.x; e < n; e += BLOCK) {
       float s = cols[e];
 #pragma unroll
-      for (int q = 1; q < GROUPS; ++q) s += cols[q * COLS + e];
+      for (int q = 1; q < GROUPS; ++q) s += cols[q * (COLS + V) + e];
       out[e] = s;
     }
   }
@@ -341,11 +486,14 @@ __global__ __launch_bounds__(1024) void rms_norm_strips_kernel(RmsGradArgs a) {
   }
 }
 
-// f.template operator()<TPR, ITEMS>() for rows of so many pieces; false: too long.  The lanes that share a block of 128 columns are
+// f.template operator()<TPR, ITEMS>() for rows of so many pieces and odd elements; false: too long.  Above 1536 pieces 1024 threads take two each: with
+// four of 512 threads the backward pass has no registers for a second block on the unit (4096 x 16384, bf16: 158 us and 114; fp32 with
+// four of 1024: 287 and 214).  The lanes that share a block of 128 columns are
 // in one group from 128 / V threads on, which is the fewest with an output in 8 bits (EIGHT)
 template <class E, bool EIGHT, bool WIDE, class F>
-bool for_row(int64_t pieces, F f) {
-  if (!EIGHT && pieces <= 4) f.template operator()<4, 1>();
+bool for_row(int64_t n, F f) {
+  const int64_t pieces = EIGHT ? DW_FP8_ROW(n) / E::V : n / E::V;
+  if (!EIGHT && pieces <= 4 && n % E::V <= 4) f.template operator()<4, 1>();
   else if ((!EIGHT || E::V == 8) && pieces <= 16) f.template operator()<16, 1>();
   else if (pieces <= 32) f.template operator()<32, 1>();
   else if (pieces <= 64) f.template operator()<64, 1>();
@@ -353,7 +501,8 @@ bool for_row(int64_t pieces, F f) {
   else if (pieces <= 256) f.template operator()<256, 1>();
   else if (pieces <= 512) f.template operator()<256, 2>();
   else if (pieces <= 1024) f.template operator()<512, 2>();
-  else if (pieces <= 2048) f.template operator()<512, 4>();
+  else if (pieces <= 1536) f.template operator()<512, 3>();
+  else if (pieces <= 2048) f.template operator()<1024, 2>();
   else if constexpr (WIDE) {
     if (pieces > 4096) return false;
     f.template operator()<1024, 4>();
@@ -369,21 +518,25 @@ struct Forward {
   template <int TPR, int ITEMS>
   void operator()() const {
     constexpr int BLOCK = block_of(TPR);
+    constexpr bool FEW = ITEMS * E::V <= 16 && TPR < 1024;
     const dim3 grid((unsigned)blocks_per_worker(a.k, a.rows, BLOCK / TPR, 2048 * (int64_t)kCus / BLOCK), (unsigned)a.k);
-    hipLaunchKernelGGL((rms_norm_kernel<E, TPR, ITEMS, BLOCK>), grid, dim3(BLOCK), 0, s, a);
+    hipLaunchKernelGGL((rms_norm_kernel<E, TPR, ITEMS, BLOCK, FEW>), grid, dim3(BLOCK), 0, s, a);
   }
 };
 template <class E>
 hipError_t forward(const RmsArgs& a, hipStream_t s) {
   const Forward<E> f{a, s};
-  const bool fits = a.q ? for_row<E, true, true>(DW_FP8_ROW(a.n) / E::V, f) : for_row<E, false, true>(ceil_div(a.n, E::V), f);
+  const bool fits = a.q ? for_row<E, true, true>(a.n, f) : for_row<E, false, true>(a.n, f);
   if (!fits)
     hipLaunchKernelGGL(rms_norm_long_kernel<E>, dim3((unsigned)blocks_per_worker(a.k, a.rows, 1, 4 * kCus), (unsigned)a.k), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 
 template <class E> constexpr bool kWideGrad = E::V == 4;
-int64_t grad_blocks(int tpr) { return (tpr >= 1024 ? 1 : tpr >= 256 ? 2 : 4) * (int64_t)kCus; }
+// blocks of the backward pass, few, so that there are few rows of partial sums: 256 threads twice a compute unit in bf16 (32768 x 2048:
+// 104 us, with three 113, with four 123), four times in fp32, whose rows have half as many columns (262, 210, 195)
+template <class E>
+int64_t grad_blocks(int tpr) { return (tpr >= 1024 ? 1 : tpr >= 512 ? 2 : tpr >= 256 && E::V == 8 ? 2 : 4) * (int64_t)kCus; }
 
 template <class E>
 struct Backward {
@@ -395,14 +548,15 @@ struct Backward {
     hipLaunchKernelGGL((rms_norm_grad_kernel<E, TPR, ITEMS, BLOCK>), dim3((unsigned)a.strips, (unsigned)a.k), dim3(BLOCK), 0, s, a);
   }
 };
+template <class E>
 struct Strips {
   int k; int64_t rows; int* strips;
   template <int TPR, int ITEMS>
-  void operator()() const { *strips = (int)blocks_per_worker(k, rows, block_of(TPR) / TPR, grad_blocks(TPR)); }
+  void operator()() const { *strips = (int)blocks_per_worker(k, rows, block_of(TPR) / TPR, grad_blocks<E>(TPR)); }
 };
 template <class E>
 hipError_t backward(const RmsGradArgs& a, hipStream_t s) {
-  if (for_row<E, false, kWideGrad<E>>(ceil_div(a.n, E::V), Backward<E>{a, s})) return hipGetLastError();
+  if (for_row<E, false, kWideGrad<E>>(a.n, Backward<E>{a, s})) return hipGetLastError();
   if (a.part) {
     hipLaunchKernelGGL(rms_norm_cols_kernel<E>, dim3((unsigned)a.strips, (unsigned)ceil_div(a.n, 256 * E::V), (unsigned)a.k), dim3(256), 0, s, a);
     const hipError_t e = hipGetLastError();
@@ -420,9 +574,8 @@ hipError_t launch_rms_norm(const RmsArgs& a, int dtype, hipStream_t s) {
 
 int rms_norm_grad_strips(int k, int64_t rows, int64_t n, int dtype) {
   int strips = 0;
-  const Strips count{k, rows, &strips};
-  const bool fits = dtype == DW_BF16 ? for_row<Bf16, false, kWideGrad<Bf16>>(ceil_div(n, Bf16::V), count)
-                                     : for_row<F32, false, kWideGrad<F32>>(ceil_div(n, F32::V), count);
+  const bool fits = dtype == DW_BF16 ? for_row<Bf16, false, kWideGrad<Bf16>>(n, Strips<Bf16>{k, rows, &strips})
+                                     : for_row<F32, false, kWideGrad<F32>>(n, Strips<F32>{k, rows, &strips});
   return fits ? strips : (int)blocks_per_worker(k, rows, 1, 2 * kCus);
 }
 
