@@ -125,6 +125,13 @@ __device__ __forceinline__ float as_stored_one(float f) {
   return E::V == 8 ? __uint_as_float(pack_bf16(f, 0.f) << 16) : f;
 }
 
+// this thread's number, for the row at hand: what follows from it alone would otherwise be worked out once and take registers throughout
+// (1024 threads with four pieces, backward: 66 of them in memory, so 32)
+__device__ __forceinline__ int anew(int t) {
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
 // the elements behind the whole pieces, from the first threads of the group to the one whose next piece they begin, for the block of 128
 // that they share with the pieces before them
 template <class E, int TPR, int ITEMS>
@@ -188,12 +195,13 @@ __global__ __launch_bounds__(BLOCK) void rms_norm_kernel(RmsArgs a) {
   if (gamma && split.has_odd) ga_odd = gamma[split.column];
   for (; r < a.rows; r += step) {
     if constexpr (!AHEAD) fetch(r);
+    const int tt = TPR * ITEMS >= 4096 ? anew(t) : t;
     float v[ITEMS][V], odd = E::value(next.odd);
     float sq = 0.f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       E::unpack(next.piece[i], v[i]);
-      if (drop) key.piece<V>(r, groups, (int64_t)(i * TPR + t) * V, v[i]);
+      if (drop) key.piece<V>(r, groups, (int64_t)(i * TPR + tt) * V, v[i]);
       if (a.res.p) {
         float b[V];
         E::unpack(next_res.piece[i], b);
@@ -316,6 +324,7 @@ __global__ __launch_bounds__(BLOCK) void rms_norm_grad_kernel(RmsGradArgs a) {
   if (gamma && split.has_odd) ga_odd = gamma[split.column];
   for (; r < a.rows; r += step) {
     if constexpr (!AHEAD) fetch(r);
+    const int tt = TPR * ITEMS >= 4096 ? anew(t) : t;
     const float rstd = next_rstd;
     float v[ITEMS][V], u[ITEMS][V], sum = 0.f;             // a, and t
     uint32_t more[ITEMS][4], more_odd = 0u;                // dh as it is in memory
@@ -358,7 +367,7 @@ __global__ __launch_bounds__(BLOCK) void rms_norm_grad_kernel(RmsGradArgs a) {
     if (a.dres.p) store_row<E, TPR, ITEMS>(dres + r * a.dres.ld, split, v, v_odd);
     if (a.dx.p) {
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i) key.piece<V>(r, groups, (int64_t)(i * TPR + t) * V, v[i]);
+      for (int i = 0; i < ITEMS; ++i) key.piece<V>(r, groups, (int64_t)(i * TPR + tt) * V, v[i]);
       if (split.odd) v_odd = key.one(r, groups, split.column, v_odd);
       store_row<E, TPR, ITEMS>(dx + r * a.dx.ld, split, v, v_odd);
     }
