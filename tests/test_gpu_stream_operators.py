@@ -3,6 +3,7 @@ past 32 bits of elements and rows past 16 bits, and what they do to the versions
 import pytest
 import torch
 
+from paper_2409_09242_amd import binding as B
 from paper_2409_09242_amd import operators as OPS
 
 pytestmark = pytest.mark.gpu
@@ -221,3 +222,32 @@ def test_written_tensors_count_as_changed():
     dg = torch.zeros(1, 40, device=DEV)
     OPS.rms_norm_grad(x, x, g, rstd, dgamma=dg)
     assert dg._version == 1 and x._version == 0 and g._version == 0
+
+
+def test_wrappers_refuse_what_does_not_fit():
+    x, g, f = torch.zeros(2, 3, 40, device=DEV), torch.zeros(2, 40, device=DEV), torch.zeros(2, 3, device=DEV)
+    i, wide = f.int(), torch.zeros(2, 3, 80, device=DEV)
+    words, history = torch.zeros(2, 3, 2, dtype=torch.int32, device=DEV), torch.zeros(2, 3, 5, dtype=torch.int32, device=DEV)
+    bad = [lambda: OPS.embedding(i.long(), x), lambda: OPS.embedding(i[0], x), lambda: OPS.embedding(i[:1], x), lambda: OPS.embedding(i.cpu(), x),
+           lambda: OPS.embedding(i, x, out=x[:, :2]), lambda: OPS.embedding(i, x.transpose(1, 2)), lambda: OPS.embedding(i.t().contiguous().t(), x),
+           lambda: OPS.embedding_grad(x, i), lambda: OPS.embedding_grad(x, i, 9, accumulate=True), lambda: OPS.embedding_grad(x, i, 0),
+           lambda: OPS.embedding_grad(x, i, out=g), lambda: OPS.embedding_grad(x, i, 9, out=x), lambda: OPS.embedding_grad(x, i, out=x.bfloat16()),
+           lambda: OPS.dropout(x, 0.1, 1, residual=x.bfloat16()), lambda: OPS.dropout(x, 0.1, 1, residual=wide), lambda: OPS.dropout(x, 0.1, 1, out=wide),
+           lambda: OPS.rms_norm(x, g[:1]), lambda: OPS.rms_norm(x, g.bfloat16()), lambda: OPS.rms_norm(x, g, residual=wide),
+           lambda: OPS.rms_norm(x, g, sum_out=wide), lambda: OPS.rms_norm(x, g, out=x.bfloat16()), lambda: OPS.rms_norm_fp8(x, g, sum_out=x.double()),
+           lambda: OPS.rms_norm_grad(x, x, g, f[:, :2]), lambda: OPS.rms_norm_grad(wide, x, g, f), lambda: OPS.rms_norm_grad(x, x, g, f, dh=wide),
+           lambda: OPS.rms_norm_grad(x, x, g, f, dgamma=f), lambda: OPS.rms_norm_grad(x, x, g, f, dres=wide),
+           lambda: OPS.adjust_logits(x, history[..., 0]), lambda: OPS.adjust_logits(x, history.long()), lambda: OPS.adjust_logits(x, history, filled=f),
+           lambda: OPS.adjust_logits(x, repetition=i), lambda: OPS.adjust_logits(x, bias=x[..., :39]), lambda: OPS.adjust_logits(x, bias=x.bfloat16()),
+           lambda: OPS.adjust_logits(x, mask=words[..., :1]), lambda: OPS.adjust_logits(x, mask=words.long()), lambda: OPS.adjust_logits(x, out=wide)]
+    for n, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("call %d was taken" % n)
+    refused = [lambda: OPS.dropout(x, 1.5, 1), lambda: OPS.rms_norm(x, eps=-1.0), lambda: OPS.rms_norm(x, out=x), lambda: OPS.embedding(i, x, float("nan")),
+               lambda: OPS.dropout(x, 0.1, 1, out=x[:1].expand(2, 3, 40)), lambda: OPS.rms_norm_grad(x, x, g, f, dres=x), lambda: OPS.embedding(i, x, out=x),
+               lambda: OPS.adjust_logits(x, out=x[:1].expand(2, 3, 40)), lambda: OPS.embedding_grad(x, i, out=x[:1].expand(2, 3, 40))]
+    for n, call in enumerate(refused):
+        with pytest.raises(B.DwError):
+            call()
+            pytest.fail("call %d was taken" % n)
