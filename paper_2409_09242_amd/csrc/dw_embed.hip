@@ -15,10 +15,10 @@
 // places whose counts of every digit are added up between the two passes over them.  One worker's 8192 places by counting 15 us, by
 // digits (two of them) 34; 65536 places 47.
 //
-// Where the whole gradient is wanted, rows that no token has are filled with zeros beside the last kernel's sums, each row written
-// once.  4 x 4096 rows of 4096, bf16, over 32000 tokens: counting 10 us, sums 62 to 85 (134 MB read, 150 written), the 2 GB of
-// zeros 340 = 5.9 TB/s (a fill alone reaches 6.4); 3 x 333 rows of 1001, fp32, over 5003: 3.0, 6.1, 12.2.  Lookups: 8 x 1024 rows of
-// 4096, fp32 to bf16, 31 us = 6.4 TB/s of what passes (common rows come from the caches); one row 2.0, less than a launch's 2.4.
+// Where the whole gradient is wanted, rows that no token has are filled with zeros beside the sort or beside the last sums.
+// Bound by writing them: 4 x 4096 rows of 4096, bf16, over 32000 tokens 422 us a call, 2.4 GB at 5.7 TB/s (a fill alone reaches 6.4);
+// added to a gradient that is there 115.  3 x 333 rows of 1001, fp32, over 5003: 19.5, three launches.  Lookups: 8 x 1024 rows of 4096,
+// fp32 to bf16, 31 us = 6.4 TB/s of what passes (common rows come from the caches); one row 2.0.
 #include "dw_ops.h"
 
 namespace dw {
@@ -122,13 +122,33 @@ constexpr int kChunk = 16;                                 // places whose rows 
 // what is no token sorts behind all tokens
 __device__ __forceinline__ int32_t key_of(int32_t token, int32_t vocab) { return (uint32_t)token < (uint32_t)vocab ? token : vocab; }
 
+// rows of the gradient that are zeros before anything is added up: a wave writes a row
+struct ZeroArgs {
+  float* grad; int64_t ld, stride, n;
+  int block_rows;
+};
+__device__ __forceinline__ void zero_row(float* row, int64_t n) {
+  const int lane = threadIdx.x & 63, whole = (int)n & ~3;
+  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int e = lane * 4; e < whole; e += 256) store_piece<F32>(row + e, zero);
+  if (whole + lane < n) row[whole + lane] = 0.f;
+}
+__device__ __forceinline__ void zero_rows(const ZeroArgs& a, int w, int64_t v0, int64_t vocab) {
+  const int64_t v1 = v0 + a.block_rows < vocab ? v0 + a.block_rows : vocab;
+  for (int64_t v = v0 + (threadIdx.x >> 6); v < v1; v += 16) zero_row(a.grad + w * a.stride + v * a.ld, a.n);
+}
+
 // 64 places a block, their keys against all of the worker's by 16 waves, 64 others at a time: a wave has those in its lanes, all
 // groups on their way at once, and hands them round one after another.  Of places before the block's an equal key counts, of
 // those behind not, and of its own those of lower lanes.
 __global__ __launch_bounds__(1024) void rank_kernel(const int32_t* __restrict__ token, int32_t* __restrict__ sorted, int32_t* __restrict__ place,
-                                                    int rows, int32_t vocab) {
+                                                    int rows, int32_t vocab, int rank_blocks, ZeroArgs zero) {
   constexpr int GROUPS = kRankRows / 1024;
   __shared__ int part[16][64];
+  if ((int)blockIdx.x >= rank_blocks) {
+    zero_rows(zero, blockIdx.y, (int64_t)(blockIdx.x - rank_blocks) * zero.block_rows, vocab);
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t* tok = token + (int64_t)blockIdx.y * rows;
   const int own = blockIdx.x, r = own * 64 + lane;
@@ -364,15 +384,8 @@ __device__ __forceinline__ void fill_rows(const SumArgs& s, int w, int64_t v0, i
     present[threadIdx.x] = lo < a.rows && key[lo] == v;
   }
   __syncthreads();
-  const int lane = threadIdx.x & 63;
-  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t v = v0 + (threadIdx.x >> 6); v < v1; v += 4) {
-    if (present[v - v0]) continue;
-    float* row = a.grad + w * a.grad_stride + v * a.grad_ld;
-    const int whole = (int)a.n & ~3;
-    for (int e = lane * 4; e < whole; e += 256) store_piece<F32>(row + e, zero);
-    if (whole + lane < a.n) row[whole + lane] = 0.f;
-  }
+  for (int64_t v = v0 + (threadIdx.x >> 6); v < v1; v += 4)
+    if (!present[v - v0]) zero_row(a.grad + w * a.grad_stride + v * a.grad_ld, a.n);
 }
 
 constexpr int kFewestThreads = 8;                          // of a chunk, so that a block's places fit its LDS
@@ -506,12 +519,24 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, hipStream_t 
   const GradLayout lay(a.k, a.rows, a.n);
   int32_t* key = reinterpret_cast<int32_t*>(a.scratch + lay.key);
   int32_t* place = reinterpret_cast<int32_t*>(a.scratch + lay.place);
-  if (a.rows == 0) {                                       // nothing to sort: every row is one to fill
-  } else if (a.rows <= kRankRows) {
-    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)ceil_div(a.rows, 64), (unsigned)a.k), dim3(1024), 0, s, a.token, key, place, (int)a.rows,
-                       (int32_t)a.vocab);
+  // The zeros: where at most a quarter of the rows can have a token, all rows beside the sort, which leaves the memory to them, and those
+  // few are written once more; otherwise, where that would write up to all of them twice, at the end those that no token has, looked for
+  // one by one (4 x 4096 rows of 4096 over 32000, the whole call: 422 us, the other way 434; 3 x 333 rows of 1001 over 5003: 19.5 and
+  // 20.8).  At most 256 KB a block, and four blocks a compute unit where there are as many rows (the latter at the end: 22.9 us by 65 rows
+  // a block, 21.0 by 15).
+  const bool first = !a.accumulate && a.vocab / 4 >= a.rows, last = !a.accumulate && !first;
+  const int64_t by_size = a.n >= 4096 ? 16 : a.n <= 256 ? 256 : 65536 / a.n, share = ceil_div(a.vocab * a.k, 4 * kCus);
+  const int fill_rows = (int)(share < by_size ? share : by_size);
+  const ZeroArgs zero = {a.grad, a.grad_ld, a.grad_stride, a.n, fill_rows < 16 ? 16 : fill_rows};
+  const int64_t zero_blocks = first ? ceil_div(a.vocab, zero.block_rows) : 0;
+  const bool digits = a.rows > kRankRows;
+  const int rank_blocks = digits ? 0 : (int)ceil_div(a.rows, 64);
+  if (rank_blocks + zero_blocks > 0) {
+    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)(rank_blocks + zero_blocks), (unsigned)a.k), dim3(1024), 0, s, a.token, key, place,
+                       digits ? 0 : (int)a.rows, (int32_t)a.vocab, rank_blocks, zero);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-  } else {
+  }
+  if (digits) {
     int32_t* key2 = reinterpret_cast<int32_t*>(a.scratch + lay.key2);
     int32_t* place2 = reinterpret_cast<int32_t*>(a.scratch + lay.place2);
     int passes = 1;
@@ -548,11 +573,8 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, hipStream_t 
   if (a.rows > 0 && (e = dtype == DW_BF16 ? sums<Bf16>(sum, s) : sums<F32>(sum, s)) != hipSuccess) return e;
   sum.log_join = log_threads(ceil_div(a.n, 4));
   sum.join_blocks = lay.chunks > 1 ? (lay.chunks - 1) * ceil_div(a.n, 1024) : 0;
-  // 256 KB a block and a row a thread at most, and four blocks a compute unit where there are as many rows (3 x 5003 rows of 1001, the
-  // whole call: 22.9 us by 65 rows a block, 21.0 by 15)
-  const int64_t most = a.n >= 4096 ? 16 : a.n <= 256 ? 256 : 65536 / a.n, share = ceil_div(a.vocab * a.k, 4 * kCus);
-  sum.fill_rows = (int)(share < most ? share : most);
-  const int64_t blocks = sum.join_blocks + (a.accumulate ? 0 : ceil_div(a.vocab, sum.fill_rows));
+  sum.fill_rows = fill_rows;
+  const int64_t blocks = sum.join_blocks + (last ? ceil_div(a.vocab, fill_rows) : 0);
   if (blocks == 0) return e;
   hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)blocks, (unsigned)a.k), dim3(256), 0, s, sum);
   return hipGetLastError();
