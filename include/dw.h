@@ -416,7 +416,8 @@ int dw_fp8_linear(const void* d_x, int64_t x_ld, int64_t x_stride, const uint8_t
  *   d_table     rows of n in `table_dtype`, worker w's row v at w*table_stride + v*table_ld; y in `dtype`
  *   d_grad      [k][vocab] rows of n floats.  accumulate 0: every row is written, zeros where no token was; 1: the sums are added
  *               to the rows of the tokens that are there, and the others are not touched
- * The rows of a token are added in fp32, in an order that follows from the tokens alone: no atomics.
+ * The rows of a token are added in fp32, in an order that follows from the tokens alone: no atomics.  (Of a table that the workers
+ * share, table_stride 0, each worker's gradient is its own part; their sum is the table's.)
  */
 int dw_embedding(const int32_t* d_token, const void* d_table, int64_t table_ld, int64_t table_stride, int table_dtype, int k,
                  int64_t rows, int64_t vocab, int64_t n, int dtype, float scale, void* d_y, int64_t y_ld, int64_t y_stride,
@@ -429,8 +430,8 @@ int dw_embedding_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const 
 /*
  * Dropout: y = residual + m x / q.  m is 1 where a 16-bit number of the counter-based stream is below round((1 - p) 65536), else 0,
  * and q = round((1 - p) 65536) / 65536, so that y's mean is x's (p comes in steps of 2^-16).  Element j of row r of worker w takes bits
- * 16 (j mod 4) to 16 (j mod 4) + 15 of mix(key(seed, w, step) + GAMMA*(r*ceil(n/4) + floor(j/4) + 1)), mix, GAMMA and key as for the
- * Rademacher stream: the mask is stored nowhere, and the backward pass is the same call on dy without a residual.  Give every
+ * 16 (j mod 4) to 16 (j mod 4) + 15 of mix(key(seed, w, step) + GAMMA*(r*ceil(n/4) + floor(j/4) + 1)), mix and GAMMA SplitMix64's and
+ * key(seed, w, step) = mix(mix(seed + GAMMA*(w+1)) + GAMMA*(step+1)), as for the Rademacher stream: the mask is stored nowhere, and the backward pass is the same call on dy without a residual.  Give every
  * dropout of a model a seed of its own, other than the configuration's.
  *   p           0 <= p <= 1; a dropped element's x is not looked at (an infinity or NaN there leaves no trace)
  *   d_step      NULL, or a device address of one 64-bit number that is added to `step` when the work runs: a captured graph

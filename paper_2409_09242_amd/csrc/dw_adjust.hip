@@ -5,7 +5,8 @@
 // A block takes SPAN tokens of a row: it counts those of the history that lie there in LDS, in 31 bits and one for "seen in the
 // prompt" (whole numbers: the order of the additions does not matter), and then goes over the logits.  Bound by memory, the logits in
 // and out; the blocks of a row read its history from the caches.  8 x 64 rows of 131072, bf16, histories of up to 2048, bias and mask:
-// 68 us = 4.1 TB/s (without a history 49 to 56: the two barriers around the counts are what is left of it); fp32 104.
+// 65 us = 4.3 TB/s (a copy 4.75; without a history 49 to 55: the two barriers around the counts are what is left of it); fp32 98.  Four rows
+// of 32000 with histories of 300: 5.3 us, two trips to memory and the barriers.
 #include "dw_ops.h"
 
 namespace dw {
@@ -170,8 +171,8 @@ template <class E>
 hipError_t adjust(const AdjustArgs& a, hipStream_t s) {
   if (a.out.p == a.logits.p && !a.bias && !a.mask && !a.history) return hipSuccess;
   // A token costs a line read and written, 128 bytes, a logit that is gone over 4 or 8.  512 rows of 131072, bf16, in place, by tokens
-  // and by all logits (us): histories of 1024 random tokens 22 and 58, 2048 45 and 67, 8192 150 and 106; of 2048 as they come in text
-  // 22 and 62
+  // and by all logits (us): histories of 1024 random tokens 22 and 58, 2048 45 and 64, 8192 150 and 107; of 2048 as they come in text
+  // 22 and 61
   if (a.out.p == a.logits.p && !a.bias && !a.mask && a.length <= a.vocab / 32 && a.length <= 8192) {
     const dim3 grid((unsigned)(a.rows < (1 << 20) ? a.rows : 1 << 20), (unsigned)a.k);
     if (a.length <= 1024) {
@@ -181,7 +182,7 @@ hipError_t adjust(const AdjustArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((adjust_history_kernel<E, 16384, 1024>), grid, dim3(1024), 0, s, a);
     return hipGetLastError();
   }
-  // four pieces a thread (512 rows of 131072, bf16, everything on: 69 us; with spans of 4096 71, 2048 93, 16384 83)
+  // four pieces a thread (512 rows of 131072, bf16, everything on, before other steps: 69 us; with spans of 4096 71, 2048 93, 16384 83)
   constexpr int SPAN = 4 * kThreads * E::V;
   const dim3 grid((unsigned)ceil_div(a.vocab, SPAN), (unsigned)(a.rows < 65535 ? a.rows : 65535), (unsigned)a.k);
   if (a.bias) hipLaunchKernelGGL((adjust_kernel<E, true, SPAN>), grid, dim3(kThreads), 0, s, a);

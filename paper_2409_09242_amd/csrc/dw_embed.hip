@@ -335,6 +335,7 @@ __device__ __forceinline__ void sum_chunk(const SumArgs& s, int w, int64_t c, in
   const typename E::T* dy = reinterpret_cast<const typename E::T*>(a.dy.p) + w * a.dy.stride + e0;
   float* grad = a.grad + w * a.grad_stride + e0;
   float* part = s.part + (w * s.chunks + c) * 2 * a.n + e0;
+  if (key[0] >= a.vocab) return;                           // nothing but what is no token
   uint32_t raw[kChunk][W == 1 ? 1 : 4];
 #pragma unroll
   for (int i = 0; i < kChunk; ++i) {

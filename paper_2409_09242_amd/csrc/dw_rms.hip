@@ -16,10 +16,10 @@
 // Backward: a group of threads takes every strips-th row of one worker and keeps its column sums in registers; one row of partial
 // sums per block goes to scratch, and a second kernel adds those up in their order.
 //
-// Bound by memory at the rate of its mix of reads and writes (a copy 4.75 TB/s, two reads a write 5.9): forward 16 x 512 rows of 4096,
-// bf16, with a residual 54 us = 5.0 TB/s, its 8-bit form with dropout, 8 x 1024 x 4096, 43 us = 5.4 and 26 for the transposed form;
-// backward 3 x 2731 rows of 5003, fp32, with a gradient from further on and a dropout's own output 161 us = 5.1 TB/s, and 5 for the
-// columns' sums.  One row 3.7 us.  Rows that registers do not hold (above 32768 columns, backward in bf16 above 16384) 2.3 TB/s.
+// Bound by memory (a copy reaches 4.75 TB/s, two reads a write 5.9; what is still in the chip's cache comes on top): forward 16 x 512 rows
+// of 4096, bf16, with a residual 43 us = 6.2 TB/s, its 8-bit form with dropout, 8 x 1024 x 4096, 43 us = 5.4 and 20 for the transposed
+// form; backward 3 x 2731 rows of 5003, fp32, with a gradient from further on and a dropout's own output 161 us = 5.1 TB/s, and 5 for the
+// columns' sums.  One row 3.7 us.  Rows that registers do not hold: above 32768 columns forward 3.9 TB/s, backward (in bf16 above 16384) 2.3.
 #include "dw_dropout.h"
 #include "dw_fp8.h"
 
