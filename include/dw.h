@@ -430,9 +430,10 @@ int dw_embedding_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const 
 /*
  * Dropout: y = residual + m x / q.  m is 1 where a 16-bit number of the counter-based stream is below round((1 - p) 65536), else 0,
  * and q = round((1 - p) 65536) / 65536, so that y's mean is x's (p comes in steps of 2^-16).  Element j of row r of worker w takes bits
- * 16 (j mod 4) to 16 (j mod 4) + 15 of mix(key(seed, w, step) + GAMMA*(r*ceil(n/4) + floor(j/4) + 1)), mix and GAMMA SplitMix64's and
- * key(seed, w, step) = mix(mix(seed + GAMMA*(w+1)) + GAMMA*(step+1)), as for the Rademacher stream: the mask is stored nowhere, and the backward pass is the same call on dy without a residual.  Give every
- * dropout of a model a seed of its own, other than the configuration's.
+ * 16 (j mod 4) to 16 (j mod 4) + 15 of mix(key(seed, w, step) + GAMMA*(r*ceil(n/4) + floor(j/4) + 1)), mix and GAMMA SplitMix64's
+ * and key(seed, w, step) = mix(mix(seed + GAMMA*(w+1)) + GAMMA*(step+1)), as for the Rademacher stream: the mask is stored nowhere,
+ * and the backward pass is the same call on dy without a residual.  Give every dropout of a model a seed of its own, other than
+ * the configuration's.
  *   p           0 <= p <= 1; a dropped element's x is not looked at (an infinity or NaN there leaves no trace)
  *   d_step      NULL, or a device address of one 64-bit number that is added to `step` when the work runs: a captured graph
  *               whose caller counts it up draws another mask at every replay
@@ -454,6 +455,7 @@ int dw_dropout(const void* d_x, int64_t x_ld, int64_t x_stride, const void* d_re
  *               form; NULL: not wanted.  The transposed form is made by a second pass, from h (d_x where h is x) and d_rstd, which it
  *               then needs
  *   d_rstd      [k][rows] floats receiving r; NULL: not wanted
+ * rows, n and eps as for dw_layer_norm; rows <= DW_MAX_FP8 with an output in 8 bits.
  */
 int dw_rms_norm(const void* d_x, int64_t x_ld, int64_t x_stride, const void* d_residual, int64_t residual_ld,
                 int64_t residual_stride, const float* d_gamma, int64_t param_stride, int k, int64_t rows, int64_t n, int dtype,

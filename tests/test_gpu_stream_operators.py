@@ -201,6 +201,39 @@ def test_more_rows_than_16_bits_count():
     assert torch.equal(OPS.embedding(token, x), x.flip(1)) and torch.equal(OPS.embedding_grad(dy, token, rows), dy.flip(1))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_workers_interleaved_row_by_row(dtype):
+    """Tensors [rows][k][n] seen as [k][rows][n], as inputs and outputs."""
+    g = _gen(12)
+    k, rows, n = 3, 41, 203
+
+    def woven(like=None):
+        t = torch.randn(rows, k, n, generator=g, device=DEV).to(dtype).transpose(0, 1)
+        return t if like is None else t.copy_(like)
+    x, res, dy = woven(), woven(), woven()
+    gamma = torch.randn(k, n, generator=g, device=DEV)
+    plain = [t.contiguous() for t in (x, res, dy)]
+    want = OPS.rms_norm(plain[0], gamma, residual=plain[1], p=0.3, seed=1)
+    got = OPS.rms_norm(x, gamma, residual=res, p=0.3, seed=1, out=woven(), sum_out=woven())
+    _same(_flat(got), _flat(want))
+    _same(_flat(OPS.rms_norm_fp8(x, gamma, residual=res, transposed=True, sum_out=woven())), _flat(OPS.rms_norm_fp8(plain[0], gamma, residual=plain[1], transposed=True)))
+    want = OPS.rms_norm_grad(plain[2], plain[0], gamma, want[2], dh=plain[1], p=0.3, seed=1)
+    _same(_flat(OPS.rms_norm_grad(dy, x, gamma, got[2], dh=res, p=0.3, seed=1, dres=woven(), dx=woven())), _flat(want))
+    assert torch.equal(OPS.dropout(x, 0.3, 2, residual=res, out=woven()), OPS.dropout(plain[0], 0.3, 2, residual=plain[1]))
+    token = torch.randint(-1, rows, (k, rows), generator=g, device=DEV, dtype=torch.int32)
+    assert torch.equal(OPS.embedding(token, x, 2.0, out=woven()), OPS.embedding(token, plain[0], 2.0))
+    for vocab in (rows, 40 * rows):                          # zeros at the end, and in front
+        grad = torch.full((vocab, k, n), 7.0, device=DEV).transpose(0, 1)
+        assert torch.equal(OPS.embedding_grad(dy, token, out=grad), OPS.embedding_grad(plain[2], token, vocab))
+    history = torch.randint(0, n, (rows, k, 9), generator=g, device=DEV, dtype=torch.int32).transpose(0, 1)
+    bias, mask = torch.randn(rows, k, n, generator=g, device=DEV).transpose(0, 1), torch.randint(-9, 9, (rows, k, 7), generator=g, device=DEV, dtype=torch.int32).transpose(0, 1)
+    rep = torch.rand(k, rows, generator=g, device=DEV) + 0.5
+    want = OPS.adjust_logits(plain[0], history.contiguous(), repetition=rep, bias=bias.contiguous(), mask=mask.contiguous())
+    assert torch.equal(OPS.adjust_logits(x, history, repetition=rep, bias=bias, mask=mask, out=woven()), want)
+    OPS.adjust_logits(x, history, repetition=rep, bias=bias, mask=mask, out=x)
+    assert torch.equal(x, want)
+
+
 def test_written_tensors_count_as_changed():
     """A graph that saved a tensor which a call has written into since refuses its backward pass."""
     x, g = torch.randn(1, 4, 40, device=DEV), torch.randn(1, 40, device=DEV)
