@@ -10,14 +10,13 @@
 // those in their order.  So every row of dy is read once, in fp32 sums whose order follows from the tokens alone, and a
 // token that fills the whole batch costs no more than others.
 //
-// The sort: up to kRankRows places by counting (a place's rank is the number of smaller tokens, and of equal ones before it), which is
+// The sort: few places by counting (a place's rank is the number of smaller tokens, and of equal ones before it), which is
 // n^2 comparisons but a single launch; longer lists digit by digit, eight bits at a time from the lowest, in blocks of kTile
-// places whose counts of every digit are added up between the two passes over them.  One worker's 8192 places by counting 15 us, by
-// digits (two of them) 34; 65536 places 47.
+// places whose counts of every digit are added up between the two passes over them.
 //
 // Where the whole gradient is wanted, rows that no token has are filled with zeros beside the sort or beside the last sums.
-// Bound by writing them: 4 x 4096 rows of 4096, bf16, over 32000 tokens 422 us a call, 2.4 GB at 5.7 TB/s (a fill alone reaches 6.4);
-// added to a gradient that is there 115.  3 x 333 rows of 1001, fp32, over 5003: 19.5, three launches.  Lookups: 8 x 1024 rows of 4096,
+// Bound by writing them: 4 x 4096 rows of 4096, bf16, over 32000 tokens 377 us a call, 2.4 GB at 6.4 TB/s (a fill alone reaches 6.8);
+// added to a gradient that is there 119.  3 x 333 rows of 1001, fp32, over 5003: 20.0, three launches.  Lookups: 8 x 1024 rows of 4096,
 // fp32 to bf16, 31 us = 6.4 TB/s of what passes (common rows come from the caches); one row 2.0.
 #include "dw_ops.h"
 
@@ -115,7 +114,14 @@ hipError_t lookup(const EmbedArgs& a, hipStream_t s) {
 
 // ---- places by token -------------------------------------------------------------------------------------------------
 
-constexpr int kRankRows = 8192;                            // up to here by counting
+// Up to so many comparisons by counting, in one launch, else by digits, in three for each eight bits (with the sums of 64 columns, us: one
+// worker's 8192 places 30 and 50, 16384 45 and 53, 32768 102 and 56; four workers' 8192 42 and 52, 16384 99 and 56; eight workers' 8192 63 and 56)
+constexpr double kRankWork = 268435456.0;
+// From so many bytes of zeros a worker's counting blocks are in front of its own zeros, below all workers' in front of all (us a call, own and
+// all: 4 x 4096 rows over 32000 by 4096 392 and 401, 4 x 2048 by 2048 181 and 188, 2 x 2048 by 2048 100 and 103; 4 x 1024 over 8000 by
+// 1024 33.1 and 31.9, 3 x 333 over 5003 by 1001 24.0 and 21.7; every 16th block of a row, which are all one die's: 445 for the first)
+constexpr double kOwnRowBytes = 268435456.0;
+constexpr int kRankPlaces = 16, kRankTile = 2048;          // places of a block, keys in its LDS
 constexpr int kTile = 4096;                                // places of a block when sorting by digits, 1024 a wave
 constexpr int kChunk = 16;                                 // places whose rows a group of threads adds up
 
@@ -158,44 +164,75 @@ __device__ __forceinline__ void zero_part(const ZeroArgs& a, int w, int64_t bloc
   for (int64_t v = v0 + (threadIdx.x >> 6); v < v1; v += 4) zero_floats(grad + v * a.ld, a.n);
 }
 
-// 64 places a block, their keys against all of the worker's by four waves, 64 others at a time: a wave has those in its lanes, the next
-// on their way, and hands them round one after another.  Of places before the block's an equal key counts, of those behind
-// not, and of its own those of lower lanes.  The blocks behind these write zeros.
+// 16 places a block, each by 16 threads: the worker's keys go through LDS kRankTile at a time, and every thread compares its place's
+// with a sixteenth of them, four to a read that a quarter of a wave shares.  Of keys before the block's an equal one counts, of
+// those behind not; only a wave that has the block's own among its keys looks at where each stands.  The first blocks of a grid
+// row are a worker's, or those of row 0 all workers' (in_first_row of them), the others write zeros.
 __global__ __launch_bounds__(256) void rank_kernel(const int32_t* __restrict__ token, int32_t* __restrict__ sorted, int32_t* __restrict__ place, int rows,
-                                                   int32_t vocab, int rank_blocks, ZeroArgs zero) {
-  __shared__ int part[4][64];
-  if ((int64_t)blockIdx.x >= rank_blocks) {
-    zero_part(zero, blockIdx.y, (int64_t)blockIdx.x - rank_blocks, vocab);
+                                                   int32_t vocab, int rank_blocks, int in_first_row, ZeroArgs zero) {
+  __shared__ __align__(16) uint32_t keys[kRankTile];
+  __shared__ int part[4][kRankPlaces];
+  const uint32_t in_front = in_first_row == 0 ? (uint32_t)rank_blocks : blockIdx.y == 0 ? (uint32_t)in_first_row : 0u;
+  if (blockIdx.x >= in_front) {
+    if (blockIdx.x - in_front < zero.blocks) zero_part(zero, blockIdx.y, blockIdx.x - in_front, vocab);
     return;
   }
+  const int w = in_first_row == 0 ? (int)blockIdx.y : (int)(blockIdx.x / (uint32_t)rank_blocks);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t* tok = token + (int64_t)blockIdx.y * rows;
-  const int own = blockIdx.x, r = own * 64 + lane;
+  const int32_t* tok = token + (int64_t)w * rows;
+  const int r0 = ((int)blockIdx.x - (in_first_row == 0 ? 0 : w * rank_blocks)) * kRankPlaces, r = r0 + (lane & 15);
   const uint32_t last = (uint32_t)vocab;                   // (what is no token is behind it, also as an unsigned number below zero)
-  auto key = [&](int s) { const uint32_t v = (uint32_t)tok[s]; return v < last ? v : last; };
-  auto others_of = [&](int g) { return g * 64 + lane < rows ? key(g * 64 + lane) : ~0u; };       // (none: above every key)
-  uint32_t next = others_of(wave);
+  auto key = [&](int s) {
+    const uint32_t v = s < rows ? (uint32_t)tok[s] : ~0u;
+    return s >= rows ? ~0u : v < last ? v : last;          // (none: above every key)
+  };
+  uint32_t next[kRankTile / 256];
+  auto fetch = [&](int s0) {
+#pragma unroll
+    for (int i = 0; i < kRankTile / 256; ++i) next[i] = key(s0 + i * 256 + (int)threadIdx.x);
+  };
+  fetch(0);
   const uint32_t mine = r < rows ? key(r) : 0u;
   int rank = 0;
-  for (int g = wave; g * 64 < rows; g += 4) {
-    const uint32_t others = next;
-    next = others_of(g + 4);
-    if (g != own) {
-      const uint32_t limit = g < own ? mine + 1u : mine;
+  for (int s0 = 0; s0 < rows; s0 += kRankTile) {
+    __syncthreads();                                       // (the tile before has been read)
 #pragma unroll
-      for (int i = 0; i < 64; ++i) rank += (uint32_t)__builtin_amdgcn_readlane((int)others, i) < limit ? 1 : 0;
+    for (int i = 0; i < kRankTile / 256; ++i) keys[i * 256 + threadIdx.x] = next[i];
+    __syncthreads();
+    if (s0 + kRankTile < rows) fetch(s0 + kRankTile);
+    const int of_wave = s0 + wave * (kRankTile / 4), of_thread = wave * (kRankTile / 4) + (lane >> 4) * (kRankTile / 16);
+    const uint4* four = reinterpret_cast<const uint4*>(keys + of_thread);
+    if (r0 + kRankPlaces <= of_wave || r0 >= of_wave + kRankTile / 4) {
+      const uint32_t limit = r0 > of_wave ? mine + 1u : mine;
+#pragma unroll 8
+      for (int i = 0; i < kRankTile / 64; ++i) {
+        const uint4 k = four[i];
+        rank += k.x < limit ? 1 : 0;
+        rank += k.y < limit ? 1 : 0;
+        rank += k.z < limit ? 1 : 0;
+        rank += k.w < limit ? 1 : 0;
+      }
     } else {
-#pragma unroll
-      for (int i = 0; i < 64; ++i) rank += (uint32_t)__builtin_amdgcn_readlane((int)others, i) < mine + (i < lane ? 1u : 0u) ? 1 : 0;
+      const int before = r - (s0 + of_thread);             // of this thread's keys those below it stand before its place
+#pragma unroll 4
+      for (int i = 0; i < kRankTile / 64; ++i) {
+        const uint4 k = four[i];
+        rank += k.x < mine + (4 * i < before ? 1u : 0u) ? 1 : 0;
+        rank += k.y < mine + (4 * i + 1 < before ? 1u : 0u) ? 1 : 0;
+        rank += k.z < mine + (4 * i + 2 < before ? 1u : 0u) ? 1 : 0;
+        rank += k.w < mine + (4 * i + 3 < before ? 1u : 0u) ? 1 : 0;
+      }
     }
   }
-  part[wave][lane] = rank;
+  rank += __shfl_xor(rank, 16);
+  rank += __shfl_xor(rank, 32);
+  if (lane < kRankPlaces) part[wave][lane] = rank;
   __syncthreads();
-  if (wave != 0 || r >= rows) return;
+  if (threadIdx.x >= kRankPlaces || r >= rows) return;
 #pragma unroll
   for (int q = 1; q < 4; ++q) rank += part[q][lane];
-  sorted[(int64_t)blockIdx.y * rows + rank] = (int32_t)mine;
-  place[(int64_t)blockIdx.y * rows + rank] = r;
+  sorted[(int64_t)w * rows + rank] = (int32_t)mine;
+  place[(int64_t)w * rows + rank] = r;
 }
 
 // the keys of a pass: the tokens themselves in the first, what the one before wrote in the others
@@ -493,11 +530,12 @@ __global__ __launch_bounds__(256) void embed_join_kernel(SumArgs s) {
 struct GradLayout {
   size_t key, place, key2, place2, count, part, total;
   int64_t tiles, chunks;
+  bool digits;
   GradLayout(int k, int64_t rows, int64_t n) : tiles(ceil_div(rows, kTile)), chunks(ceil_div(rows, kChunk)) {
     size_t pos = 0;
     auto take = [&](size_t bytes) { const size_t at = pos; pos += (bytes + 255) / 256 * 256; return at; };
     const size_t list = (size_t)k * rows * 4;
-    const bool digits = rows > kRankRows;
+    digits = (double)k * rows * rows > kRankWork;
     key = take(list);
     place = take(list);
     key2 = take(digits ? list : 0);
@@ -534,21 +572,22 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, hipStream_t 
   const GradLayout lay(a.k, a.rows, a.n);
   int32_t* key = reinterpret_cast<int32_t*>(a.scratch + lay.key);
   int32_t* place = reinterpret_cast<int32_t*>(a.scratch + lay.place);
-  // The zeros: where at most a quarter of the rows can have a token, all rows beside the sort, which leaves the memory to them, and those
-  // few are written once more; otherwise, where that would write up to all of them twice, at the end those that no token has, looked for
-  // one by one (4 x 4096 rows of 4096 over 32000, the whole call: 422 us, the other way 434; 3 x 333 rows of 1001 over 5003: 19.5 and
-  // 20.8).  At most 256 KB a block, and four blocks a compute unit where there are as many rows (the latter at the end: 22.9 us by 65 rows
-  // a block, 21.0 by 15).
+  // The zeros: where at most a quarter of the rows can have a token, all rows beside the sort, page by page, and those few are written
+  // once more; otherwise, where that would write up to all of them twice, at the end those that no token has, looked for one by one, at
+  // most 256 KB a block, and four blocks a compute unit where there are as many rows (4 x 4096 rows of 4096 over 32000, the whole call: 377
+  // us, the other way 434; 3 x 333 rows of 1001 over 5003: 20.0 and 20.8, and that 22.9 by 65 rows a block).
   const bool first = !a.accumulate && a.vocab / 4 >= a.rows, last = !a.accumulate && !first;
   const int64_t by_size = a.n >= 4096 ? 16 : a.n <= 256 ? 256 : 65536 / a.n, share = ceil_div(a.vocab * a.k, 4 * kCus);
   const int fill_rows = (int)(share < by_size ? share : by_size);
-  const bool digits = a.rows > kRankRows;
-  const int rank_blocks = digits ? 0 : (int)ceil_div(a.rows, 64);
+  const bool digits = lay.digits;
+  const int rank_blocks = digits ? 0 : (int)ceil_div(a.rows, kRankPlaces);
   ZeroArgs zero = {a.grad, a.grad_ld, a.grad_stride, a.n, fill_rows, 0};
   if (first) zero.blocks = a.grad_ld == a.n ? ceil_div(a.vocab * a.n * 4, kPage) + 1 : ceil_div(a.vocab, fill_rows);       // (a page more: it may begin within one)
-  if (rank_blocks + zero.blocks > 0) {
-    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)(rank_blocks + zero.blocks), (unsigned)a.k), dim3(256), 0, s, a.token, key, place,
-                       digits ? 0 : (int)a.rows, (int32_t)a.vocab, rank_blocks, zero);
+  const bool own_row = first && (double)a.k * a.vocab * a.n * 4.0 >= kOwnRowBytes;
+  const int in_front = rank_blocks * (own_row ? 1 : a.k);
+  if (in_front + zero.blocks > 0) {
+    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)(in_front + zero.blocks), (unsigned)(own_row || zero.blocks > 0 ? a.k : 1)), dim3(256), 0, s, a.token, key,
+                       place, digits ? 0 : (int)a.rows, (int32_t)a.vocab, rank_blocks, own_row ? 0 : in_front, zero);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (digits) {

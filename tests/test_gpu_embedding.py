@@ -123,6 +123,23 @@ def test_a_token_alone_in_a_large_batch():
             assert torch.equal(got[0].double(), want)
 
 
+# around the counting blocks' places and the keys they hold at a time, on both sides of the change of sorts by workers, and of the
+# amount of zeros from which a worker's counting blocks stand in front of its own (k * vocab * n * 4 = 2^28)
+@pytest.mark.parametrize("k,rows,vocab,n", [(3, 15, 9, 2), (3, 16, 9, 2), (3, 17, 100, 2), (2, 2047, 30, 2), (2, 2048, 9000, 2), (2, 2049, 2, 2), (3, 4113, 700, 3),
+                                            (1, 16384, 900, 2), (1, 16385, 900, 2), (4, 8192, 40000, 2), (4, 8193, 40000, 2), (64, 2048, 50, 2), (64, 2049, 50, 2),
+                                            (4, 500, 4096, 4095), (4, 500, 4096, 4096), (3, 333, 45001, 517), (2, 12000, 50000, 700)])
+def test_places_in_order(k, rows, vocab, n):
+    """Whole numbers, whose sums are exact whatever their order, each worker's own."""
+    g = _gen(rows + k)
+    dy = torch.randint(-8, 9, (k, rows, n), generator=g, device=DEV).float()
+    token = torch.randint(-1, vocab + 1, (k, rows), generator=g, device=DEV, dtype=torch.int32)
+    got = OPS.embedding_grad(dy, token, vocab)
+    kept = (token >= 0) & (token < vocab)
+    for w in range(k):
+        want = torch.zeros(vocab, n, device=DEV).index_add_(0, token[w][kept[w]].long(), dy[w][kept[w]])
+        assert torch.equal(got[w], want), "worker %d" % w
+
+
 def test_gradient_against_differences():
     """The lookup is linear in the table: <embedding(T), dy> = <T, embedding_grad(dy)>."""
     g = _gen(6)

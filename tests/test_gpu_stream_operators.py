@@ -70,7 +70,7 @@ def _adjust(dtype):
 
 
 # rows of a wave, of a block, too long for registers; places sorted by counting and by digits
-CASES = [_norm(64), _norm(1003), _norm(33000), _embed(300, 50, 33), _embed(9000, 700, 8), _adjust]
+CASES = [_norm(64), _norm(1003), _norm(33000), _embed(300, 50, 33), _embed(9000, 700, 8), _embed(20000, 700, 8), _adjust]
 
 
 def _fill(inputs, g):
