@@ -416,6 +416,7 @@ int dw_fp8_linear(const void* d_x, int64_t x_ld, int64_t x_stride, const uint8_t
  *   d_table     rows of n in `table_dtype`, worker w's row v at w*table_stride + v*table_ld; y in `dtype`
  *   d_grad      [k][vocab] rows of n floats.  accumulate 0: every row is written, zeros where no token was; 1: the sums are added
  *               to the rows of the tokens that are there, and the others are not touched
+ * The gradient takes up to 2^27 rows and 2^36 numbers of dy a worker; more return DW_ERR_TOO_LARGE.
  * The rows of a token are added in fp32, in an order that follows from the tokens alone: no atomics.  (Of a table that the workers
  * share, table_stride 0, each worker's gradient is its own part; their sum is the table's.)
  */

@@ -142,14 +142,15 @@ __device__ __forceinline__ void zero_floats(float* p, int64_t n) {
 // blocks that run at the same time then write next to each other, which is what memory takes fastest (2 GB: 6.8 TB/s; two pieces a
 // thread 6.0, four 5.9, 64 KB a block 5.6, a row of 16 KB a wave 6.2 and of 6932 bytes 4.9)
 constexpr int kPage = 4096;
+constexpr int64_t kMostPages = 1 << 23;                    // of a worker (a launch has fewer than 2^32 threads a row); above by rows
 struct ZeroArgs {
   float* grad; int64_t ld, stride, n;
-  int block_rows;                                          // where rows have gaps
+  int block_rows;                                          // otherwise; 0: pages
   int64_t blocks;                                          // of a worker
 };
 __device__ __forceinline__ void zero_part(const ZeroArgs& a, int w, int64_t block, int64_t vocab) {
   float* grad = a.grad + w * a.stride;
-  if (a.ld == a.n) {
+  if (a.block_rows == 0) {
     const uintptr_t from = reinterpret_cast<uintptr_t>(grad), to = from + (uintptr_t)(vocab * a.n) * 4;
     const uintptr_t p = from / kPage * kPage + (uintptr_t)block * kPage + threadIdx.x * 16;
     if (p >= from && p + 16 <= to) {
@@ -581,8 +582,10 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, hipStream_t 
   const int fill_rows = (int)(share < by_size ? share : by_size);
   const bool digits = lay.digits;
   const int rank_blocks = digits ? 0 : (int)ceil_div(a.rows, kRankPlaces);
-  ZeroArgs zero = {a.grad, a.grad_ld, a.grad_stride, a.n, fill_rows, 0};
-  if (first) zero.blocks = a.grad_ld == a.n ? ceil_div(a.vocab * a.n * 4, kPage) + 1 : ceil_div(a.vocab, fill_rows);       // (a page more: it may begin within one)
+  const int64_t pages = ceil_div(a.vocab * a.n * 4, kPage) + 1;                 // (one more: it may begin within one)
+  const bool by_page = a.grad_ld == a.n && pages <= kMostPages;
+  ZeroArgs zero = {a.grad, a.grad_ld, a.grad_stride, a.n, by_page ? 0 : fill_rows, 0};
+  if (first) zero.blocks = by_page ? pages : ceil_div(a.vocab, fill_rows);
   const bool own_row = first && (double)a.k * a.vocab * a.n * 4.0 >= kOwnRowBytes;
   const int in_front = rank_blocks * (own_row ? 1 : a.k);
   if (in_front + zero.blocks > 0) {

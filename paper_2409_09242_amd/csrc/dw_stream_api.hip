@@ -61,6 +61,7 @@ int dw_embedding_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const 
   if (k < 1 || k > DW_MAX_K || !is_type(dtype)) return DW_ERR_CONFIG;
   if (!shape_ok(rows, n) || vocab < 1 || vocab > DW_MAX_VOCAB || (accumulate != 0 && accumulate != 1)) return DW_ERR_ARG;
   if (!std::isfinite(scale)) return DW_ERR_HYPER;
+  if (rows > (1 << 27) || rows * n > (1ll << 36)) return DW_ERR_TOO_LARGE;      // (2^24 blocks of 256 threads are too many for a launch)
   if (rows == 0 && accumulate) return DW_OK;
   if (!d_grad) return DW_ERR_NULL;
   if (!out_ok(d_grad, grad_ld, grad_stride, k, vocab, n, 4)) return DW_ERR_ARG;

@@ -140,6 +140,20 @@ def test_places_in_order(k, rows, vocab, n):
         assert torch.equal(got[w], want), "worker %d" % w
 
 
+def test_gradient_of_more_zeros_than_a_launch_has_pages():
+    """A table of 2^35 bytes and a few rows, with and without a page more than a launch writes."""
+    for vocab in ((1 << 21) - 1, (1 << 21) + 1):
+        out = torch.full((1, vocab, 4096), 3.0, device=DEV)
+        token = torch.tensor([[5, vocab - 1, 5]], dtype=torch.int32, device=DEV)
+        dy = torch.ones(1, 3, 4096, device=DEV)
+        OPS.embedding_grad(dy, token, vocab, out=out)
+        assert bool((out[0, 5] == 2).all()) and bool((out[0, vocab - 1] == 1).all())
+        out[0, 5] = 0
+        out[0, vocab - 1] = 0
+        assert all(not bool(part.any()) for part in out[0].split(1 << 16))
+        del out
+
+
 def test_gradient_against_differences():
     """The lookup is linear in the table: <embedding(T), dy> = <T, embedding_grad(dy)>."""
     g = _gen(6)

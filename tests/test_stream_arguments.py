@@ -11,7 +11,7 @@ from paper_2409_09242_amd import operators as OPS
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 P = 0x10000              # addresses that are never followed: every call below is refused, or has nothing to do
-NULL, CONFIG, HYPER, WORKSPACE, ARG = -1, -2, -3, -4, -5
+NULL, CONFIG, HYPER, WORKSPACE, ARG, TOO_LARGE = -1, -2, -3, -4, -5, -8
 NAN, INF = float("nan"), float("inf")
 
 
@@ -43,6 +43,7 @@ def test_embedding(kw, status):
     (dict(scale=NAN), HYPER), (dict(grad=None), NULL), (dict(dy=None), NULL), (dict(token=None), NULL), (dict(token=P + 1), ARG), (dict(dy=P + 2), ARG),
     (dict(dy=2 * P), ARG), (dict(ld=7), ARG), (dict(g_ld=7), ARG), (dict(g_st=79), ARG), (dict(g_st=0), ARG), (dict(grad=2 * P + 2), ARG),
     (dict(scratch=None), WORKSPACE), (dict(scratch=P + 64), WORKSPACE), (dict(bytes=16), WORKSPACE), (dict(rows=0, acc=1), 0),
+    (dict(rows=(1 << 27) + 1), TOO_LARGE), (dict(rows=1 << 20, n=65537, ld=65537, st=65537 << 20, g_ld=65537, g_st=655370), TOO_LARGE),
 ])
 def test_embedding_grad(kw, status):
     a = dict(dy=P, ld=8, st=24, token=P, k=2, rows=3, vocab=10, n=8, dtype=0, scale=1.0, acc=0, grad=2 * P, g_ld=8, g_st=80, scratch=P, bytes=1 << 20,
