@@ -9,6 +9,8 @@ using namespace dw;
 namespace {
 
 inline bool shape_ok(int64_t rows, int64_t n) { return rows >= 0 && rows < kMaxRows && n >= 1 && n <= DW_MAX_NORM; }
+// the table gradient's (2^24 blocks of 256 threads are too many for a launch)
+inline bool grad_rows_ok(int64_t rows, int64_t n) { return rows <= 1 << 27 && rows * n <= 1ll << 36; }
 inline bool share_ok(float p) { return p >= 0.f && p <= 1.f; }
 
 // a 16-bit number below the limit keeps an element
@@ -51,7 +53,7 @@ int dw_embedding(const int32_t* d_token, const void* d_table, int64_t table_ld, 
 }
 
 size_t dw_embedding_grad_scratch_bytes(int k, int64_t rows, int64_t vocab, int64_t n) {
-  if (k < 1 || k > DW_MAX_K || !shape_ok(rows, n) || vocab < 1 || vocab > DW_MAX_VOCAB || rows == 0) return 0;
+  if (k < 1 || k > DW_MAX_K || !shape_ok(rows, n) || vocab < 1 || vocab > DW_MAX_VOCAB || rows == 0 || !grad_rows_ok(rows, n)) return 0;
   return embedding_grad_scratch(k, rows, vocab, n);
 }
 
@@ -61,7 +63,7 @@ int dw_embedding_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const 
   if (k < 1 || k > DW_MAX_K || !is_type(dtype)) return DW_ERR_CONFIG;
   if (!shape_ok(rows, n) || vocab < 1 || vocab > DW_MAX_VOCAB || (accumulate != 0 && accumulate != 1)) return DW_ERR_ARG;
   if (!std::isfinite(scale)) return DW_ERR_HYPER;
-  if (rows > (1 << 27) || rows * n > (1ll << 36)) return DW_ERR_TOO_LARGE;      // (2^24 blocks of 256 threads are too many for a launch)
+  if (!grad_rows_ok(rows, n)) return DW_ERR_TOO_LARGE;
   if (rows == 0 && accumulate) return DW_OK;
   if (!d_grad) return DW_ERR_NULL;
   if (!out_ok(d_grad, grad_ld, grad_stride, k, vocab, n, 4)) return DW_ERR_ARG;

@@ -57,6 +57,7 @@ def test_scratch_sizes():
     f = lib.dw_embedding_grad_scratch_bytes
     assert f(0, 10, 10, 8) == f(1, 0, 10, 8) == f(1, 10, 0, 8) == f(1, 10, 10, 0) == 0
     assert f(1, 10, 10, 8) >= 2 * 10 * 4
+    assert f(1, 1 << 27, 10, 512) > 0 and f(1, (1 << 27) + 1, 10, 512) == f(1, 1 << 27, 10, 513) == 0
     for rows in (1, 31, 33, 1000, 8192, 8193, 100000):       # two lists of places, partial sums, and what sorting takes
         assert 2 * 3 * rows * 4 <= f(3, rows, 50, 64) <= 3 * (rows * (16 + 64) + 64 * 4 * 4) + (1 << 20)
     g = lib.dw_rms_norm_grad_scratch_bytes
