@@ -18,7 +18,7 @@
 //
 // Bound by memory (a copy reaches 4.75 TB/s, two reads a write 5.9; what is still in the chip's cache comes on top): forward 16 x 512 rows
 // of 4096, bf16, with a residual 43 us = 6.2 TB/s, its 8-bit form with dropout, 8 x 1024 x 4096, 43 us = 5.4 and 20 for the transposed
-// form; backward 3 x 2731 rows of 5003, fp32, with a gradient from further on and a dropout's own output 161 us = 5.1 TB/s, and 5 for the
+// form; backward 3 x 2731 rows of 5003, fp32, with a gradient from further on and a dropout's own output 157 us = 5.2 TB/s, and 5 for the
 // columns' sums.  One row 3.7 us.  Rows that registers do not hold: above 32768 columns forward 3.9 TB/s, backward (in bf16 above 16384) 2.3.
 #include "dw_dropout.h"
 #include "dw_fp8.h"
@@ -95,7 +95,7 @@ struct Split {
 
 // ITEMS pieces of a row and its odd element as they are in memory, so that nothing waits for them before they are used; what a thread
 // has not reads as zero.  They stream through once: without displacing what is read again, they are read faster too (16384 x 4096, bf16,
-// forward: 85 us and 105, backward 95 and 108).
+// forward: 85 us and 105, backward, with more blocks, 95 and 108).
 template <class E, int TPR, int ITEMS>
 struct RowRegs {
   uint32_t piece[ITEMS][4], odd;
@@ -478,14 +478,23 @@ __global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(RmsGradArgs a)
   }
 }
 
-// dgamma from the blocks' partial sums: 64 columns a block, its 16 waves take every 16th strip each
+// dgamma from the blocks' partial sums: 64 columns a block, its 16 waves take every 16th strip each, eight at a time (they are few
+// columns, so that the trips to memory are what it takes)
 __global__ __launch_bounds__(1024) void rms_norm_strips_kernel(RmsGradArgs a) {
   __shared__ float lds[16][64];
   const int w = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n = a.n, e = (int64_t)blockIdx.x * 64 + lane;
   float s = 0.f;
-  if (e < n)
-    for (int p = wave; p < a.strips; p += 16) s += a.part[((int64_t)w * a.strips + p) * n + e];
+  if (e < n) {
+    const float* part = a.part + (int64_t)w * a.strips * n + e;
+    for (int p = wave; p < a.strips; p += 128) {
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = p + 16 * j < a.strips ? part[(p + 16 * j) * n] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += f[j];
+    }
+  }
   lds[wave][lane] = s;
   __syncthreads();
   if (wave == 0 && e < n) {
@@ -542,10 +551,14 @@ hipError_t forward(const RmsArgs& a, hipStream_t s) {
 }
 
 template <class E> constexpr bool kWideGrad = E::V == 4;
-// blocks of the backward pass, few, so that there are few rows of partial sums: 256 threads twice a compute unit in bf16 (32768 x 2048:
-// 104 us, with three 113, with four 123), four times in fp32, whose rows have half as many columns (262, 210, 195)
+// Blocks of the backward pass: a unit reads best with 8 KB or more of rows from each tensor at work, not many more, and fewer leave fewer rows of
+// partial sums (us with 1, 2, 3 and 4 a unit: bf16, 65536 x 1024, 8 KB a block 88, 88, 93, 98; 1024 x 4096, 8 KB 14, 17, 19, 22;
+// 13413 x 5003, 10 KB 128, 132, 134, 139; 32768 x 2048, 4 KB 126, 89, 92, 93; fp32, 129055 x 520, 2 KB 421, 248, 218, 227)
 template <class E>
-int64_t grad_blocks(int tpr) { return (tpr >= 1024 ? 1 : tpr >= 512 ? 2 : tpr >= 256 && E::V == 8 ? 2 : 4) * (int64_t)kCus; }
+int64_t grad_blocks(int groups, int64_t n) {
+  const int64_t bytes = groups * n * (int64_t)sizeof(typename E::T);
+  return (bytes >= 8192 ? 1 : bytes >= 3000 ? 2 : 3) * (int64_t)kCus;
+}
 
 template <class E>
 struct Backward {
@@ -559,9 +572,9 @@ struct Backward {
 };
 template <class E>
 struct Strips {
-  int k; int64_t rows; int* strips;
+  int k; int64_t rows, n; int* strips;
   template <int TPR, int ITEMS>
-  void operator()() const { *strips = (int)blocks_per_worker(k, rows, block_of(TPR) / TPR, grad_blocks<E>(TPR)); }
+  void operator()() const { *strips = (int)blocks_per_worker(k, rows, block_of(TPR) / TPR, grad_blocks<E>(block_of(TPR) / TPR, n)); }
 };
 template <class E>
 hipError_t backward(const RmsGradArgs& a, hipStream_t s) {
@@ -583,8 +596,8 @@ hipError_t launch_rms_norm(const RmsArgs& a, int dtype, hipStream_t s) {
 
 int rms_norm_grad_strips(int k, int64_t rows, int64_t n, int dtype) {
   int strips = 0;
-  const bool fits = dtype == DW_BF16 ? for_row<Bf16, false, kWideGrad<Bf16>>(n, Strips<Bf16>{k, rows, &strips})
-                                     : for_row<F32, false, kWideGrad<F32>>(n, Strips<F32>{k, rows, &strips});
+  const bool fits = dtype == DW_BF16 ? for_row<Bf16, false, kWideGrad<Bf16>>(n, Strips<Bf16>{k, rows, n, &strips})
+                                     : for_row<F32, false, kWideGrad<F32>>(n, Strips<F32>{k, rows, n, &strips});
   return fits ? strips : (int)blocks_per_worker(k, rows, 1, 2 * kCus);
 }
 

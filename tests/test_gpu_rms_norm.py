@@ -180,6 +180,19 @@ def test_backward(n, dtype):
             assert torch.equal(got[0], dres) and torch.equal(got[1], dx) and torch.equal(got[2], dgamma)
 
 
+# rows of partial sums around the sixteen waves that add them up and the eight of each at a time; rows past one for every block
+@pytest.mark.parametrize("n", [70, 520, 4096])
+@pytest.mark.parametrize("rows", [1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 255, 256, 257, 400, 1100, 5000])
+def test_column_sums(rows, n):
+    """Whole numbers, whose sums are exact whatever their order."""
+    g = _gen(rows + n)
+    for dtype in (F32, BF16):
+        dy, h = (torch.randint(-8, 9, (2, rows, n), generator=g, device=DEV).to(dtype) for _ in range(2))
+        rstd = torch.exp2(torch.randint(-1, 2, (2, rows), generator=g, device=DEV).float())
+        dgamma = OPS.rms_norm_grad(dy, h, None, rstd)[2]
+        assert torch.equal(dgamma.double(), (dy.double() * h.double() * rstd.double()[..., None]).sum(1))
+
+
 def test_gradients_against_differences():
     """Quotients of differences of L = <dy, y> + <dh, h> in 64 bits, in directions for x, the residual and gamma."""
     g = _gen(9)
