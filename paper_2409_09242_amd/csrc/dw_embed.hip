@@ -15,7 +15,7 @@
 // places whose counts of every digit are added up between the two passes over them.
 //
 // Where the whole gradient is wanted, rows that no token has are filled with zeros beside the sort or beside the last sums.
-// Bound by writing them: 4 x 4096 rows of 4096, bf16, over 32000 tokens 377 us a call, 2.4 GB at 6.4 TB/s (a fill alone reaches 6.8);
+// Bound by writing them: 4 x 4096 rows of 4096, bf16, over 32000 tokens 374 us a call, 2.4 GB at 6.4 TB/s (a fill alone reaches 6.8);
 // added to a gradient that is there 119.  3 x 333 rows of 1001, fp32, over 5003: 20.0, three launches.  Lookups: 8 x 1024 rows of 4096,
 // fp32 to bf16, 31 us = 6.4 TB/s of what passes (common rows come from the caches); one row 2.0.
 #include "dw_ops.h"
@@ -350,7 +350,8 @@ struct SumArgs {
   float* part;                                             // [k][chunks][2][n]: of a token that came from the chunk before, and that goes on
   int64_t chunks;
   int log_tpr;                                             // threads of a chunk
-  int slices;                                              // parts of a row by so many pieces; one more for what is behind the whole pieces
+  int slices;                                              // parts of a row by so many pieces
+  int64_t piece_blocks;                                    // of a worker, for those; behind them the blocks for what is behind the whole pieces
   int log_join;                                            // threads of a row in the last kernel
   int64_t join_blocks;                                     // of a worker, in the last kernel; those behind them fill rows that no token has
   int fill_rows;                                           // of a block
@@ -441,7 +442,7 @@ __device__ __forceinline__ void fill_rows(const SumArgs& s, int w, int64_t v0, i
     if (!present[v - v0]) zero_floats(a.grad + w * a.grad_stride + v * a.grad_ld, a.n);
 }
 
-constexpr int kFewestThreads = 8;                          // of a chunk, so that a block's places fit its LDS
+constexpr int kLogFewest = 3, kFewestThreads = 1 << kLogFewest;                  // of a chunk, so that a block's places fit its LDS
 
 template <class E>
 __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
@@ -449,13 +450,16 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
   __shared__ __align__(16) int32_t key[CHUNKS * KEYS], place[CHUNKS * kChunk];
   const EmbedGradArgs& a = s.a;
   const int w = blockIdx.y;
-  const int slices = s.slices + (a.n % E::V ? 1 : 0), slice = blockIdx.x % slices;
-  const int t = threadIdx.x & ((1 << s.log_tpr) - 1), g = threadIdx.x >> s.log_tpr;
-  const int64_t c = (int64_t)(blockIdx.x / slices) * (256 >> s.log_tpr) + g, i0 = c * kChunk;
+  // the last blocks take the columns behind the whole pieces, fewest threads a chunk (4 x 16267 rows of 933, bf16: this
+  // kernel 38 us, with as many as the others take 55; rows of 936 36)
+  const bool behind = blockIdx.x >= s.piece_blocks;
+  const int log_tpr = behind ? kLogFewest : s.log_tpr, slice = behind ? 0 : blockIdx.x % s.slices;
+  const int t = threadIdx.x & ((1 << log_tpr) - 1), g = threadIdx.x >> log_tpr;
+  const int64_t c = (int64_t)(behind ? blockIdx.x - s.piece_blocks : blockIdx.x / s.slices) * (256 >> log_tpr) + g, i0 = c * kChunk;
   const int count = i0 + kChunk < a.rows ? kChunk : (int)(a.rows - i0);         // (not positive: no chunk)
   int32_t* my_key = key + g * KEYS + 4;
   int32_t* my_place = place + g * kChunk;
-  for (int i = t; i < kChunk + 2; i += 1 << s.log_tpr) {
+  for (int i = t; i < kChunk + 2; i += 1 << log_tpr) {
     const int64_t at = i0 + i - 1;
     my_key[i - 1] = at >= 0 && at < a.rows ? s.key[w * a.rows + at] : -1;
     if (i < kChunk) my_place[i] = i < count ? s.place[w * a.rows + i0 + i] : 0;
@@ -463,7 +467,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
   __syncthreads();
   if (count <= 0) return;
   const int64_t whole = a.n / E::V;
-  if (slice == s.slices) {
+  if (behind) {
     if (whole * E::V + t < a.n) sum_chunk<E, 1>(s, w, c, count, my_key, my_place, whole * E::V + t);
     return;
   }
@@ -552,9 +556,10 @@ hipError_t sums(SumArgs& s, hipStream_t stream) {
   const EmbedGradArgs& a = s.a;
   const int64_t whole = a.n / E::V;
   s.log_tpr = log_threads(whole);
-  if ((1 << s.log_tpr) < kFewestThreads) s.log_tpr = log_threads(kFewestThreads);
+  if (s.log_tpr < kLogFewest) s.log_tpr = kLogFewest;
   s.slices = (int)ceil_div(whole, 1 << s.log_tpr);
-  const int64_t blocks = ceil_div(s.chunks, 256 >> s.log_tpr) * (s.slices + (a.n % E::V ? 1 : 0));
+  s.piece_blocks = ceil_div(s.chunks, 256 >> s.log_tpr) * s.slices;
+  const int64_t blocks = s.piece_blocks + (a.n % E::V ? ceil_div(s.chunks, 256 / kFewestThreads) : 0);
   hipLaunchKernelGGL(embed_sum_kernel<E>, dim3((unsigned)blocks, (unsigned)a.k), dim3(256), 0, stream, s);
   return hipGetLastError();
 }
@@ -575,7 +580,7 @@ hipError_t launch_embedding_grad(const EmbedGradArgs& a, int dtype, hipStream_t 
   int32_t* place = reinterpret_cast<int32_t*>(a.scratch + lay.place);
   // The zeros: where at most a quarter of the rows can have a token, all rows beside the sort, page by page, and those few are written
   // once more; otherwise, where that would write up to all of them twice, at the end those that no token has, looked for one by one, at
-  // most 256 KB a block, and four blocks a compute unit where there are as many rows (4 x 4096 rows of 4096 over 32000, the whole call: 377
+  // most 256 KB a block, and four blocks a compute unit where there are as many rows (4 x 4096 rows of 4096 over 32000, the whole call: 374
   // us, the other way 434; 3 x 333 rows of 1001 over 5003: 20.0 and 20.8, and that 22.9 by 65 rows a block).
   const bool first = !a.accumulate && a.vocab / 4 >= a.rows, last = !a.accumulate && !first;
   const int64_t by_size = a.n >= 4096 ? 16 : a.n <= 256 ? 256 : 65536 / a.n, share = ceil_div(a.vocab * a.k, 4 * kCus);
