@@ -20,7 +20,7 @@ template <class E>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
   const int w = blockIdx.z, t = threadIdx.x & 15;
   const int64_t b = blockIdx.x;                             // block of 128 along the row
-  const int64_t r = (int64_t)blockIdx.y * 16 + (threadIdx.x >> 4);
+  const int64_t r = (int64_t)(a.first + blockIdx.y) * 16 + (threadIdx.x >> 4);
   const int64_t np = DW_FP8_ROW(a.n), ns = DW_FP8_SCALES(a.n);
   if (r >= a.rows) return;                                  // (16 lanes at once: those that exchange values stay together)
   const typename E::T* x = reinterpret_cast<const typename E::T*>(a.x.p) + w * a.x.stride + r * a.x.ld;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kTileThreads, NORM ? (E::V == 8 ? 8 : 6) : 1) void 
   if ((int)gridDim.z > a.k) {                               // few tiles: one block for each form
     if (w >= a.k) { w -= a.k; a.q = nullptr; } else a.qt = nullptr;
   }
-  const int64_t c0 = (int64_t)blockIdx.x * 128, r0 = (int64_t)blockIdx.y * 128;
+  const int64_t c0 = (int64_t)blockIdx.x * 128, r0 = (int64_t)(a.first + blockIdx.y) * 128;
   const int tc = threadIdx.x & 15, tr = threadIdx.x >> 4;   // this thread's 8 columns from 8 tc, 4 rows from 4 tr
   const int wave = threadIdx.x >> 6;
   const int64_t np = DW_FP8_ROW(a.n), ns = DW_FP8_SCALES(a.n), rp = DW_FP8_ROW(a.rows), rs = DW_FP8_SCALES(a.rows);
@@ -173,29 +173,44 @@ __global__ __launch_bounds__(kTileThreads, NORM ? (E::V == 8 ? 8 : 6) : 1) void 
   }
   if (threadIdx.x < 128 && c0 + threadIdx.x < a.n) {
     uint8_t* sc = a.scale_t + (w * a.n + c0 + threadIdx.x) * rs;
-    sc[blockIdx.y] = (uint8_t)mine.byte;
-    if (blockIdx.y == gridDim.y - 1)
-      for (int64_t q = blockIdx.y + 1; q < rs; ++q) sc[q] = 127;
+    const uint32_t b = a.first + blockIdx.y;
+    sc[b] = (uint8_t)mine.byte;
+    if (b == (uint32_t)(rp / 128) - 1)
+      for (int64_t q = b + 1; q < rs; ++q) sc[q] = 127;
   }
 }
 
-template <class E>
-hipError_t quantize(const QuantArgs& a, hipStream_t s) {
-  if (!a.square && !a.qt) {
-    const dim3 grid((unsigned)(DW_FP8_ROW(a.n) / 128), (unsigned)ceil_div(a.rows, 16), (unsigned)a.k);
-    hipLaunchKernelGGL(quantize_rows_kernel<E>, grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+// A grid has at most 65535 blocks along y: more blocks of `high` rows are several launches
+template <class F>
+hipError_t by_rows(QuantArgs a, int64_t high, F launch) {
+  constexpr uint32_t kMost = 65535;
+  const uint32_t blocks = (uint32_t)ceil_div(a.rows, high);
+  for (a.first = 0; a.first < blocks; a.first += kMost) {
+    launch(a, blocks - a.first < kMost ? blocks - a.first : kMost);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
+  return hipSuccess;
+}
+
+template <class E>
+hipError_t quantize(const QuantArgs& all, hipStream_t s) {
+  const unsigned columns = (unsigned)(DW_FP8_ROW(all.n) / 128);
+  if (!all.square && !all.qt)
+    return by_rows(all, 16, [&](const QuantArgs& a, unsigned blocks) {
+      hipLaunchKernelGGL(quantize_rows_kernel<E>, dim3(columns, blocks, (unsigned)a.k), dim3(256), 0, s, a);
+    });
   // Both forms of at most a tile a compute unit: a block for each form, which shares the work among twice as many (us, one
   // block for both and a block for each; 3 x 333 x 784 fp32, 63 tiles: 6.1, 5.1; 3 x 1000 x 784, 168: 7.1, 6.6; 1 x 64 x 4096 bf16,
   // 32: 5.5, 4.5; 2 x 1500 x 1500, 288: 10.3, 9.0 and in fp32 10.7, 11.2; 1 x 2048 x 4096, 512: 10.7, 10.3 and 12.8, 16.3)
-  const int64_t tiles = DW_FP8_ROW(a.n) / 128 * (DW_FP8_ROW(a.rows) / 128) * a.k;
-  const int forms = a.q && a.qt && tiles <= kCus ? 2 : 1;
-  const dim3 grid((unsigned)(DW_FP8_ROW(a.n) / 128), (unsigned)(DW_FP8_ROW(a.rows) / 128), (unsigned)(a.k * forms));
-  if (a.rstd) hipLaunchKernelGGL((quantize_tile_kernel<E, false, true>), grid, dim3(kTileThreads), 0, s, a);
-  else if (a.square) hipLaunchKernelGGL((quantize_tile_kernel<E, true, false>), grid, dim3(kTileThreads), 0, s, a);
-  else hipLaunchKernelGGL((quantize_tile_kernel<E, false, false>), grid, dim3(kTileThreads), 0, s, a);
-  return hipGetLastError();
+  const int64_t tiles = DW_FP8_ROW(all.n) / 128 * (DW_FP8_ROW(all.rows) / 128) * all.k;
+  const int forms = all.q && all.qt && tiles <= kCus ? 2 : 1;
+  return by_rows(all, 128, [&](const QuantArgs& a, unsigned blocks) {
+    const dim3 grid(columns, blocks, (unsigned)(a.k * forms));
+    if (a.rstd) hipLaunchKernelGGL((quantize_tile_kernel<E, false, true>), grid, dim3(kTileThreads), 0, s, a);
+    else if (a.square) hipLaunchKernelGGL((quantize_tile_kernel<E, true, false>), grid, dim3(kTileThreads), 0, s, a);
+    else hipLaunchKernelGGL((quantize_tile_kernel<E, false, false>), grid, dim3(kTileThreads), 0, s, a);
+  });
 }
 
 }  // namespace

@@ -268,6 +268,7 @@ struct QuantArgs {
   uint8_t* qt; uint8_t* scale_t;                           // [k][n][DW_FP8_ROW(rows)], [k][n][DW_FP8_SCALES(rows)], or nullptr
   const float* rstd;                                       // [k][rows]: the numbers are x rstd gamma (x alone where nullptr)
   const float* gamma; int64_t gamma_stride;                // [k] rows of n, or nullptr: 1
+  uint32_t first;                                          // a launch's first block along the rows (0 from the caller)
 };
 hipError_t launch_fp8_quantize(const QuantArgs& a, int dtype, hipStream_t s);
 
