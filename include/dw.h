@@ -417,7 +417,7 @@ int dw_fp8_linear(const void* d_x, int64_t x_ld, int64_t x_stride, const uint8_t
  *   d_grad      [k][vocab] rows of n floats.  accumulate 0: every row is written, zeros where no token was; 1: the sums are added
  *               to the rows of the tokens that are there, and the others are not touched
  * The gradient takes up to 2^27 rows and 2^36 numbers of dy a worker; more return DW_ERR_TOO_LARGE.
- * The rows of a token are added in fp32, in an order that follows from the tokens alone: no atomics.  (Of a table that the workers
+ * The rows of a token are added in fp32, in an order that follows from the tokens and n alone: no atomics.  (Of a table that the workers
  * share, table_stride 0, each worker's gradient is its own part; their sum is the table's.)
  */
 int dw_embedding(const int32_t* d_token, const void* d_table, int64_t table_ld, int64_t table_stride, int table_dtype, int k,
@@ -447,7 +447,8 @@ int dw_dropout(const void* d_x, int64_t x_ld, int64_t x_stride, const void* d_re
 /*
  * Root-mean-square norm behind the residual's addition:
  *   h = residual + dropout(x)  (dw_dropout's, in `dtype`),    y = h r gamma,    r = 1/sqrt(mean(h^2) + eps) over a row of n
- * where h is what is stored, rounded to `dtype`: what the norm's backward pass reads is what it was the norm of.
+ * where h is what is stored, rounded to `dtype`: what the norm's backward pass reads is what it was the norm of.  Squares are added in
+ * fp32: a row whose sum of squares passes 3.4e38 has r = 0, and with eps = 0 one whose mean square vanishes r = infinity.
  *   d_residual, p ... d_step   as for dw_dropout; NULL and 0: h is x, and d_h may be NULL too
  *   d_gamma     [k] rows of n floats, worker w's at w*param_stride; NULL: 1
  *   d_h         NULL: not wanted.  May be d_x or d_residual itself (same ld and stride)
@@ -497,6 +498,7 @@ int dw_rms_norm_grad(const void* d_dy, int64_t dy_ld, int64_t dy_stride, const v
  *                 mask_stride (in words) may be 0
  *   d_out         may be d_logits itself (same ld and stride)
  * An element that nothing of this applies to is handed on as it is.  A row whose mask allows nothing is -inf throughout.
+ * z / repetition is z times the rounded reciprocal: a magnitude of the repetition from 2^-126 to 2^126 costs no more than that rounding.
  */
 #define DW_MAX_HISTORY (1 << 24)
 int dw_adjust_logits(const void* d_logits, int64_t ld, int64_t stride, const int32_t* d_history, int64_t history_ld,

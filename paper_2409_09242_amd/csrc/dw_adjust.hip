@@ -6,7 +6,8 @@
 // prompt" (whole numbers: the order of the additions does not matter), and then goes over the logits.  Bound by memory, the logits in
 // and out; the blocks of a row read its history from the caches.  8 x 64 rows of 131072, bf16, histories of up to 2048, bias and mask:
 // 65 us = 4.3 TB/s (a copy 4.75; without a history 49 to 55: the two barriers around the counts are what is left of it); fp32 98.  Four rows
-// of 32000 with histories of 300: 5.3 us, two trips to memory and the barriers.
+// of 32000 with histories of 300: 5.3 us, two trips to memory and the barriers.  Every block of a row goes over all of its history, a piece of four
+// tokens a thread on its way at a time: 63 us with histories of up to 300 and of up to 2048, 76 of up to 8192 (fp32 98 and 120), 84 where all 8192 count.
 #include "dw_ops.h"
 
 namespace dw {

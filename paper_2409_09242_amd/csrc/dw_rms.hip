@@ -19,7 +19,9 @@
 // Bound by memory (a copy reaches 4.75 TB/s, two reads a write 5.9; what is still in the chip's cache comes on top): forward 16 x 512 rows
 // of 4096, bf16, with a residual 43 us = 6.2 TB/s, its 8-bit form with dropout, 8 x 1024 x 4096, 43 us = 5.4 and 20 for the transposed
 // form; backward 3 x 2731 rows of 5003, fp32, with a gradient from further on and a dropout's own output 157 us = 5.2 TB/s, and 5 for the
-// columns' sums.  One row 3.7 us.  Rows that registers do not hold: above 32768 columns forward 3.9 TB/s, backward (in bf16 above 16384) 2.3.
+// columns' sums.  One row 3.7 us.  Registers hold rows of up to 4096 pieces of 16 bytes, in the backward pass of bf16 2048, and fewer elements
+// behind them than a piece: bf16 forward to 32775 columns (32768 in 8 bits) and backward to 16391, fp32 both to 16387 (16384).  Of longer
+// rows the forward pass reads h, or x, a second time (3.7 to 4.3 TB/s of the formulas' bytes), the backward pass dy and h three times (1.8 to 2.3).
 #include "dw_dropout.h"
 #include "dw_fp8.h"
 
@@ -126,7 +128,7 @@ __device__ __forceinline__ float as_stored_one(float f) {
 }
 
 // this thread's number, for the row at hand: what follows from it alone would otherwise be worked out once and take registers throughout
-// (1024 threads with four pieces, backward: 66 of them in memory, so 32)
+// (1024 threads with four pieces, fp32, backward: 66 of them in memory, so 32.  Forward in bf16 with four 27, backward with two 8, the others none)
 __device__ __forceinline__ int anew(int t) {
   asm volatile("" : "+v"(t));
   return t;
